@@ -364,6 +364,97 @@ ssg_status ssg_adam_step_wait(const ssg_adam_desc *desc, const void *grad, float
 /* pointers into `state` as left by step `step` (0 = after ssg_adam_init) */
 ssg_status ssg_adam_view_state(int64_t n, int32_t step, const void *state, ssg_adam_state_view *out);
 
+/* ---- routing to experts, and experts in 8-bit integers -------------------------
+ * A mixture of the block's MLPs: a router sends every token to k of E experts.  The entry points below take any number of tokens or rows,
+ * also none (nothing is launched then, but for the counts and offsets of ssg_route; the addresses of empty tensors may be NULL).
+ *
+ * Token t's score of expert e from the router's logits z = logits[t,:] is softmax(z)_e, or 1 / (1 + e^-z_e).  Experts are
+ * chosen by key: z_e itself, or with a balance bias b the sum fl32(score_e + b_e).  With groups > 1 the E experts are that many
+ * groups of neighbours, of which only the top_groups best stay: a group counts by its best key (group_top = 1) or by the sum of
+ * its two best scores, with the bias where there is one (group_top = 2; what it has, if that is one).  Then the k largest keys are
+ * chosen, in descending order; ties go to the lower index.  The weights are scale * score_e, with renorm = 1
+ * divided by the sum of the chosen scores; the bias enters the choice only.
+ * An expert whose logit is -inf or NaN, or whose biased key is, is closed to the token (a closed one has score 0); +inf counts as the largest finite
+ * number.  Where fewer than k experts are open the last ids are -1 and their weights 0: a row of -inf is a padding token.
+ *
+ * The order of dispatch: assignment a = t * k + j, sorted by expert and by a within one; each expert's rows start at a multiple of
+ * row_align.  counts[e]: rows of expert e; offsets[e]: its first row, offsets[E] the end of the last; place[a]: the row of an
+ * assignment, -1 for id -1; source[row]: the assignment of a row, -1 for rows that only fill up, of ssg_route_rows(desc) rows.
+ * No atomics decide an order: results are the same bits in every call. */
+typedef enum { SSG_ROUTE_SOFTMAX = 0, SSG_ROUTE_SIGMOID = 1 } ssg_route_score;
+typedef struct {
+    int64_t T;               /* tokens, T * k up to 2^26 */
+    int64_t ld;              /* elements from one token's logits to the next, at least E */
+    int32_t E, k;            /* up to 1024 experts, up to 32 chosen */
+    int32_t logits_dtype;    /* ssg_dtype */
+    int32_t score;           /* ssg_route_score */
+    int32_t groups, top_groups;   /* groups divides E, up to 64; 1, 1: no groups.  The groups that stay hold at least k experts */
+    int32_t group_top;       /* 1 or 2 */
+    int32_t renorm;          /* 0 or 1 */
+    float scale;
+    int32_t row_align;       /* a power of two up to 256 */
+    int32_t reserved[2];     /* must be 0 */
+} ssg_route_desc;
+size_t ssg_route_workspace_bytes(const ssg_route_desc *desc);
+int64_t ssg_route_rows(const ssg_route_desc *desc);      /* most rows that dispatch can need: the extent of source; < 0: a status */
+/* logits [T,E], ld apart, aligned to an element; bias [E] or NULL; ids, weights [T,k]; counts [E], offsets [E+1], place [T*k], source
+ * [ssg_route_rows]: all of them, or all NULL (choice and weights only; no workspace needed). */
+ssg_status ssg_route(const ssg_route_desc *desc, const void *logits, const float *bias, int32_t *ids, float *weights, int32_t *counts,
+                     int32_t *offsets, int32_t *place, int32_t *source, void *workspace, size_t workspace_bytes, void *stream);
+/* The gradient of sum(weights * dweights) with respect to the logits, the choice held constant.  ids, weights as ssg_route left
+ * them; dweights [T,k] fp32 (entries of id -1 are not read into the sum); dlogits out [T,E] contiguous, of the logits' type. */
+ssg_status ssg_route_bwd(const ssg_route_desc *desc, const void *logits, const int32_t *ids, const float *weights, const float *dweights,
+                         void *dlogits, void *stream);
+
+/* Rows in 8-bit integers with a scale each -- tokens of activations, channels of weights:
+ *     scale_r = fl32(amax_r / 127),  code = round to nearest even(fl32(x fl32(127 / amax_r)))
+ * (scale at least 2^-126, with 2^126 as the factor there; a row of zeros has scale 0; one with a NaN or an infinity a NaN, and codes 0).
+ * They live in a buffer of ssg_i8_bytes(rows, K) bytes, 256-byte aligned, in the layout that the products read: blocks of 16 rows by 64
+ * codes, 1 KB each, code (r, k) at byte ((r / 16) * (Kp / 64) + k / 64) * 1024 + (k % 64 / 16) * 256 + r % 16 * 16 + k % 16
+ * with Kp = K filled up to 64 by zeros; at the next multiple of 256 bytes the scales, rows filled up to 16.  rows up to 2^26, K a
+ * multiple of 16 up to 131056 (sums stay exact in 32 bits for all codes from -128 to 127).
+ * ssg_i8_quantize: from rows of src, ld elements apart, rows on 16 bytes.  ssg_i8_pack: from codes [rows,K] and scales [rows]
+ * that a program has already; ssg_i8_unpack the way back. */
+size_t ssg_i8_bytes(int64_t rows, int64_t K);
+ssg_status ssg_i8_quantize(const void *src, ssg_dtype src_dtype, int64_t rows, int64_t K, int64_t ld, void *q, size_t q_bytes, void *stream);
+ssg_status ssg_i8_pack(const int8_t *codes, const float *scales, int64_t rows, int64_t K, void *q, size_t q_bytes, void *stream);
+ssg_status ssg_i8_unpack(const void *q, size_t q_bytes, int64_t rows, int64_t K, int8_t *codes, float *scales, void *stream);
+/* C[m,n] = (sum_k a[m,k] b[n,k]) sa[m] sb[n]: the sum exact, then fl32(fl32(fl32(sum) sa) sb).  A: M rows, any number; B: N
+ * rows, a multiple of 16; C rows ldc elements apart, on 16 bytes. */
+ssg_status ssg_i8_gemm(const void *A, size_t A_bytes, int64_t M, const void *B, size_t B_bytes, int64_t N, int64_t K, void *C,
+                       ssg_dtype c_dtype, int64_t ldc, void *stream);
+/* y = x W^T with x quantized in the call, a scale for each token: ssg_i8_quantize and ssg_i8_gemm.  W: N rows of K. */
+size_t ssg_i8_linear_workspace_bytes(int64_t M, int64_t K);
+ssg_status ssg_i8_linear(const void *x, ssg_dtype x_dtype, int64_t M, int64_t K, int64_t ldx, const void *W, size_t W_bytes, int64_t N,
+                         void *y, ssg_dtype y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The mixture's forward: routing, then with every expert's own W1, W2 [f,d] and W3 [d,f] in 8-bit integers
+ *     h = (x w1)(Swish(x w2)) in bf16, quantized with a scale for each token;  o = h w3^T in y's type
+ *     y_t = sum_j weights[t,j] o[place[t,j]]  in fp32, in the order of j
+ * W1, W2: buffers of E*f rows of K = d, expert e's rows from e*f; W3: E*d rows of K = f.  x [T,d] bf16; y [T,d] of y_dtype.  d, f
+ * multiples of 16.  A token without an open expert gets zeros.  Inference only: the integer products have no gradient. */
+typedef struct {
+    ssg_route_desc route;    /* row_align must be 16 */
+    int64_t d, f;
+    int32_t y_dtype;
+    int32_t reserved[3];     /* must be 0 */
+} ssg_moe_desc;
+size_t ssg_moe_workspace_bytes(const ssg_moe_desc *desc);
+ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logits, const float *bias, const void *W1, size_t W1_bytes,
+                       const void *W2, size_t W2_bytes, const void *W3, size_t W3_bytes, void *y, void *workspace, size_t workspace_bytes,
+                       void *stream);
+/* Pointers into `workspace` after a call, for tests and reports. */
+typedef struct {
+    int64_t rows;                        /* rows of x_q, h, h_q and o; those from offsets[E] on are not written */
+    const int32_t *ids;
+    const float *weights;
+    const int32_t *counts, *offsets, *place, *source;
+    const void *x_q, *h_q;               /* quantized rows of K = d and K = f */
+    const void *h;                       /* bf16 [rows, f] */
+    const void *o;                       /* [rows, d] of y_dtype */
+} ssg_moe_workspace_view;
+ssg_status ssg_moe_view_workspace(const ssg_moe_desc *desc, const void *workspace, ssg_moe_workspace_view *out);
+
 /* ---- kernel timing for benchmarks (optional) --------------------------------
  * The one piece of state the library keeps, off by default.  While enabled, every kernel launch of the
  * library is bracketed by two HIP events recorded on the launch's own stream (events are host objects; no
@@ -387,7 +478,9 @@ ssg_status ssg_adam_view_state(int64_t n, int32_t step, const void *state, ssg_a
  * of the SwiGLU product from bf16 U, G with per-channel factors, 43 = cast of W3 with the inverse factors folded
  * in, 44 = per-column range, 45 = small bookkeeping kernels (resets, factors, history update), 46 = bf16 transposes
  * (w3_layer_bf16 = 1), 47 = the passes of 42 and 43 in one launch.
- * Adam: 32 = range pass, 33 = update pass. */
+ * Adam: 32 = range pass, 33 = update pass.
+ * Experts: 48 = choice (and with few tokens the dispatch), 49 = dispatch, 50 = gradient of the weights, 51 = weighted sum of the experts'
+ * rows, 52 = quantization of rows in 8-bit integers; 53 = their products and 54 = the gate/up form (bytes = 0). */
 ssg_status ssg_profile_enable(int max_records);
 ssg_status ssg_profile_select(int tag);
 int ssg_profile_read(float *ms, int *tags, double *bytes, int cap);

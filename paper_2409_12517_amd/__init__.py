@@ -28,6 +28,7 @@ SSG_E4M3, SSG_E5M2 = 0, 1
 SSG_BF16, SSG_F32 = 0, 1
 SSG_SCALE_CURRENT, SSG_SCALE_GIVEN, SSG_SCALE_DELAYED = 0, 1, 2
 SSG_ROUND_EXACT_DIV, SSG_ROUND_POW2 = 0, 1
+SSG_ROUTE_SOFTMAX, SSG_ROUTE_SIGMOID = 0, 1
 
 EXPORTS = [
     "ssg_last_error", "ssg_version", "ssg_amax", "ssg_quantize", "ssg_quantize_wait", "ssg_gemm_fp8", "ssg_gemm_fp8_layout", "ssg_gemm_fp8_plan", "ssg_swiglu",
@@ -37,6 +38,9 @@ EXPORTS = [
     "ssg_infer_prepared_bytes", "ssg_infer_workspace_bytes", "ssg_infer_prepare", "ssg_infer_fwd", "ssg_infer_view",
     "ssg_infer_noalloc_max_bytes", "ssg_infer_fwd_noalloc",
     "ssg_adam_state_bytes", "ssg_adam_init", "ssg_adam_step", "ssg_adam_step_wait", "ssg_adam_view_state",
+    "ssg_route_workspace_bytes", "ssg_route_rows", "ssg_route", "ssg_route_bwd",
+    "ssg_i8_bytes", "ssg_i8_quantize", "ssg_i8_pack", "ssg_i8_unpack", "ssg_i8_gemm", "ssg_i8_linear_workspace_bytes", "ssg_i8_linear",
+    "ssg_moe_workspace_bytes", "ssg_moe_fwd", "ssg_moe_view_workspace",
     "ssg_profile_enable", "ssg_profile_select", "ssg_profile_read",
 ]
 
@@ -73,6 +77,21 @@ class ssg_adam_desc(Structure):
 
 class ssg_adam_state_view(Structure):
     _fields_ = [(n, c_void_p) for n in ("m_q", "v_q", "scales")]
+
+
+class ssg_route_desc(Structure):
+    _fields_ = [("T", c_int64), ("ld", c_int64)] + [(n, c_int32) for n in (
+        "E", "k", "logits_dtype", "score", "groups", "top_groups", "group_top", "renorm")] + [
+        ("scale", c_float), ("row_align", c_int32), ("reserved", c_int32 * 2)]
+
+
+class ssg_moe_desc(Structure):
+    _fields_ = [("route", ssg_route_desc), ("d", c_int64), ("f", c_int64), ("y_dtype", c_int32), ("reserved", c_int32 * 3)]
+
+
+class ssg_moe_workspace_view(Structure):
+    _fields_ = [("rows", c_int64)] + [(n, c_void_p) for n in (
+        "ids", "weights", "counts", "offsets", "place", "source", "x_q", "h_q", "h", "o")]
 
 
 class ssg_mlp_saved_view(Structure):
@@ -134,9 +153,29 @@ _lib.ssg_adam_init.argtypes = [c_int64, c_void_p, c_void_p]
 _lib.ssg_adam_step.argtypes = [POINTER(ssg_adam_desc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
 _lib.ssg_adam_step_wait.argtypes = [POINTER(ssg_adam_desc), c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p]
 _lib.ssg_adam_view_state.argtypes = [c_int64, c_int32, c_void_p, POINTER(ssg_adam_state_view)]
+_lib.ssg_route_workspace_bytes.argtypes = [POINTER(ssg_route_desc)]
+_lib.ssg_route_workspace_bytes.restype = c_size_t
+_lib.ssg_route_rows.argtypes = [POINTER(ssg_route_desc)]
+_lib.ssg_route.argtypes = [POINTER(ssg_route_desc)] + [c_void_p] * 9 + [c_size_t, c_void_p]
+_lib.ssg_route_bwd.argtypes = [POINTER(ssg_route_desc)] + [c_void_p] * 6
+_lib.ssg_i8_bytes.argtypes = [c_int64, c_int64]
+_lib.ssg_i8_bytes.restype = c_size_t
+_lib.ssg_i8_quantize.argtypes = [c_void_p, c_int, c_int64, c_int64, c_int64, c_void_p, c_size_t, c_void_p]
+_lib.ssg_i8_pack.argtypes = [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_size_t, c_void_p]
+_lib.ssg_i8_unpack.argtypes = [c_void_p, c_size_t, c_int64, c_int64, c_void_p, c_void_p, c_void_p]
+_lib.ssg_i8_gemm.argtypes = [c_void_p, c_size_t, c_int64, c_void_p, c_size_t, c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p]
+_lib.ssg_i8_linear_workspace_bytes.argtypes = [c_int64, c_int64]
+_lib.ssg_i8_linear_workspace_bytes.restype = c_size_t
+_lib.ssg_i8_linear.argtypes = [c_void_p, c_int, c_int64, c_int64, c_int64, c_void_p, c_size_t, c_int64, c_void_p, c_int, c_int64,
+                               c_void_p, c_size_t, c_void_p]
+_lib.ssg_moe_workspace_bytes.argtypes = [POINTER(ssg_moe_desc)]
+_lib.ssg_moe_workspace_bytes.restype = c_size_t
+_lib.ssg_moe_fwd.argtypes = [POINTER(ssg_moe_desc)] + [c_void_p] * 3 + [c_void_p, c_size_t] * 3 + [c_void_p, c_void_p, c_size_t, c_void_p]
+_lib.ssg_moe_view_workspace.argtypes = [POINTER(ssg_moe_desc), c_void_p, POINTER(ssg_moe_workspace_view)]
 for _n in EXPORTS[2:]:
     if not _n.endswith("_bytes"):          # the size queries return size_t, everything else a status
         getattr(_lib, _n).restype = c_int
+_lib.ssg_route_rows.restype = c_int64
 
 
 class SsgError(RuntimeError):
@@ -380,6 +419,82 @@ def ssg_adam_step_wait(desc, grad, w, w_bf16, state, polls, stream=None) -> None
 def ssg_adam_view_state(n: int, step: int, state) -> ssg_adam_state_view:
     v = ssg_adam_state_view()
     _check(_lib.ssg_adam_view_state(n, step, _ptr(state), ctypes.byref(v)))
+    return v
+
+
+def make_route_desc(T, E, k, ld=None, logits_dtype=SSG_F32, score=SSG_ROUTE_SOFTMAX, groups=1, top_groups=1, group_top=1, renorm=1,
+                    scale=1.0, row_align=16) -> ssg_route_desc:
+    return ssg_route_desc(T, E if ld is None else ld, E, k, logits_dtype, score, groups, top_groups, group_top, renorm, scale, row_align,
+                          (c_int32 * 2)(0, 0))
+
+
+def ssg_route_workspace_bytes(desc) -> int:
+    return int(_lib.ssg_route_workspace_bytes(ctypes.byref(desc)))
+
+
+def ssg_route_rows(desc) -> int:
+    rows = _lib.ssg_route_rows(ctypes.byref(desc))
+    if rows < 0:
+        raise SsgError(rows, ssg_last_error())
+    return rows
+
+
+def ssg_route(desc, logits, bias, ids, weights, counts, offsets, place, source, workspace, stream=None, workspace_bytes=None) -> None:
+    _check(_lib.ssg_route(ctypes.byref(desc), _ptr(logits), _ptr(bias), _ptr(ids), _ptr(weights), _ptr(counts), _ptr(offsets), _ptr(place),
+                          _ptr(source), _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def ssg_route_bwd(desc, logits, ids, weights, dweights, dlogits, stream=None) -> None:
+    _check(_lib.ssg_route_bwd(ctypes.byref(desc), _ptr(logits), _ptr(ids), _ptr(weights), _ptr(dweights), _ptr(dlogits), _stream(stream)))
+
+
+def ssg_i8_bytes(rows: int, K: int) -> int:
+    return int(_lib.ssg_i8_bytes(rows, K))
+
+
+def ssg_i8_quantize(src, src_dtype, rows, K, ld, q, stream=None, q_bytes=None) -> None:
+    _check(_lib.ssg_i8_quantize(_ptr(src), src_dtype, rows, K, ld, _ptr(q), _nbytes(q, q_bytes), _stream(stream)))
+
+
+def ssg_i8_pack(codes, scales, rows, K, q, stream=None, q_bytes=None) -> None:
+    _check(_lib.ssg_i8_pack(_ptr(codes), _ptr(scales), rows, K, _ptr(q), _nbytes(q, q_bytes), _stream(stream)))
+
+
+def ssg_i8_unpack(q, rows, K, codes, scales, stream=None, q_bytes=None) -> None:
+    _check(_lib.ssg_i8_unpack(_ptr(q), _nbytes(q, q_bytes), rows, K, _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+def ssg_i8_gemm(A, M, B, N, K, C, c_dtype, ldc, stream=None, A_bytes=None, B_bytes=None) -> None:
+    _check(_lib.ssg_i8_gemm(_ptr(A), _nbytes(A, A_bytes), M, _ptr(B), _nbytes(B, B_bytes), N, K, _ptr(C), c_dtype, ldc, _stream(stream)))
+
+
+def ssg_i8_linear_workspace_bytes(M: int, K: int) -> int:
+    return int(_lib.ssg_i8_linear_workspace_bytes(M, K))
+
+
+def ssg_i8_linear(x, x_dtype, M, K, ldx, W, N, y, y_dtype, ldy, workspace, stream=None, W_bytes=None, workspace_bytes=None) -> None:
+    _check(_lib.ssg_i8_linear(_ptr(x), x_dtype, M, K, ldx, _ptr(W), _nbytes(W, W_bytes), N, _ptr(y), y_dtype, ldy, _ptr(workspace),
+                              _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def make_moe_desc(route: ssg_route_desc, d: int, f: int, y_dtype: int = SSG_BF16) -> ssg_moe_desc:
+    return ssg_moe_desc(route, d, f, y_dtype, (c_int32 * 3)(0, 0, 0))
+
+
+def ssg_moe_workspace_bytes(desc) -> int:
+    return int(_lib.ssg_moe_workspace_bytes(ctypes.byref(desc)))
+
+
+def ssg_moe_fwd(desc, x, logits, bias, W1, W2, W3, y, workspace, stream=None, W1_bytes=None, W2_bytes=None, W3_bytes=None,
+                workspace_bytes=None) -> None:
+    _check(_lib.ssg_moe_fwd(ctypes.byref(desc), _ptr(x), _ptr(logits), _ptr(bias), _ptr(W1), _nbytes(W1, W1_bytes), _ptr(W2),
+                            _nbytes(W2, W2_bytes), _ptr(W3), _nbytes(W3, W3_bytes), _ptr(y), _ptr(workspace),
+                            _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def ssg_moe_view_workspace(desc, workspace) -> ssg_moe_workspace_view:
+    v = ssg_moe_workspace_view()
+    _check(_lib.ssg_moe_view_workspace(ctypes.byref(desc), _ptr(workspace), ctypes.byref(v)))
     return v
 
 

@@ -5,7 +5,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -13,20 +12,18 @@
 #include <vector>
 
 #include "../../include/ssg.h"
+#include "ssg_check.h"
 #include "ssg_device.h"
 #include "ssg_internal.h"
 
-namespace {
-
-thread_local char g_err[512] = "";
-
-ssg_status fail(ssg_status code, const char *fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_err, sizeof(g_err), fmt, ap);
-    va_end(ap);
-    return code;
+namespace ssg {
+char *error_text() {
+    static thread_local char text[kErrorText] = "";
+    return text;
 }
+}  // namespace ssg
+
+namespace {
 
 // Grouped launches of the backward GEMMs are on unless the environment says SSG_GEMM_GROUPING=0 (read once; a
 // switch for A/B timing, the results are the same either way).
@@ -103,49 +100,12 @@ int dw3_split_sets(const ssg::GemmArgs &dh, const ssg::GemmArgs &dw3, const ssg:
     return split;
 }
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool extent_ok(int64_t v) { return v > 0 && (v % 16) == 0; }
 constexpr int64_t kMaxElems = (int64_t)1 << 32;   // kernels address operand tiles with 32-bit byte offsets
 
-ssg_status check_launch(const char *what) {
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return fail(SSG_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-    return SSG_OK;
-}
-
-// An error some earlier HIP call of the process left behind would otherwise be reported as this entry
-// point's own launch failure: it is read (which clears it) and reported before anything is enqueued.
-ssg_status check_entry(const char *what) {
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess)
-        return fail(SSG_ERR_HIP, "%s: a HIP error was already pending on entry (%s); nothing was launched", what,
-                    hipGetErrorString(e));
-    return SSG_OK;
-}
-
-#define SSG_REQUIRE_PTR(p)                                                                     \
-    do {                                                                                       \
-        if ((p) == nullptr) return fail(SSG_ERR_ARG, "%s: %s is NULL", __func__, #p);          \
-        if (!aligned16(p)) return fail(SSG_ERR_ARG, "%s: %s is not 16-byte aligned", __func__, #p); \
-    } while (0)
-#define SSG_OPTIONAL_PTR(p)                                                                    \
-    do {                                                                                       \
-        if ((p) != nullptr && !aligned16(p))                                                   \
-            return fail(SSG_ERR_ARG, "%s: %s is not 16-byte aligned", __func__, #p);           \
-    } while (0)
-#define SSG_REQUIRE_SCALAR_PTR(p)                                                              \
-    do {                                                                                       \
-        if ((p) == nullptr) return fail(SSG_ERR_ARG, "%s: %s is NULL", __func__, #p);          \
-        if (reinterpret_cast<uintptr_t>(p) & 3u)                                               \
-            return fail(SSG_ERR_ARG, "%s: %s is not 4-byte aligned", __func__, #p);            \
-    } while (0)
-
 ssg::SrcKind src_kind(ssg_dtype dt) { return dt == SSG_BF16 ? ssg::SRC_BF16 : ssg::SRC_F32; }
-bool dtype_ok(int dt) { return dt == SSG_BF16 || dt == SSG_F32; }
 bool fmt_ok(int f) { return f == SSG_E4M3 || f == SSG_E5M2; }
 
 // ---- buffer layouts -----------------------------------------------------------
-size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 struct SavedLayout {
     size_t scalars, partials, s, sinv, h_camax, w3_camax, x_q, w1_q, w2_q, U, G, h_q, w3_q, h_b, h_bT, w3T, total;
@@ -571,7 +531,7 @@ ssg_status ssg_adam_view_state(int64_t n, int32_t step, const void *state, ssg_a
     return SSG_OK;
 }
 
-const char *ssg_last_error(void) { return g_err; }
+const char *ssg_last_error(void) { return ssg::error_text(); }
 const char *ssg_version(void) { return "ssg 0.1 (gfx950)"; }
 
 ssg_status ssg_amax(const void *src, ssg_dtype src_dtype, size_t n, float *amax_dev, void *stream) {

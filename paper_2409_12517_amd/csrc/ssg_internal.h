@@ -264,4 +264,73 @@ size_t adam_scalar_words();
 void launch_adam_init(uint32_t *scalars, uint8_t *codes, size_t code_bytes, hipStream_t st);
 void launch_adam_step(const AdamArgs &a, hipStream_t st);
 
+// ---- routing to experts (ssg_route.hip) --------------------------------------------
+struct RouteArgs {
+    const void *logits = nullptr;    // [T, E], `ld` elements from one token's to the next
+    const float *bias = nullptr;     // [E] or null
+    int *ids = nullptr;              // [T, k]
+    float *weights = nullptr;        // [T, k]
+    int *counts = nullptr, *offsets = nullptr, *place = nullptr, *source = nullptr;   // all or none (place decides)
+    uint32_t *hist = nullptr;        // route_hist_words() words
+    int64_t T = 0, ld = 0, rows = 0;
+    int E = 0, k = 0, bf16 = 0, score = 0, groups = 1, top_groups = 1, group_top = 1, renorm = 0, align = 1;
+    float scale = 1.0f;
+    int block_tokens = 0, lds_keys = 0;     // filled in by the launcher
+};
+struct RouteBwdArgs {
+    const void *logits = nullptr;
+    const int *ids = nullptr;
+    const float *weights = nullptr, *dweights = nullptr;
+    void *dlogits = nullptr;         // [T, E], of the logits' type
+    int64_t T = 0, ld = 0;
+    int E = 0, k = 0, bf16 = 0, score = 0, renorm = 0;
+    float scale = 1.0f;
+};
+struct CombineArgs {
+    const void *o = nullptr;         // rows of d, fp32 (f32 = 1) or bf16
+    void *y = nullptr;               // [T, d] of the same type
+    const int *place = nullptr;      // [T, k]
+    const float *weights = nullptr;
+    int64_t T = 0, d = 0;
+    int k = 0, f32 = 0;
+};
+constexpr int kMaxExperts = 1024, kMaxChosen = 32, kMaxGroups = 64;
+size_t route_hist_words(const RouteArgs &a);
+void launch_route(RouteArgs a, hipStream_t st);
+void launch_route_bwd(const RouteBwdArgs &a, hipStream_t st);
+void launch_combine(const CombineArgs &a, hipStream_t st);
+
+// ---- products in 8-bit integers (ssg_i8_rows.hip, ssg_i8_gemm.hip) --------------------
+// Codes lie in blocks of 16 rows by 64 codes of K, 1 KB each, a row of blocks after the other, K filled up with zeros to 64:
+// code (r, k) at ((r / 16) * (Kp / 64) + k / 64) * 1024 + (k % 64 / 16) * 256 + (r % 16) * 16 + k % 16, which is the order in which
+// the 64 lanes of a wave hold the operand of v_mfma_i32_16x16x64_i8, 16 bytes each.  Behind them the rows' scales, one float each, for
+// the rows filled up to 16.
+constexpr int64_t i8_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+constexpr int64_t i8_code_bytes(int64_t rows, int64_t K) { return i8_up(rows, 16) * i8_up(K, 64); }
+struct I8RowsArgs {
+    const void *src = nullptr;       // rows of K, `ld` elements apart
+    uint8_t *codes = nullptr;
+    float *scales = nullptr;
+    int64_t rows = 0, K = 0, ld = 0; // rows of the result
+    int bf16 = 0;
+    const int *source = nullptr;     // row r is src row source[r] / k, or zeros where source[r] < 0; null: row r
+    const int *live_rows = nullptr;  // device: rows from here on are left alone; null: all rows
+    int k = 1;
+};
+void launch_i8_quantize(const I8RowsArgs &a, hipStream_t st);
+void launch_i8_pack(const int8_t *codes, const float *scales, int64_t rows, int64_t K, uint8_t *out, float *out_scales, hipStream_t st);
+void launch_i8_unpack(const uint8_t *in, const float *in_scales, int64_t rows, int64_t K, int8_t *codes, float *scales, hipStream_t st);
+struct I8GemmArgs {
+    const uint8_t *A = nullptr, *B = nullptr, *B2 = nullptr;      // laid-out codes; B2: the Swish branch's weights (SwiGLU form)
+    const float *sa = nullptr, *sb = nullptr, *sb2 = nullptr;
+    void *C = nullptr;
+    int64_t M = 0, N = 0, K = 0, ldc = 0;     // N: columns of the result (of one expert)
+    int c_f32 = 0;
+    const int *offsets = nullptr;    // device [E + 1], multiples of 16: expert e's rows; its weights are rows e N .. of B.  null: one expert
+    int E = 1;
+    int64_t rows_expected = 0;       // with offsets: rows that tokens fill, of M
+};
+void launch_i8_gemm(const I8GemmArgs &a, hipStream_t st);
+constexpr int kTagRoute = 48, kTagDispatch = 49, kTagRouteBwd = 50, kTagCombine = 51, kTagI8Rows = 52, kTagI8Gemm = 53, kTagI8Swiglu = 54;
+
 }  // namespace ssg

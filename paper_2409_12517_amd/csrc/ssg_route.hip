@@ -1,0 +1,570 @@
+// Routing to experts: a token's scores, the experts it is sent to and their weights; the order in which the experts' products
+// take the rows; the gradient of the weights with respect to the logits; and the weighted sum of the experts' results.
+//
+//   s_e = softmax(z)_e or 1 / (1 + e^-z_e)         over the experts that are open to the token (z neither -inf nor NaN)
+//   key = z_e, or fl32(s_e + b_e) with a balance bias b      (both scores grow with z)
+//   groups of neighbouring experts: those with the best keys (or sums of the two best scores) stay
+//   the k largest keys, ties to the lower expert;  w_j = scale s_j [/ sum of the chosen scores]
+//
+// A group of LPT lanes owns a token, expert e in lane e % LPT, so that a wave of 16-lane groups chooses for four tokens at once.
+// Keys are compared as integers that order like the floats; 0 is "closed" or "already taken".  Each of the k rounds is a scan of the
+// lane's own keys and two reductions over the group (largest key, lowest expert that has it) in DPP steps.
+#include "ssg_device.h"
+#include "ssg_internal.h"
+
+namespace ssg {
+
+namespace {
+
+constexpr int kBlock = 1024;                              // threads of the kernels that choose and sort
+constexpr int kWaves = kBlock / 64;
+
+// float -> integer in the same order; -0 counts as +0
+__device__ __forceinline__ uint32_t ordered(float v) {
+    const uint32_t u = __float_as_uint(v + 0.0f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu)); }
+
+// Lane exchanges inside groups of 16: neighbours, pairs, then mirrored halves (which are uniform by then).
+template <int STEP> __device__ __forceinline__ uint32_t exchange(uint32_t v) {
+    constexpr int ctrl = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, ctrl, 0xf, 0xf, false);
+}
+// Every lane of the group gets op over the group, in the same order of operations in every lane's value.
+template <int LPT, class Op> __device__ __forceinline__ uint32_t reduce(uint32_t v, Op op) {
+    v = op(v, exchange<0>(v));
+    v = op(v, exchange<1>(v));
+    v = op(v, exchange<2>(v));
+    v = op(v, exchange<3>(v));
+    if (LPT == 64) {
+        v = op(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+        v = op(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+    }
+    return v;
+}
+template <int LPT> __device__ __forceinline__ uint32_t reduce_max(uint32_t v) {
+    return reduce<LPT>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+template <int LPT> __device__ __forceinline__ uint32_t reduce_min(uint32_t v) {
+    return reduce<LPT>(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+template <int LPT> __device__ __forceinline__ float reduce_sum(float v) {
+    return __uint_as_float(reduce<LPT>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+
+template <bool BF16> __device__ __forceinline__ float load_logit(const void *p, int64_t at) {
+    return BF16 ? bf16_bits_to_f32(static_cast<const uint16_t *>(p)[at]) : static_cast<const float *>(p)[at];
+}
+__device__ __forceinline__ bool is_open(float z) { return z > -INFINITY; }            // false for NaN
+__device__ __forceinline__ float held(float z) { return fminf(z, 3.402823466e+38f); } // +inf: the largest finite number
+
+constexpr float kTiny = 1e-38f;                           // what a sum of scores is held above where it divides
+
+// The experts of token t: lane j of the group returns the j-th (or -1) in id, its weight in w.  `keys`: E words of LDS of the
+// group's own (used with groups only).  All lanes of a wave come here together; `live` says whether the group has a token.
+template <int LPT, int VPL, bool BF16>
+__device__ __forceinline__ void choose(const RouteArgs &a, int64_t t, bool live, uint32_t *keys, int &id, float &w) {
+    const int g0 = threadIdx.x & (LPT - 1);
+    const bool softmax = a.score == 0, biased = a.bias != nullptr, grouped = a.top_groups < a.groups;
+    float z[VPL];
+    uint32_t key[VPL];
+    const int64_t row = t * a.ld;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        const int e = g0 + i * LPT;
+        z[i] = live && e < a.E ? load_logit<BF16>(a.logits, row + e) : -INFINITY;
+    }
+    // softmax: largest logit and sum of exponentials over the open experts
+    float top = 0.0f, sum = 0.0f;
+    if (softmax) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            const uint32_t u = is_open(z[i]) ? ordered(held(z[i])) : 0u;
+            m = m > u ? m : u;
+        }
+        m = reduce_max<LPT>(m);
+        top = m ? from_ordered(m) : 0.0f;
+        if (biased || !a.renorm || (grouped && a.group_top == 2)) {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) sum += is_open(z[i]) ? expf(held(z[i]) - top) : 0.0f;
+            sum = fmaxf(reduce_sum<LPT>(sum), kTiny);
+        }
+    }
+    auto score = [&](float v) { return softmax ? expf(held(v) - top) / sum : sigmoid_f32(held(v)); };
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        const int e = g0 + i * LPT;
+        float v = z[i];
+        if (biased && is_open(v)) v = score(v) + a.bias[e];
+        key[i] = is_open(v) ? ordered(held(v)) : 0u;
+    }
+    if (grouped) {
+        // L lanes to a group of experts; the two best of each, then the group's rank among the others
+        const int size = a.E / a.groups;
+        int L = 1;
+        while (2 * L * a.groups <= LPT) L *= 2;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            const int e = g0 + i * LPT;
+            if (e < a.E) keys[e] = a.group_top == 2 && !biased && key[i] ? ordered(score(z[i])) : key[i];
+        }
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
+        const int group = g0 / L, sub = g0 % L;
+        uint32_t first = 0, second = 0;
+        if (group < a.groups)
+            for (int i = sub; i < size; i += L) {
+                const uint32_t u = keys[group * size + i];
+                second = u > first ? first : (u > second ? u : second);
+                first = u > first ? u : first;
+            }
+        for (int step = 1; step < L; step *= 2) {
+            const uint32_t f = (uint32_t)__shfl_xor((int)first, step, 64), s = (uint32_t)__shfl_xor((int)second, step, 64);
+            const uint32_t low = f > first ? first : f;
+            first = f > first ? f : first;
+            second = second > s ? second : s;
+            second = second > low ? second : low;
+        }
+        uint32_t mine = first;
+        if (a.group_top == 2 && first && second) mine = ordered(from_ordered(first) + from_ordered(second));
+        int ahead = 0;
+        const int lane0 = (threadIdx.x & 63) - g0;
+        for (int g = 0; g < a.groups; ++g) {
+            const uint32_t other = (uint32_t)__shfl((int)mine, lane0 + g * L, 64);
+            ahead += other > mine || (other == mine && g < group);
+        }
+        const uint64_t kept = __ballot(group < a.groups && ahead < a.top_groups) >> lane0;
+        const uint32_t inv = ((1u << 20) + size - 1) / size;          // e * inv >> 20 = e / size for e, size up to 1024
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            const uint32_t g = ((uint32_t)(g0 + i * LPT) * inv) >> 20;
+            if (g < (uint32_t)a.groups && !(kept >> (g * L) & 1)) key[i] = 0;
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    id = -1;
+    for (int j = 0; j < a.k; ++j) {
+        uint32_t best = 0, e = 0xffffffffu;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i)
+            if (key[i] > best) { best = key[i]; e = (uint32_t)(g0 + i * LPT); }
+        const uint32_t all = reduce_max<LPT>(best);
+        e = reduce_min<LPT>(best == all ? e : 0xffffffffu);
+        if (all == 0) e = 0xffffffffu;
+        if (g0 == j) id = (int)e;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i)
+            if (e == (uint32_t)(g0 + i * LPT)) key[i] = 0;
+    }
+    w = 0.0f;
+    if (id >= 0) {
+        const float v = held(load_logit<BF16>(a.logits, row + id));
+        if (softmax) w = sum > 0.0f ? expf(v - top) / sum : expf(v - top);
+        else w = sigmoid_f32(v);
+    }
+    if (a.renorm) w = w / fmaxf(reduce_sum<LPT>(w), kTiny);
+    w = w * a.scale;
+}
+
+// What a block of the sort needs in LDS: the experts' totals, rows before this block's, offsets, and the running counts.
+struct SortLds {
+    uint32_t *total, *before, *offset, *wave_count;       // E, E, E + 1, kWaves * E words
+};
+
+// Exclusive prefix over up to 1024 experts of their rows, rounded up to the alignment; offset[E] = all rows.
+__device__ __forceinline__ void scan_offsets(const RouteArgs &a, const SortLds &s, uint32_t *wave_sum) {
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    uint32_t v = 0;
+    if (tid < a.E) v = (s.total[tid] + a.align - 1) / a.align * a.align;
+    uint32_t inc = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t o = (uint32_t)__shfl_up((int)inc, d, 64);
+        if (lane >= d) inc += o;
+    }
+    if (lane == 63) wave_sum[wv] = inc;
+    __syncthreads();
+    uint32_t base = 0;
+    for (int i = 0; i < wv; ++i) base += wave_sum[i];
+    if (tid < a.E) {
+        s.offset[tid] = base + inc - v;
+        if (tid == a.E - 1) s.offset[a.E] = base + inc;
+    }
+    __syncthreads();
+}
+
+// The rows of assignments [first, last), in their order, behind `before` others of the same expert; and this block's share of
+// what no assignment fills.
+__device__ __forceinline__ void scatter(const RouteArgs &a, const SortLds &s, int64_t first, int64_t last, int block, int blocks) {
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    int bits = 0;
+    while ((1 << bits) < a.E) ++bits;
+    for (int64_t base = first; base < last; base += kBlock) {
+        for (int i = tid; i < kWaves * a.E; i += kBlock) s.wave_count[i] = 0;
+        __syncthreads();
+        const int64_t at = base + tid;
+        const int e = at < last ? a.ids[at] : -1;
+        // lanes of this wave with the same expert
+        uint64_t same = __ballot(e >= 0);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot((e >> b) & 1);
+            same &= (e >> b) & 1 ? set : ~set;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        if (e >= 0 && rank == 0) s.wave_count[wv * a.E + e] = (uint32_t)__popcll(same);
+        __syncthreads();
+        if (e >= 0) {
+            uint32_t row = s.offset[e] + s.before[e] + rank;
+            for (int i = 0; i < wv; ++i) row += s.wave_count[i * a.E + e];
+            a.place[at] = (int)row;
+            a.source[row] = (int)at;
+        } else if (at < last) {
+            a.place[at] = -1;
+        }
+        __syncthreads();
+        for (int x = tid; x < a.E; x += kBlock) {
+            uint32_t n = 0;
+            for (int i = 0; i < kWaves; ++i) n += s.wave_count[i * a.E + x];
+            s.before[x] += n;
+        }
+        __syncthreads();
+    }
+    // rows that fill up an expert's last set, and those beyond all experts
+    for (int e = block; e < a.E; e += blocks)
+        for (int64_t r = (int64_t)s.offset[e] + s.total[e] + tid; r < s.offset[e + 1]; r += kBlock) a.source[r] = -1;
+    for (int64_t r = s.offset[a.E] + (int64_t)block * kBlock + tid; r < a.rows; r += (int64_t)blocks * kBlock) a.source[r] = -1;
+    if (block == 0)
+        for (int e = tid; e <= a.E; e += kBlock) {
+            a.offsets[e] = (int)s.offset[e];
+            if (e < a.E) a.counts[e] = (int)s.total[e];
+        }
+}
+
+__device__ __forceinline__ SortLds sort_lds(uint32_t *lds, int E) { return SortLds{lds, lds + E, lds + 2 * E, lds + 3 * E + 1}; }
+
+// One block per a.block_tokens tokens.  With one block in all it sorts too; otherwise it leaves its experts' counts.
+template <int LPT, int VPL, bool BF16> __global__ __launch_bounds__(kBlock) void route_kernel(RouteArgs a) {
+    extern __shared__ uint32_t lds[];
+    __shared__ uint32_t wave_sum[kWaves];
+    const int tid = threadIdx.x;
+    uint32_t *hist = lds;                                  // = the totals of the sort
+    if (a.place)
+        for (int e = tid; e < a.E; e += kBlock) hist[e] = 0;
+    __syncthreads();
+    uint32_t *keys = lds + a.lds_keys + (size_t)(tid / LPT) * a.E;
+    const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
+    const int64_t t1 = t0 + a.block_tokens < a.T ? t0 + a.block_tokens : a.T;
+    constexpr int kAtOnce = kBlock / LPT;
+    for (int64_t t = t0 + tid / LPT; t - tid / LPT < t1; t += kAtOnce) {
+        const int64_t wave_first = t - (tid & 63) / LPT;
+        if (wave_first >= t1) continue;                    // the whole wave is beyond
+        int id;
+        float w;
+        choose<LPT, VPL, BF16>(a, t, t < t1, keys, id, w);
+        const int j = tid & (LPT - 1);
+        if (t < t1 && j < a.k) {
+            a.ids[t * a.k + j] = id;
+            a.weights[t * a.k + j] = w;
+            if (a.place && id >= 0) atomicAdd(&hist[id], 1u);
+        }
+    }
+    if (!a.place) return;
+    __syncthreads();                                       // (also: this block's ids are visible to it)
+    if (gridDim.x > 1) {
+        const int stride = (a.E + 3) & ~3;
+        for (int e = tid; e < stride; e += kBlock) a.hist[(size_t)blockIdx.x * stride + e] = e < a.E ? hist[e] : 0;
+        return;
+    }
+    const SortLds s = sort_lds(lds, a.E);
+    for (int e = tid; e < a.E; e += kBlock) s.before[e] = 0;
+    scan_offsets(a, s, wave_sum);
+    scatter(a, s, 0, a.T * a.k, 0, 1);
+}
+
+// Second launch where there are several blocks: every block sums up all blocks' counts (up to 256 KB, out of the L2) for the
+// experts' totals and for what lies before its own tokens.
+__global__ __launch_bounds__(kBlock) void dispatch_kernel(RouteArgs a, int blocks) {
+    extern __shared__ uint32_t lds[];
+    __shared__ uint32_t wave_sum[kWaves];
+    const SortLds s = sort_lds(lds, a.E);
+    const int tid = threadIdx.x, block = blockIdx.x;
+    for (int e = tid; e < 2 * a.E; e += kBlock) lds[e] = 0;
+    __syncthreads();
+    const int quads = (a.E + 3) / 4, parts = kBlock / quads;          // E <= 1024: at least four parts
+    const int q = tid % quads, part = tid / quads;
+    if (part < parts) {
+        uint32_t total[4] = {0, 0, 0, 0}, before[4] = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int b = part; b < blocks; b += parts) {
+            const uint4 v = reinterpret_cast<const uint4 *>(a.hist)[(size_t)b * quads + q];
+            const uint32_t n[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                total[i] += n[i];
+                if (b < block) before[i] += n[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (4 * q + i < a.E) {
+                atomicAdd(&s.total[4 * q + i], total[i]);
+                atomicAdd(&s.before[4 * q + i], before[i]);
+            }
+    }
+    __syncthreads();
+    scan_offsets(a, s, wave_sum);
+    const int64_t first = (int64_t)block * a.block_tokens * a.k, end = first + (int64_t)a.block_tokens * a.k;
+    scatter(a, s, first, end < a.T * a.k ? end : a.T * a.k, block, blocks);
+}
+
+// ---- gradient ----------------------------------------------------------------------------------------------
+// With q_j = ds/dw of the chosen: (scale dw_j - sum_i w_i dw_i) / S where renormalised (S the sum of the chosen scores), else scale dw_j;
+//   sigmoid: dz_j = q_j s_j (1 - s_j)        softmax: dz_e = s_e ([e chosen] q_e - sum_j q_j s_j)
+// and with renormalised softmax weights the last sum is zero and s_j / S = w_j / scale: only the chosen experts' logits have one.
+// A block forms the rows of its tokens in LDS, 16 lanes to a token, and streams them out.
+constexpr int kBwdThreads = 256, kBwdTokens = kBwdThreads / 16;
+template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_kernel(RouteBwdArgs a) {
+    extern __shared__ float rows[];
+    const int tid = threadIdx.x, g0 = tid & 15;
+    const int64_t t0 = (int64_t)blockIdx.x * kBwdTokens, t = t0 + tid / 16;
+    const bool live = t < a.T, softmax = a.score == 0, dense = softmax && !a.renorm;
+    float *mine = rows + (tid / 16) * a.E;
+    // k up to 32: two assignments to a lane
+    int id[2];
+    float w[2], dw[2], z[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int j = g0 + 16 * i;
+        const bool ok = live && j < a.k;
+        id[i] = ok ? a.ids[t * a.k + j] : -1;
+        if (id[i] >= a.E) id[i] = -1;
+        w[i] = ok ? a.weights[t * a.k + j] : 0.0f;
+        dw[i] = ok && id[i] >= 0 ? a.dweights[t * a.k + j] : 0.0f;
+        z[i] = id[i] >= 0 ? held(load_logit<BF16>(a.logits, t * a.ld + id[i])) : 0.0f;
+    }
+    float top = 0.0f, sum = 1.0f;
+    if (softmax) {
+        uint32_t m = 0;
+        if (dense) {
+            for (int e = g0; e < a.E; e += 16) {
+                const float v = live ? load_logit<BF16>(a.logits, t * a.ld + e) : -INFINITY;
+                mine[e] = v;
+                const uint32_t u = is_open(v) ? ordered(held(v)) : 0u;
+                m = m > u ? m : u;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t u = id[i] >= 0 && is_open(z[i]) ? ordered(z[i]) : 0u;
+                m = m > u ? m : u;
+            }
+        }
+        m = reduce_max<16>(m);
+        top = m ? from_ordered(m) : 0.0f;
+        if (dense) {
+            sum = 0.0f;
+            for (int e = g0; e < a.E; e += 16) {
+                const float p = is_open(mine[e]) ? expf(held(mine[e]) - top) : 0.0f;
+                mine[e] = p;
+                sum += p;
+            }
+            sum = fmaxf(reduce_sum<16>(sum), kTiny);
+        }
+    }
+    float s[2], part = 0.0f, chosen = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        s[i] = 0.0f;
+        if (id[i] >= 0) s[i] = softmax ? expf(z[i] - top) / sum : sigmoid_f32(z[i]);
+        part += w[i] * dw[i];
+        chosen += s[i];
+    }
+    if (a.renorm) {
+        part = reduce_sum<16>(part);
+        chosen = fmaxf(reduce_sum<16>(chosen), kTiny);
+    }
+    float q[2], mean = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        q[i] = a.renorm ? (a.scale * dw[i] - part) / chosen : a.scale * dw[i];
+        if (id[i] < 0) q[i] = 0.0f;
+        mean += q[i] * s[i];
+    }
+    if (dense) {
+        mean = reduce_sum<16>(mean);
+        const float by = mean / sum;
+        for (int e = g0; e < a.E; e += 16) mine[e] = -mine[e] * by;
+    } else {
+        for (int e = g0; e < a.E; e += 16) mine[e] = 0.0f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (id[i] >= 0) {
+            const float d = softmax ? q[i] * s[i] : q[i] * s[i] * (1.0f - s[i]);
+            if (dense) mine[id[i]] += d;
+            else mine[id[i]] = d;
+        }
+    __syncthreads();
+    // the block's rows are one run of memory that starts on 16 bytes (kBwdTokens rows are a multiple of it)
+    const int n = (int)((a.T - t0 < kBwdTokens ? a.T - t0 : kBwdTokens) * a.E);
+    constexpr int kVec = BF16 ? 8 : 4;
+    uint8_t *out = static_cast<uint8_t *>(a.dlogits) + t0 * a.E * (BF16 ? 2 : 4);
+    for (int i = tid * kVec; i < n; i += kBwdThreads * kVec) {
+        if (i + kVec <= n) {
+            uint4 v;
+            if (BF16) v = make_uint4(pack_bf16x2(rows[i], rows[i + 1]), pack_bf16x2(rows[i + 2], rows[i + 3]),
+                                     pack_bf16x2(rows[i + 4], rows[i + 5]), pack_bf16x2(rows[i + 6], rows[i + 7]));
+            else v = make_uint4(__float_as_uint(rows[i]), __float_as_uint(rows[i + 1]), __float_as_uint(rows[i + 2]), __float_as_uint(rows[i + 3]));
+            *reinterpret_cast<uint4 *>(out + (size_t)i * (BF16 ? 2 : 4)) = v;
+        } else {
+            for (int x = i; x < n; ++x) {
+                if (BF16) reinterpret_cast<uint16_t *>(out)[x] = (uint16_t)f32_to_bf16_bits(rows[x]);
+                else reinterpret_cast<float *>(out)[x] = rows[x];
+            }
+        }
+    }
+}
+
+// ---- the weighted sum of the experts' rows -------------------------------------------------------------------
+// y[t] = sum_j w[t,j] o[place[t,j]], in the order of j, in fp32.  A thread owns 8 columns of a token.
+template <bool F32> __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
+    const int per_row = (int)(a.d / 8);
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.T * per_row) return;
+    const int64_t t = i / per_row;
+    const int64_t c = (i - t * per_row) * 8;
+    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+    for (int j = 0; j < a.k; ++j) {
+        const int row = a.place[t * a.k + j];
+        if (row < 0) continue;
+        const float w = a.weights[t * a.k + j];
+        float v[8];
+        if (F32) {
+            const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(a.o) + (int64_t)row * a.d + c);
+            const float4 x = p[0], y = p[1];
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        } else {
+            const uint4 x = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.o) + (int64_t)row * a.d + c);
+            const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int b = 0; b < 4; ++b) { v[2 * b] = __uint_as_float(u[b] << 16); v[2 * b + 1] = __uint_as_float(u[b] & 0xffff0000u); }
+        }
+#pragma unroll
+        for (int b = 0; b < 8; ++b) acc[b] = __fmaf_rn(w, v[b], acc[b]);
+    }
+    if (F32) {
+        float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(a.y) + t * a.d + c);
+        p[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        p[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    } else {
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.y) + t * a.d + c) =
+            make_uint4(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]), pack_bf16x2(acc[4], acc[5]), pack_bf16x2(acc[6], acc[7]));
+    }
+}
+
+// Tokens to a block, so that there are at most 256 blocks and 64 K counts (which every block of the second launch reads).
+constexpr int kOneLaunch = 128;                            // tokens that one block chooses for and sorts
+int most_blocks(int E) { return std::min(256, 65536 / E); }
+struct RoutePlan { int lpt, vpl, block_tokens, blocks; };
+RoutePlan route_plan(const RouteArgs &a) {
+    RoutePlan p;
+    // 16 lanes to a token choose for four tokens in one wave; 64 where the experts, their groups or k need them, and for the
+    // few tokens of a decode step, which are a wave's latency whatever the others do
+    p.lpt = a.E > 256 || a.k > 16 || a.groups > 16 || a.T <= 16 ? 64 : 16;
+    p.vpl = 1;
+    while (p.vpl * p.lpt < a.E) p.vpl *= 2;
+    const int most = most_blocks(a.E);
+    const int64_t pass = kBlock / p.lpt;
+    int64_t tokens = (a.T + most - 1) / most;
+    tokens = (tokens + pass - 1) / pass * pass;
+    if (a.T <= kOneLaunch) tokens = std::max<int64_t>(tokens, a.T);          // one launch: a second costs more than a longer block
+    p.block_tokens = (int)std::min<int64_t>(tokens, 1 << 30);
+    p.blocks = (int)((a.T + p.block_tokens - 1) / p.block_tokens);
+    return p;
+}
+
+template <int LPT, int VPL> void launch_route_as(const RouteArgs &a, int blocks, size_t lds, hipStream_t st) {
+    if (a.bf16) hipLaunchKernelGGL((route_kernel<LPT, VPL, true>), dim3(blocks), dim3(kBlock), lds, st, a);
+    else hipLaunchKernelGGL((route_kernel<LPT, VPL, false>), dim3(blocks), dim3(kBlock), lds, st, a);
+}
+
+// T = 0: no expert has a row
+__global__ void no_rows_kernel(int *counts, int *offsets, int E) {
+    for (int e = threadIdx.x; e <= E; e += blockDim.x) {
+        offsets[e] = 0;
+        if (e < E) counts[e] = 0;
+    }
+}
+
+}  // namespace
+
+size_t route_hist_words(const RouteArgs &a) {
+    // (of the most blocks, so that it does not fall as T grows)
+    return a.T > kOneLaunch ? (size_t)most_blocks(a.E) * ((a.E + 3) & ~3) : 0;
+}
+
+void launch_route(RouteArgs a, hipStream_t st) {
+    if (a.T == 0) {
+        if (a.offsets) hipLaunchKernelGGL(no_rows_kernel, dim3(1), dim3(256), 0, st, a.counts, a.offsets, a.E);
+        return;
+    }
+    const RoutePlan p = route_plan(a);
+    a.block_tokens = p.block_tokens;
+    const bool grouped = a.top_groups < a.groups;
+    const size_t sort_words = 3 * (size_t)a.E + 1 + (size_t)kWaves * a.E;
+    // the keys of all tokens in hand (with groups), and the sort's words; in the launch that sorts too, one after the other
+    a.lds_keys = a.E;
+    const size_t key_words = a.E + (grouped ? (size_t)kBlock / p.lpt * a.E : 0);
+    const size_t words = a.place && p.blocks == 1 ? std::max(sort_words, key_words) : key_words;
+    const double bytes = (double)a.T * a.E * (a.bf16 ? 2 : 4) + 8.0 * a.T * a.k;
+    profile_before(kTagRoute, st, bytes);
+    const size_t lds = words * 4;
+    if (p.lpt == 16) {
+        switch (p.vpl) {
+            case 1: launch_route_as<16, 1>(a, p.blocks, lds, st); break;
+            case 2: launch_route_as<16, 2>(a, p.blocks, lds, st); break;
+            case 4: launch_route_as<16, 4>(a, p.blocks, lds, st); break;
+            case 8: launch_route_as<16, 8>(a, p.blocks, lds, st); break;
+            default: launch_route_as<16, 16>(a, p.blocks, lds, st); break;
+        }
+    } else {
+        switch (p.vpl) {
+            case 1: launch_route_as<64, 1>(a, p.blocks, lds, st); break;
+            case 2: launch_route_as<64, 2>(a, p.blocks, lds, st); break;
+            case 4: launch_route_as<64, 4>(a, p.blocks, lds, st); break;
+            case 8: launch_route_as<64, 8>(a, p.blocks, lds, st); break;
+            default: launch_route_as<64, 16>(a, p.blocks, lds, st); break;
+        }
+    }
+    profile_after(st);
+    if (!a.place || p.blocks == 1) return;
+    profile_before(kTagDispatch, st, 12.0 * a.T * a.k + 4.0 * a.rows);
+    hipLaunchKernelGGL(dispatch_kernel, dim3(p.blocks), dim3(kBlock), sort_words * 4, st, a, p.blocks);
+    profile_after(st);
+}
+
+void launch_route_bwd(const RouteBwdArgs &a, hipStream_t st) {
+    if (a.T == 0) return;
+    const int64_t blocks = (a.T + kBwdTokens - 1) / kBwdTokens;
+    const size_t lds = (size_t)kBwdTokens * a.E * 4;
+    profile_before(kTagRouteBwd, st, (double)a.T * a.E * (a.bf16 ? 2 : 4));
+    if (a.bf16) hipLaunchKernelGGL(route_bwd_kernel<true>, dim3((unsigned)blocks), dim3(kBwdThreads), lds, st, a);
+    else hipLaunchKernelGGL(route_bwd_kernel<false>, dim3((unsigned)blocks), dim3(kBwdThreads), lds, st, a);
+    profile_after(st);
+}
+
+void launch_combine(const CombineArgs &a, hipStream_t st) {
+    if (a.T == 0) return;
+    const int64_t blocks = (a.T * (a.d / 8) + 255) / 256;
+    const double size = a.f32 ? 4 : 2;
+    profile_before(kTagCombine, st, (a.k + 1.0) * size * a.T * a.d);
+    if (a.f32) hipLaunchKernelGGL(combine_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(combine_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    profile_after(st);
+}
+
+}  // namespace ssg
