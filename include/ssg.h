@@ -407,7 +407,7 @@ ssg_status ssg_route_bwd(const ssg_route_desc *desc, const void *logits, const i
                          void *dlogits, void *stream);
 
 /* Rows in 8-bit integers with a scale each -- tokens of activations, channels of weights:
- *     scale_r = fl32(amax_r / 127),  code = round to nearest even(fl32(x fl32(127 / amax_r)))
+ *     scale_r = fl32(amax_r / 127),  code = round to nearest even(fl32(x fl32(127 fl32(1 / amax_r))))
  * (scale at least 2^-126, with 2^126 as the factor there; a row of zeros has scale 0; one with a NaN or an infinity a NaN, and codes 0).
  * They live in a buffer of ssg_i8_bytes(rows, K) bytes, 256-byte aligned, in the layout that the products read: blocks of 16 rows by 64
  * codes, 1 KB each, code (r, k) at byte ((r / 16) * (Kp / 64) + k / 64) * 1024 + (k % 64 / 16) * 256 + r % 16 * 16 + k % 16

@@ -13,7 +13,7 @@ def quantize(x: np.ndarray):
     amax = np.abs(np.where(bad[:, None], F(0), x)).max(-1).astype(F) if x.shape[1] else np.zeros(x.shape[0], F)
     with np.errstate(all="ignore"):
         scale = (amax / F(127)).astype(F)
-        factor = (F(127) / amax).astype(F)
+        factor = (F(127) * (F(1) / amax).astype(F)).astype(F)
     small = scale < F(2.0 ** -126)
     scale = np.where(small, np.where(amax > 0, F(2.0 ** -126), F(0)), scale).astype(F)
     factor = np.where(small, np.where(amax > 0, F(2.0 ** 126), F(0)), factor).astype(F)

@@ -50,7 +50,7 @@ def choose(z, k, score=SOFTMAX, bias=None, groups=1, top_groups=1, group_top=1, 
         for j in range(min(k, E)):
             if best[j] > -np.inf:
                 ids[t, j] = order[j]
-                if j + 1 < len(best) and 0 < best[j] - best[j + 1] < np.inf:
+                if j + 1 < len(best) and best[j + 1] > -np.inf and best[j] > best[j + 1]:
                     gap[t] = min(gap[t], best[j] - best[j + 1])
     w = weights(s, ids, renorm, scale)
     return ids, w, gap

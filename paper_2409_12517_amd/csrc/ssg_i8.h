@@ -11,7 +11,7 @@ __device__ __forceinline__ I8Scale i8_scale(uint32_t top_bits) {
     if (top_bits >= 0x7f800000u) return {__uint_as_float(0x7fc00000u), 0.0f};
     const float amax = __uint_as_float(top_bits);
     const float scale = __fdiv_rn(amax, 127.0f);
-    if (scale >= 0x1p-126f) return {scale, __fdiv_rn(127.0f, amax)};
+    if (scale >= 0x1p-126f) return {scale, __fmul_rn(127.0f, __fdiv_rn(1.0f, amax))};
     return amax > 0.0f ? I8Scale{0x1p-126f, 0x1p126f} : I8Scale{0.0f, 0.0f};
 }
 

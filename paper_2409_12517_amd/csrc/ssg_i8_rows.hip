@@ -1,8 +1,8 @@
 // Rows in 8-bit integers with a scale each (tokens of activations, channels of weights), in the layout of the products:
 //
-//   amax = max_k |x_rk|,  scale_r = fl32(amax / 127),  code = round-to-nearest-even(fl32(x * fl32(127 / amax)))     -127 .. 127
+//   amax = max_k |x_rk|,  scale_r = fl32(amax / 127),  code = round-to-nearest-even(fl32(x f)),  f = fl32(127 fl32(1 / amax))
 //
-// (scale at least 2^-126, 1 / scale the factor there; amax = 0: scale 0, codes 0; a row that holds a NaN or an infinity has
+// (the factor in the two steps that tensor programs form it in, so that their codes are these; codes -127 to 127; scale at least 2^-126, 1 / scale the factor there; amax = 0: scale 0, codes 0; a row that holds a NaN or an infinity has
 // a NaN for its scale and codes 0, so that everything made from it is NaN).
 #include "ssg_device.h"
 #include "ssg_i8.h"
