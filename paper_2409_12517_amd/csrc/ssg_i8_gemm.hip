@@ -120,7 +120,8 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
     __shared__ __attribute__((aligned(1024))) uint8_t smem[kI8Stages * kStage];
     I8Tile tile;
     if (!find_tile(p, kEdge, blockIdx.x, tile)) return;
-    const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w >> 1, wn = w & 1;
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w >> 1, wn = w & 1;
+    int l = tid & 63;
     const int KB = p.KB, col_blocks = (int)(p.N / 16);
     const int first_rb = tile.row / 16, last_rb = tile.row_end / 16 - 1;
     const int first_cb = tile.col * (kCols / 16);
@@ -141,10 +142,21 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
         if (j < WB) dma16_s(a_src, a_lane[j], a_dst + slot + j * 1024u);
         else dma16_s(b_src, b_lane[j - WB], b_dst + slot + (j - WB) * 1024u);
     };
-    auto advance = [&]() { a_src += 1024; b_src += 1024; };
+    // The sources stop at the last block of K: the loop issues loads in every step, the last ones into stages that nothing reads,
+    // so that it is one piece of code with one count of loads to wait for.
+    int loaded = 0;
+    auto advance = [&]() {
+        const int by = ++loaded < KB ? 1024 : 0;
+        a_src += by;
+        b_src += by;
+    };
     constexpr int kLoads = 2 * WB;
-    const int ahead = KB < kI8Stages ? KB : kI8Stages;
-    for (int s = 0; s < ahead; ++s) {
+    static_assert(kLoads == RB, "a load to every column of blocks");
+    // Steps come in pairs; where their number is odd the first of a pair multiplies zeros, in the place of a step -1.
+    const int odd_steps = KB & 1;
+#pragma unroll
+    for (int s = 0; s < kI8Stages; ++s) {
+        if (s == kI8Stages - 1 && odd_steps) break;      // (step -1 loads it)
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) issue_one(j, s * kStage);
         advance();
@@ -162,19 +174,20 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
         if (i % 2 == 0) fa[set][i / 2] = *reinterpret_cast<const v4i_t *>(a_frag + slot + i / 2 * 1024);
         else fb[set][i / 2] = *reinterpret_cast<const v4i_t *>(b_frag + slot + col_block(i / 2) * 1024);
     };
-    if (ahead == kI8Stages) wait_dma<(kI8Stages - 1) * kLoads>();
-    else wait_dma<0>();
+    wait_dma<(kI8Stages - 2) * kLoads>();                // (stage 0, and with an even number of steps stage 1)
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < 2 * RB; ++i) read_one(0, i, 0);
-    uint32_t slot = 0;                                   // of this step's stage
-    auto step = [&](auto fast, auto parity, int k) {
-        constexpr bool FAST = decltype(fast)::value;
+    if (odd_steps) {
+#pragma unroll
+        for (int i = 0; i < RB; ++i) fa[0][i] = v4i_t{0, 0, 0, 0};
+    }
+    uint32_t slot = odd_steps ? (kI8Stages - 1) * kStage : 0;        // of this step's stage
+    auto step = [&](auto parity) {
         constexpr int set = decltype(parity)::value;
         const uint32_t next = slot == (kI8Stages - 1) * kStage ? 0 : slot + kStage;
-        if (FAST || k + kI8Stages - 1 < KB) wait_dma<(kI8Stages - 2) * kLoads>();     // the next step's stage has landed
-        else wait_dma<0>();
+        wait_dma<(kI8Stages - 2) * kLoads>();            // the next step's stage has landed
         __builtin_amdgcn_s_waitcnt(0xC07F);              // this step's fragments are here
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
@@ -183,55 +196,53 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
         for (int t = 0; t < RB * RB; ++t) {
             const int c = t / RB, r = c & 1 ? RB - 1 - t % RB : t % RB;
             acc[r][c] = mfma_i8(fb[set][c], fa[set][r], acc[r][c]);
-            if (t % kEvery == 0) read_one(set ^ 1, t / kEvery, next);        // (after the last step: a stale stage, never used)
-            if (FAST && t % RB == RB / 4) issue_one(t / RB, slot);
+            if (t % kEvery == 0) read_one(set ^ 1, t / kEvery, next);        // (after the last step: never used)
+            if (t % RB == RB / 4) issue_one(t / RB, slot);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (FAST) advance();
+        advance();
         slot = next;
     };
-    static_assert(kLoads == RB, "a load to every column of blocks");
-    constexpr std::integral_constant<int, 0> even{};
-    constexpr std::integral_constant<int, 1> odd{};
-    int k = 0;
-    for (; k + kI8Stages + 1 < KB; k += 2) {
-        step(std::true_type{}, even, k);
-        step(std::true_type{}, odd, k + 1);
+#pragma nounroll
+    for (int k = -odd_steps; k < KB; k += 2) {
+        step(std::integral_constant<int, 0>{});
+        step(std::integral_constant<int, 1>{});
     }
-    if (k + kI8Stages < KB) {
-        step(std::true_type{}, even, k);
-        for (++k; k < KB; k += 2) {
-            step(std::false_type{}, odd, k);
-            if (k + 1 < KB) step(std::false_type{}, even, k + 1);
-        }
-    } else {
-        for (; k < KB; k += 2) {
-            step(std::false_type{}, even, k);
-            if (k + 1 < KB) step(std::false_type{}, odd, k + 1);
-        }
-    }
-    // a lane stores four neighbouring columns of a row at a time
+    wait_dma<0>();                                       // (the workgroup's LDS is another's after it)
+    asm volatile("" : "+v"(l));
+    // a lane stores four neighbouring columns of a row at a time.  All scales are read before the first store: behind one the compiler
+    // would read them again.
     constexpr int kOut = DUAL ? RB / 2 : RB;
     const float *sb = p.sb + (int64_t)tile.expert * p.N, *sb2 = DUAL ? p.sb2 + (int64_t)tile.expert * p.N : nullptr;
+    float sa[RB];
+    float4 s1[kOut], s2[kOut];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int rb = first_rb + wm * RB + r;
+        sa[r] = p.sa[(int64_t)(rb < last_rb ? rb : last_rb) * 16 + (l & 15)];
+    }
+#pragma unroll
+    for (int c = 0; c < kOut; ++c) {
+        const int cb = first_cb + wn * kOut + c;
+        const int64_t col = (int64_t)(cb < col_blocks ? cb : col_blocks - 1) * 16 + (l >> 4) * 4;
+        s1[c] = *reinterpret_cast<const float4 *>(sb + col);
+        if (DUAL) s2[c] = *reinterpret_cast<const float4 *>(sb2 + col);
+    }
 #pragma unroll
     for (int c = 0; c < kOut; ++c) {
         const int cb = first_cb + wn * kOut + c;
         if (cb >= col_blocks) continue;
         const int64_t col = (int64_t)cb * 16 + (l >> 4) * 4;
-        const float4 s1 = *reinterpret_cast<const float4 *>(sb + col);
-        float4 s2 = s1;
-        if (DUAL) s2 = *reinterpret_cast<const float4 *>(sb2 + col);
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             const int rb = first_rb + wm * RB + r;
             if (rb > last_rb) continue;
             const int64_t row = (int64_t)rb * 16 + (l & 15);
-            const float sa = p.sa[row];
             float v[4];
-            scaled4(acc[r][c], sa, s1, v);
+            scaled4(acc[r][c], sa[r], s1[c], v);
             if (DUAL) {
                 float g[4];
-                scaled4(acc[r][c + RB / 2], sa, s2, g);
+                scaled4(acc[r][c + RB / 2], sa[r], s2[c], g);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = swiglu_f32(v[i], g[i]);
             }
@@ -341,7 +352,8 @@ template <bool DUAL> void launch_form(const I8GemmArgs &a, hipStream_t st) {
     profile_before(DUAL ? kTagI8Swiglu : kTagI8Gemm, st);
     if (rows <= 16) go(i8_few_kernel<1, 1, DUAL>, 16, 16, 64 * kFewWaves);
     else if (rows <= 32) go(i8_few_kernel<2, 1, DUAL>, 32, 16, 64 * kFewWaves);
-    else go(i8_tile_kernel<2, DUAL>, 128, DUAL ? 64 : 128, 256);
+    else if (rows <= 256) go(i8_tile_kernel<2, DUAL>, 128, DUAL ? 64 : 128, 256);
+    else go(i8_tile_kernel<4, DUAL>, 256, DUAL ? 128 : 256, 256);
     profile_after(st);
 }
 
