@@ -42,13 +42,29 @@ template <bool BF16> struct I8Run {
         const uint32_t w = words[i % 8 / 2];
         return __uint_as_float(i % 2 ? w & 0xffff0000u : w << 16);
     }
+    // Largest absolute value so far: bits of fp32, or of two bf16 side by side, which are compared as 16-bit integers.
     __device__ __forceinline__ uint32_t max_bits(uint32_t top) const {
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t u = __float_as_uint(value(i)) & 0x7fffffffu;
-            top = top > u ? top : u;
+        for (const auto &q : v) {
+            const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (uint32_t w : words) {
+                if (BF16) top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, w & 0x7fff7fffu)));
+                else top = top > (w & 0x7fffffffu) ? top : w & 0x7fffffffu;
+            }
         }
         return top;
+    }
+    static __device__ __forceinline__ uint32_t as_f32_bits(uint32_t top) {
+        if (!BF16) return top;
+        const uint32_t hi = top & 0xffff0000u, lo = top << 16;
+        return hi > lo ? hi : lo;
+    }
+    // From here on the values are what lies in their registers (else the compiler keeps every value that it has unpacked).
+    __device__ __forceinline__ void opaque() {
+#pragma unroll
+        for (auto &q : v) asm volatile("" : "+v"(q.x), "+v"(q.y), "+v"(q.z), "+v"(q.w));
     }
     // A factor of 0 (a row of zeros, or one that is not finite) gives codes 0 whatever the values are.
     __device__ __forceinline__ uint4 codes(float factor) const {

@@ -2,8 +2,9 @@
 //
 //   amax = max_k |x_rk|,  scale_r = fl32(amax / 127),  code = round-to-nearest-even(fl32(x f)),  f = fl32(127 fl32(1 / amax))
 //
-// (the factor in the two steps that tensor programs form it in, so that their codes are these; codes -127 to 127; scale at least 2^-126, 1 / scale the factor there; amax = 0: scale 0, codes 0; a row that holds a NaN or an infinity has
-// a NaN for its scale and codes 0, so that everything made from it is NaN).
+// (the factor in the two steps that tensor programs form it in, so that their codes are these; codes -127 to 127; scale at
+// least 2^-126, 1 / scale the factor there; amax = 0: scale 0, codes 0; a row that holds a NaN or an infinity has a NaN for its
+// scale and codes 0, so that everything made from it is NaN).
 #include "ssg_device.h"
 #include "ssg_i8.h"
 #include "ssg_internal.h"
@@ -12,60 +13,74 @@ namespace ssg {
 
 namespace {
 
-// A block owns 16 rows, as the layout does: thread t has row t % 16 and every (threads / 16)-th run of 16 codes, so that a wave
-// reads 16 rows x 64 elements and writes 1 KB of codes in one piece.  The first kHeld runs stay in registers between the maximum and the
-// codes; what a row has beyond them is read again, out of the L2.
-constexpr int kHeld = 4;
-template <bool BF16, int THREADS> __global__ __launch_bounds__(THREADS) void i8_rows_kernel(I8RowsArgs a) {
-    constexpr int kCols = THREADS / 16;
-    __shared__ uint32_t maxima[THREADS / 64][16];
-    const int tid = threadIdx.x, r = tid & 15, c0 = tid >> 4;
-    const int64_t row = (int64_t)blockIdx.x * 16 + r;
-    if (a.live_rows && (int64_t)blockIdx.x * 16 >= *a.live_rows) return;
+// Bound by memory.  A block owns 8 rows, half of one of the layout's: thread t has row t % 8 and every (threads / 8)-th run of 16 codes, so
+// that a wave reads 8 rows x 128 elements and writes pieces of 128 bytes.  The first HELD runs of a thread stay in registers between the
+// maximum and the codes; what a row has beyond them is read again, out of the L2.
+constexpr int kRows = 8;
+template <bool BF16, int THREADS, int HELD> __global__ __launch_bounds__(THREADS) void i8_rows_kernel(I8RowsArgs a) {
+    constexpr int kCols = THREADS / kRows, kWaves = THREADS / 64;
+    __shared__ uint32_t maxima[kWaves][kRows];
+    const int tid = threadIdx.x, r = tid % kRows, c0 = tid / kRows;
+    const int64_t row = (int64_t)blockIdx.x * kRows + r;
+    if (a.live_rows && (int64_t)blockIdx.x * kRows >= *a.live_rows) return;
     int64_t from = row < a.rows ? row : -1;
     if (a.source && from >= 0) {
-        from = a.source[row];
-        if (from >= 0) from /= a.k;
+        const int s = a.source[row];
+        from = s >= 0 ? s / a.k : -1;
     }
     const int runs = (int)(a.K / 16), padded = (int)(i8_up(a.K, 64) / 16);
     const uint8_t *src = static_cast<const uint8_t *>(a.src) + (from >= 0 ? from : 0) * a.ld * (BF16 ? 2 : 4);
-    I8Run<BF16> held[kHeld];
+    I8Run<BF16> held[HELD];
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
         held[i].clear();
         const int c = c0 + i * kCols;
         if (from >= 0 && c < runs) held[i].load(src, c);
     }
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) top = held[i].max_bits(top);
+    for (int i = 0; i < HELD; ++i) top = held[i].max_bits(top);
     if (from >= 0)
-        for (int c = c0 + kHeld * kCols; c < runs; c += kCols) {
+        for (int c = c0 + HELD * kCols; c < runs; c += kCols) {
             I8Run<BF16> run;
             run.load(src, c);
             top = run.max_bits(top);
         }
+    top = I8Run<BF16>::as_f32_bits(top);
     auto larger = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
-    top = larger(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-    top = larger(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-    if ((tid & 63) < 16) maxima[tid >> 6][r] = top;
+#pragma unroll
+    for (int d = kRows; d < 64; d *= 2) top = larger(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    if ((tid & 63) < kRows) maxima[tid >> 6][r] = top;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < THREADS / 64; ++i) top = larger(top, maxima[i][r]);
+    for (int i = 0; i < kWaves; ++i) top = larger(top, maxima[i][r]);
     const I8Scale s = i8_scale(top);
-    if (tid < 16) a.scales[row] = s.scale;
-    uint8_t *out = a.codes + (int64_t)blockIdx.x * padded * 256 + r * 16;
+    if (tid < kRows) a.scales[row] = s.scale;
+    uint8_t *out = a.codes + (row / 16 * padded * 16 + row % 16) * 16;
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
         const int c = c0 + i * kCols;
+        held[i].opaque();
         if (c < padded) *reinterpret_cast<uint4 *>(out + (int64_t)c * 256) = held[i].codes(s.factor);
     }
-    for (int c = c0 + kHeld * kCols; c < padded; c += kCols) {
+    for (int c = c0 + HELD * kCols; c < padded; c += kCols) {
         I8Run<BF16> run;
         run.clear();
         if (from >= 0 && c < runs) run.load(src, c);
         *reinterpret_cast<uint4 *>(out + (int64_t)c * 256) = run.codes(s.factor);
     }
+}
+
+template <bool BF16> void launch_rows(const I8RowsArgs &a, hipStream_t st) {
+    const unsigned blocks = (unsigned)(i8_up(a.rows, 16) / kRows);
+    const int runs = (int)(i8_up(a.K, 64) / 16);
+    // the smallest block whose registers hold the rows: 88 registers of values are 11 runs of bf16, 80 5 of fp32
+    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, st, a); };
+    constexpr int kFew = BF16 ? 4 : 2, kMost = BF16 ? 11 : 5;
+    if (runs <= 32 * kFew) go(i8_rows_kernel<BF16, 256, kFew>, 256);
+    else if (runs <= 32 * kMost) go(i8_rows_kernel<BF16, 256, kMost>, 256);
+    else if (runs <= 64 * kMost) go(i8_rows_kernel<BF16, 512, kMost>, 512);
+    else go(i8_rows_kernel<BF16, 1024, kMost>, 1024);
 }
 
 // Row-major codes and scales into the layout and back, 16 bytes to a thread.
@@ -92,10 +107,9 @@ __global__ void i8_unpack_kernel(const uint8_t *in, const float *in_scales, int6
 
 void launch_i8_quantize(const I8RowsArgs &a, hipStream_t st) {
     if (a.rows == 0) return;
-    const unsigned blocks = (unsigned)((a.rows + 15) / 16);
     profile_before(kTagI8Rows, st, (double)a.rows * a.K * (a.bf16 ? 3 : 5));
-    if (a.bf16) hipLaunchKernelGGL((i8_rows_kernel<true, 1024>), dim3(blocks), dim3(1024), 0, st, a);
-    else hipLaunchKernelGGL((i8_rows_kernel<false, 1024>), dim3(blocks), dim3(1024), 0, st, a);
+    if (a.bf16) launch_rows<true>(a, st);
+    else launch_rows<false>(a, st);
     profile_after(st);
 }
 
