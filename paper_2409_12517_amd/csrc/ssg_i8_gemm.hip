@@ -209,9 +209,11 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
         step(std::integral_constant<int, 1>{});
     }
     wait_dma<0>();                                       // (the workgroup's LDS is another's after it)
+    __syncthreads();                                     // the ring is free
     asm volatile("" : "+v"(l));
-    // a lane stores four neighbouring columns of a row at a time.  All scales are read before the first store: behind one the compiler
-    // would read them again.
+    // 16 rows at a time go through a patch of LDS of the wave's own, so that rows leave in pieces of 16 bytes side by side (straight from
+    // the accumulators, 8 bytes of 16 rows in a store, the epilogue of the large tile took 9 us more).  All scales are read
+    // before the first store: behind one the compiler would read them again.
     constexpr int kOut = DUAL ? RB / 2 : RB;
     const float *sb = p.sb + (int64_t)tile.expert * p.N, *sb2 = DUAL ? p.sb2 + (int64_t)tile.expert * p.N : nullptr;
     float sa[RB];
@@ -228,36 +230,50 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
         s1[c] = *reinterpret_cast<const float4 *>(sb + col);
         if (DUAL) s2[c] = *reinterpret_cast<const float4 *>(sb2 + col);
     }
-#pragma unroll
-    for (int c = 0; c < kOut; ++c) {
-        const int cb = first_cb + wn * kOut + c;
-        if (cb >= col_blocks) continue;
-        const int64_t col = (int64_t)cb * 16 + (l >> 4) * 4;
+    auto store = [&](auto f32) {
+        constexpr bool F32 = decltype(f32)::value;
+        constexpr int kSize = F32 ? 4 : 2, kRowBytes = kOut * 16 * kSize, kPitch = kRowBytes + 16;
+        constexpr int kLanes = kRowBytes / 16, kAtOnce = 64 / kLanes;        // lanes to a row, rows to a store
+        static_assert(4 * 16 * kPitch <= kI8Stages * kStage, "the patches fit the ring");
+        uint8_t *patch = smem + w * 16 * kPitch;
+        const int64_t col0 = ((int64_t)first_cb + wn * kOut) * 16 + (l % kLanes) * (16 / kSize);
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             const int rb = first_rb + wm * RB + r;
-            if (rb > last_rb) continue;
-            const int64_t row = (int64_t)rb * 16 + (l & 15);
-            float v[4];
-            scaled4(acc[r][c], sa[r], s1[c], v);
-            if (DUAL) {
-                float g[4];
-                scaled4(acc[r][c + RB / 2], sa[r], s2[c], g);
+            if (rb > last_rb) break;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = swiglu_f32(v[i], g[i]);
+            for (int c = 0; c < kOut; ++c) {
+                float v[4];
+                scaled4(acc[r][c], sa[r], s1[c], v);
+                if (DUAL) {
+                    float g[4];
+                    scaled4(acc[r][c + RB / 2], sa[r], s2[c], g);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = swiglu_f32(v[i], g[i]);
+                }
+                uint8_t *at = patch + (l & 15) * kPitch + (c * 16 + (l >> 4) * 4) * kSize;
+                if (F32) *reinterpret_cast<float4 *>(at) = make_float4(v[0], v[1], v[2], v[3]);
+                else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
             }
-            store4(p, row, col, v);
+#pragma unroll
+            for (int i = 0; i < 16 / kAtOnce; ++i) {
+                const int at = i * kAtOnce + l / kLanes;
+                const uint4 v = *reinterpret_cast<const uint4 *>(patch + at * kPitch + l % kLanes * 16);
+                const int64_t row = (int64_t)rb * 16 + at;
+                if (row < p.M && col0 < p.N) *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.C) + (row * p.ldc + col0) * kSize) = v;
+            }
         }
-    }
+    };
+    if (!DUAL && p.c_f32) store(std::true_type{});
+    else store(std::false_type{});
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------
-// RB blocks of 16 rows by CB blocks of 16 columns to a workgroup, whose 8 waves share K out and add their sums, integers, in LDS.
+// RB blocks of 16 rows by CB blocks of 16 columns to a workgroup, whose waves share K out and add their sums, integers, in LDS.
 // Weights and rows come straight from memory in the order of the lanes; bound by the weights' bytes.
-constexpr int kFewWaves = 8;
-template <int RB, int CB, bool DUAL> __global__ __launch_bounds__(64 * kFewWaves) void i8_few_kernel(I8Params p) {
+template <int RB, int CB, int WAVES, bool DUAL> __global__ __launch_bounds__(64 * WAVES) void i8_few_kernel(I8Params p) {
     constexpr int NB = DUAL ? 2 * CB : CB;
-    __shared__ v4i_t part[kFewWaves][RB * NB][64];
+    __shared__ v4i_t part[WAVES][RB * NB][64];
     I8Tile tile;
     if (!find_tile(p, 16 * RB, blockIdx.x, tile)) return;
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -274,7 +290,7 @@ template <int RB, int CB, bool DUAL> __global__ __launch_bounds__(64 * kFewWaves
         const int at = first_cb + c % CB, cb = at < col_blocks ? at : col_blocks - 1;
         b_src[c] = (c < CB ? p.B : p.B2) + ((int64_t)tile.expert * col_blocks + cb) * KB * 1024 + l * 16;
     }
-    const int share = (KB + kFewWaves - 1) / kFewWaves;
+    const int share = (KB + WAVES - 1) / WAVES;
     const int k1 = (w + 1) * share < KB ? (w + 1) * share : KB;
     v4i_t acc[RB][NB];
 #pragma unroll
@@ -298,7 +314,7 @@ template <int RB, int CB, bool DUAL> __global__ __launch_bounds__(64 * kFewWaves
 #pragma unroll
                 for (int r = 0; r < RB; ++r) acc[r][c] = mfma_i8(fb[u][c], fa[u][r], acc[r][c]);
     };
-    constexpr int U = RB * NB >= 8 ? 4 : 8;
+    constexpr int U = RB + NB > 4 ? 4 : 8;
     int k = w * share;
     for (; k + U <= k1; k += U) steps(std::integral_constant<int, U>{}, k);
     for (; k + 2 <= k1; k += 2) steps(std::integral_constant<int, 2>{}, k);
@@ -309,13 +325,13 @@ template <int RB, int CB, bool DUAL> __global__ __launch_bounds__(64 * kFewWaves
         for (int c = 0; c < NB; ++c) part[w][r * NB + c][l] = acc[r][c];
     __syncthreads();
     const float *sb = p.sb + (int64_t)tile.expert * p.N, *sb2 = DUAL ? p.sb2 + (int64_t)tile.expert * p.N : nullptr;
-    for (int i = w; i < RB * CB; i += kFewWaves) {
+    for (int i = w; i < RB * CB; i += WAVES) {
         const int r = i / CB, c = i % CB, rb = first_rb + r, cb = first_cb + c;
         if (rb > last_rb || cb >= col_blocks) continue;
         auto sum = [&](int block) {
             v4i_t v = part[0][block][l];
 #pragma unroll
-            for (int x = 1; x < kFewWaves; ++x) v += part[x][block][l];
+            for (int x = 1; x < WAVES; ++x) v += part[x][block][l];
             return v;
         };
         const int64_t row = (int64_t)rb * 16 + (l & 15), col = (int64_t)cb * 16 + (l >> 4) * 4;
@@ -350,8 +366,8 @@ template <bool DUAL> void launch_form(const I8GemmArgs &a, hipStream_t st) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, st, p);
     };
     profile_before(DUAL ? kTagI8Swiglu : kTagI8Gemm, st);
-    if (rows <= 16) go(i8_few_kernel<1, 1, DUAL>, 16, 16, 64 * kFewWaves);
-    else if (rows <= 32) go(i8_few_kernel<2, 1, DUAL>, 32, 16, 64 * kFewWaves);
+    if (rows <= 16) go(i8_few_kernel<1, 1, 8, DUAL>, 16, 16, 512);
+    else if (rows <= 32) go(i8_few_kernel<2, 1, 8, DUAL>, 32, 16, 512);
     else if (rows <= 256) go(i8_tile_kernel<2, DUAL>, 128, DUAL ? 64 : 128, 256);
     else go(i8_tile_kernel<4, DUAL>, 256, DUAL ? 128 : 256, 256);
     profile_after(st);
