@@ -7,6 +7,8 @@
 // is one 1 KB load, to LDS or straight to registers, with nothing to permute and no LDS bank conflicts.
 // With experts the rows of C are sorted by expert and every expert's start at a multiple of 16; a workgroup finds its expert from the
 // offsets on the device, so that nothing waits for the host.
+#include <cmath>
+
 #include "ssg_gemm_tile.h"
 #include "ssg_i8.h"
 
@@ -355,21 +357,54 @@ int64_t row_tiles_bound(const I8GemmArgs &a, int edge) {
     return (a.M + active * (edge - 16)) / edge;
 }
 
+// Which kernel, from the extents alone.
+// One matrix.  Up to 16 and up to 32 rows the blocks that fit them.  Then 64 x 32 where 128 x 128 tiles would leave three quarters
+// of the chip idle (4096 x 11008 by 128 rows 20 us and 49 in 32 tiles; 1040 x 2736 by 333 8 and 12; with 96 tiles, 4096 x 4096 by 333,
+// 22 and 17), and up to 64 rows always (11008 x 4096 17.5 and 19.6).
+// Experts: blocks of 16 rows while an expert has no more on average than 12, which reads weights at 6.0 TB/s (64 experts, d = 2048,
+// f = 1376, 64 tokens of 8: gate/up 60 us, 69 in 128 x 128 tiles; with 16 rows on average 74 and 72, with 32 120 and 77).
+// Between the tiles: estimated times, where a step of 64 along K takes a compute unit .52 us with two small tiles on it, .28 with
+// one, .70 with a large one, and a tile 4 and 9 us beside its steps; with experts half a tile each beyond their average
+// rows.  (4096 x 4096 x 11008 133 us in large and 176 in small tiles, 2048 rows 102 and 92; the 64 experts at 4096 tokens 223 and
+// 241, at 2048 161 and 141.  Over 98 products 3 % above the better one on average, at most 14 %.)
+enum I8Form { FEW_16, FEW_16_EXPERTS, FEW_32, FEW_64, TILE_128, TILE_256 };
+I8Form choose_form(const I8GemmArgs &a, bool dual) {
+    const double KB = (double)((a.K + 63) / 64), small_step = .52 * KB + 4, small_alone = .28 * KB + 4, large_step = .70 * KB + 9;
+    const int64_t cols = dual ? 2 * a.N : a.N, cols128 = (cols + 127) / 128, cols256 = (cols + 255) / 256;
+    if (!a.offsets) {
+        const int64_t tiles128 = (a.M + 127) / 128 * cols128, tiles256 = (a.M + 255) / 256 * cols256;
+        if (a.M <= 16) return FEW_16;
+        if (a.M <= 32) return FEW_32;
+        if (a.M <= 64 || tiles128 <= 64) return FEW_64;
+        const int64_t rounds = tiles128 / 512, rest = tiles128 % 512;
+        const double small = rounds * small_step + (rest == 0 ? 0 : rest <= 256 ? small_alone : small_step);
+        return (double)((tiles256 + 255) / 256) * large_step < small ? TILE_256 : TILE_128;
+    }
+    const double active = (double)std::min<int64_t>(a.E, a.rows_expected), rows = (double)a.rows_expected / active;
+    if (rows <= 12) return FEW_16_EXPERTS;
+    const double small = active * std::max(1.0, rows / 128 + .5) * cols128 / 512 * small_step;
+    const double large = std::ceil(active * std::max(1.0, rows / 256 + .5) * cols256 / 256) * large_step;
+    return large < small ? TILE_256 : TILE_128;
+}
+
 template <bool DUAL> void launch_form(const I8GemmArgs &a, hipStream_t st) {
     I8Params p;
     p.A = a.A; p.B = a.B; p.B2 = a.B2; p.sa = a.sa; p.sb = a.sb; p.sb2 = a.sb2; p.C = a.C;
     p.M = a.M; p.N = a.N; p.ldc = a.ldc; p.KB = (int)((a.K + 63) / 64); p.c_f32 = a.c_f32; p.offsets = a.offsets; p.E = a.E;
-    const double rows = a.offsets ? (double)a.rows_expected / a.E : (double)a.M;       // to an expert, on average
     auto go = [&](auto kernel, int edge, int cols, int threads) {
         p.tiles_n = (int)((a.N + cols - 1) / cols);
         const int64_t blocks = row_tiles_bound(a, edge) * p.tiles_n;
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, st, p);
     };
     profile_before(DUAL ? kTagI8Swiglu : kTagI8Gemm, st);
-    if (rows <= 16) go(i8_few_kernel<1, 1, 8, DUAL>, 16, 16, 512);
-    else if (rows <= 32) go(i8_few_kernel<2, 1, 8, DUAL>, 32, 16, 512);
-    else if (rows <= 256) go(i8_tile_kernel<2, DUAL>, 128, DUAL ? 64 : 128, 256);
-    else go(i8_tile_kernel<4, DUAL>, 256, DUAL ? 128 : 256, 256);
+    switch (choose_form(a, DUAL)) {
+        case FEW_16: go(i8_few_kernel<1, 1, 8, DUAL>, 16, 16, 512); break;
+        case FEW_16_EXPERTS: go(i8_few_kernel<1, 1, 4, DUAL>, 16, 16, 256); break;
+        case FEW_32: go(i8_few_kernel<2, 1, 4, DUAL>, 32, 16, 256); break;
+        case FEW_64: go(i8_few_kernel<4, 2, 8, DUAL>, 64, 32, 512); break;
+        case TILE_128: go(i8_tile_kernel<2, DUAL>, 128, DUAL ? 64 : 128, 256); break;
+        case TILE_256: go(i8_tile_kernel<4, DUAL>, 256, DUAL ? 128 : 256, 256); break;
+    }
     profile_after(st);
 }
 
