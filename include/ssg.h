@@ -383,7 +383,7 @@ ssg_status ssg_adam_view_state(int64_t n, int32_t step, const void *state, ssg_a
  * No atomics decide an order: results are the same bits in every call. */
 typedef enum { SSG_ROUTE_SOFTMAX = 0, SSG_ROUTE_SIGMOID = 1 } ssg_route_score;
 typedef struct {
-    int64_t T;               /* tokens, T * k up to 2^26 */
+    int64_t T;               /* tokens, up to 2^22 - 1024, T * k up to 2^26 */
     int64_t ld;              /* elements from one token's logits to the next, at least E */
     int32_t E, k;            /* up to 1024 experts, up to 32 chosen */
     int32_t logits_dtype;    /* ssg_dtype */

@@ -271,7 +271,7 @@ struct RouteArgs {
     int *ids = nullptr;              // [T, k]
     float *weights = nullptr;        // [T, k]
     int *counts = nullptr, *offsets = nullptr, *place = nullptr, *source = nullptr;   // all or none (place decides)
-    uint32_t *hist = nullptr;        // route_hist_words() words
+    uint16_t *hist = nullptr;        // route_hist_bytes() bytes
     int64_t T = 0, ld = 0, rows = 0;
     int E = 0, k = 0, bf16 = 0, score = 0, groups = 1, top_groups = 1, group_top = 1, renorm = 0, align = 1;
     float scale = 1.0f;
@@ -295,7 +295,8 @@ struct CombineArgs {
     int k = 0, f32 = 0;
 };
 constexpr int kMaxExperts = 1024, kMaxChosen = 32, kMaxGroups = 64;
-size_t route_hist_words(const RouteArgs &a);
+constexpr int64_t kMaxTokens = ((int64_t)1 << 22) - 1024;     // a block of 64 for 1024 experts counts them in 16 bits
+size_t route_hist_bytes(const RouteArgs &a);
 void launch_route(RouteArgs a, hipStream_t st);
 void launch_route_bwd(const RouteBwdArgs &a, hipStream_t st);
 void launch_combine(const CombineArgs &a, hipStream_t st);

@@ -18,8 +18,8 @@ ssg_status check_route(const ssg_route_desc *d, const char *who) {
     if (d->E < 1 || d->E > ssg::kMaxExperts) return fail(SSG_ERR_SHAPE, "%s: E = %d experts (1 to %d)", who, d->E, ssg::kMaxExperts);
     if (d->k < 1 || d->k > ssg::kMaxChosen || d->k > d->E)
         return fail(SSG_ERR_SHAPE, "%s: k = %d of %d experts (1 to %d)", who, d->k, d->E, ssg::kMaxChosen);
-    if (d->T < 0 || d->T > kMaxAssignments / d->k)
-        return fail(SSG_ERR_SHAPE, "%s: T = %lld tokens (T k from 0 to %lld)", who, (long long)d->T, (long long)kMaxAssignments);
+    if (d->T < 0 || d->T > std::min(ssg::kMaxTokens, kMaxAssignments / d->k))
+        return fail(SSG_ERR_SHAPE, "%s: T = %lld tokens (0 to %lld, T k to %lld)", who, (long long)d->T, (long long)ssg::kMaxTokens, (long long)kMaxAssignments);
     if (d->ld < d->E || d->ld > ((int64_t)1 << 31)) return fail(SSG_ERR_SHAPE, "%s: ld = %lld below E = %d, or too large", who, (long long)d->ld, d->E);
     if (!dtype_ok(d->logits_dtype)) return fail(SSG_ERR_ARG, "%s: logits_dtype %d", who, d->logits_dtype);
     if (d->score != SSG_ROUTE_SOFTMAX && d->score != SSG_ROUTE_SIGMOID) return fail(SSG_ERR_ARG, "%s: score %d", who, d->score);
@@ -100,7 +100,7 @@ MoeLayout moe_layout(const ssg_moe_desc &d) {
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o += align256(bytes); return at; };
     L.ids = take(n * 4); L.weights = take(n * 4); L.counts = take((size_t)r.E * 4); L.offsets = take(((size_t)r.E + 1) * 4);
-    L.place = take(n * 4); L.source = take((size_t)L.rows * 4); L.hist = take(ssg::route_hist_words(route_args(r)) * 4);
+    L.place = take(n * 4); L.source = take((size_t)L.rows * 4); L.hist = take(ssg::route_hist_bytes(route_args(r)));
     L.x_q = take(i8_bytes(L.rows, d.d));
     L.h = take((size_t)L.rows * d.f * 2);
     L.h_q = take(i8_bytes(L.rows, d.f));
@@ -128,7 +128,7 @@ ssg_status check_moe(const ssg_moe_desc *d, const char *who) {
 // ---- routing -------------------------------------------------------------------------------------------
 size_t ssg_route_workspace_bytes(const ssg_route_desc *desc) {
     if (check_route(desc, "ssg_route_workspace_bytes") != SSG_OK) return 0;
-    return std::max<size_t>(align256(ssg::route_hist_words(route_args(*desc)) * 4), 256);
+    return std::max<size_t>(align256(ssg::route_hist_bytes(route_args(*desc))), 256);
 }
 
 int64_t ssg_route_rows(const ssg_route_desc *desc) {
@@ -151,14 +151,14 @@ ssg_status ssg_route(const ssg_route_desc *desc, const void *logits, const float
     SSG_CHECK(check_ptr(who, "place", place, 4, sorts && tokens));
     SSG_CHECK(check_ptr(who, "source", source, 4, sorts && tokens));
     ssg::RouteArgs a = route_args(*desc);
-    const size_t need = sorts ? ssg::route_hist_words(a) * 4 : 0;
+    const size_t need = sorts ? ssg::route_hist_bytes(a) : 0;
     if (need) {
         SSG_CHECK(check_ptr(who, "workspace", workspace, 16, true));
         if (workspace_bytes < need) return fail(SSG_ERR_WORKSPACE, "%s: workspace holds %zu bytes, %zu needed", who, workspace_bytes, need);
     }
     SSG_CHECK(check_entry(who));
     a.logits = logits; a.bias = bias; a.ids = ids; a.weights = weights; a.counts = counts; a.offsets = offsets; a.place = place; a.source = source;
-    a.hist = static_cast<uint32_t *>(workspace);
+    a.hist = static_cast<uint16_t *>(workspace);
     ssg::launch_route(a, (hipStream_t)stream);
     return check_launch(who);
 }
@@ -319,7 +319,7 @@ ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logi
     a.ids = reinterpret_cast<int *>(b + L.ids); a.weights = reinterpret_cast<float *>(b + L.weights);
     a.counts = reinterpret_cast<int *>(b + L.counts); a.offsets = reinterpret_cast<int *>(b + L.offsets);
     a.place = reinterpret_cast<int *>(b + L.place); a.source = reinterpret_cast<int *>(b + L.source);
-    a.hist = reinterpret_cast<uint32_t *>(b + L.hist);
+    a.hist = reinterpret_cast<uint16_t *>(b + L.hist);
     ssg::launch_route(a, st);
 
     // x in the order of the experts, a scale for each token

@@ -16,6 +16,7 @@ namespace ssg {
 
 namespace {
 
+constexpr int kOneLaunch = 64;                            // tokens that one block chooses for and sorts
 constexpr int kBlock = 1024;                              // threads of the kernels that choose and sort
 constexpr int kWaves = kBlock / 64;
 
@@ -38,8 +39,11 @@ template <int LPT, class Op> __device__ __forceinline__ uint32_t reduce(uint32_t
     v = op(v, exchange<2>(v));
     v = op(v, exchange<3>(v));
     if (LPT == 64) {
-        v = op(v, (uint32_t)__shfl_xor((int)v, 16, 64));
-        v = op(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+        // both operands the same: the even rows (the lower half) in one result and the odd ones (the upper half) in the other
+        const auto rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = op(rows[0], rows[1]);
+        const auto halves = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = op(halves[0], halves[1]);
     }
     return v;
 }
@@ -114,12 +118,14 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t t, bool live,
         __threadfence_block();
         const int group = g0 / L, sub = g0 % L;
         uint32_t first = 0, second = 0;
-        if (group < a.groups)
+        if (group < a.groups) {
+#pragma unroll 4
             for (int i = sub; i < size; i += L) {
                 const uint32_t u = keys[group * size + i];
                 second = u > first ? first : (u > second ? u : second);
                 first = u > first ? u : first;
             }
+        }
         for (int step = 1; step < L; step *= 2) {
             const uint32_t f = (uint32_t)__shfl_xor((int)first, step, 64), s = (uint32_t)__shfl_xor((int)second, step, 64);
             const uint32_t low = f > first ? first : f;
@@ -231,9 +237,13 @@ __device__ __forceinline__ void scatter(const RouteArgs &a, const SortLds &s, in
         }
         __syncthreads();
     }
-    // rows that fill up an expert's last set, and those beyond all experts
-    for (int e = block; e < a.E; e += blocks)
-        for (int64_t r = (int64_t)s.offset[e] + s.total[e] + tid; r < s.offset[e + 1]; r += kBlock) a.source[r] = -1;
+    // rows that fill up an expert's last set (fewer than the alignment; all experts' side by side, since one after the other 256 of them
+    // took 23 us), and those beyond all experts
+    for (int i = block * kBlock + tid; i < a.E * a.align; i += blocks * kBlock) {
+        const int e = i / a.align;
+        const uint32_t r = s.offset[e] + s.total[e] + (uint32_t)(i % a.align);
+        if (r < s.offset[e + 1]) a.source[r] = -1;
+    }
     for (int64_t r = s.offset[a.E] + (int64_t)block * kBlock + tid; r < a.rows; r += (int64_t)blocks * kBlock) a.source[r] = -1;
     if (block == 0)
         for (int e = tid; e <= a.E; e += kBlock) {
@@ -243,6 +253,9 @@ __device__ __forceinline__ void scatter(const RouteArgs &a, const SortLds &s, in
 }
 
 __device__ __forceinline__ SortLds sort_lds(uint32_t *lds, int E) { return SortLds{lds, lds + E, lds + 2 * E, lds + 3 * E + 1}; }
+
+// Counts of a block: at most its tokens, since a token takes an expert once; 16 bits each, rows of 16 bytes.
+__host__ __device__ constexpr int hist_stride(int E) { return (E + 7) & ~7; }
 
 // One block per a.block_tokens tokens.  With one block in all it sorts too; otherwise it leaves its experts' counts.
 template <int LPT, int VPL, bool BF16> __global__ __launch_bounds__(kBlock) void route_kernel(RouteArgs a) {
@@ -273,8 +286,8 @@ template <int LPT, int VPL, bool BF16> __global__ __launch_bounds__(kBlock) void
     if (!a.place) return;
     __syncthreads();                                       // (also: this block's ids are visible to it)
     if (gridDim.x > 1) {
-        const int stride = (a.E + 3) & ~3;
-        for (int e = tid; e < stride; e += kBlock) a.hist[(size_t)blockIdx.x * stride + e] = e < a.E ? hist[e] : 0;
+        const int stride = hist_stride(a.E);
+        for (int e = tid; e < stride; e += kBlock) a.hist[(size_t)blockIdx.x * stride + e] = (uint16_t)(e < a.E ? hist[e] : 0);
         return;
     }
     const SortLds s = sort_lds(lds, a.E);
@@ -283,35 +296,44 @@ template <int LPT, int VPL, bool BF16> __global__ __launch_bounds__(kBlock) void
     scatter(a, s, 0, a.T * a.k, 0, 1);
 }
 
-// Second launch where there are several blocks: every block sums up all blocks' counts (up to 256 KB, out of the L2) for the
+// Second launch where there are several blocks: every block sums up all blocks' counts (up to 128 KB, out of the L2) for the
 // experts' totals and for what lies before its own tokens.
 __global__ __launch_bounds__(kBlock) void dispatch_kernel(RouteArgs a, int blocks) {
     extern __shared__ uint32_t lds[];
     __shared__ uint32_t wave_sum[kWaves];
     const SortLds s = sort_lds(lds, a.E);
     const int tid = threadIdx.x, block = blockIdx.x;
-    for (int e = tid; e < 2 * a.E; e += kBlock) lds[e] = 0;
+    // sums of expert 8 q + i lie at i * eights + q meanwhile, so that neighbouring lanes are in neighbouring banks
+    const int eights = hist_stride(a.E) / 8, parts = kBlock / eights;          // E <= 1024: at least eight parts
+    uint32_t *total = s.wave_count, *before = total + 8 * eights;
+    for (int i = tid; i < 16 * eights; i += kBlock) total[i] = 0;
     __syncthreads();
-    const int quads = (a.E + 3) / 4, parts = kBlock / quads;          // E <= 1024: at least four parts
-    const int q = tid % quads, part = tid / quads;
+    const int q = tid % eights, part = tid / eights;
     if (part < parts) {
-        uint32_t total[4] = {0, 0, 0, 0}, before[4] = {0, 0, 0, 0};
+        uint32_t all[8] = {}, mine[8] = {};
 #pragma unroll 4
         for (int b = part; b < blocks; b += parts) {
-            const uint4 v = reinterpret_cast<const uint4 *>(a.hist)[(size_t)b * quads + q];
+            const uint4 v = reinterpret_cast<const uint4 *>(a.hist)[(size_t)b * eights + q];
             const uint32_t n[4] = {v.x, v.y, v.z, v.w};
+            const uint32_t mask = b < block ? 0xffffffffu : 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                total[i] += n[i];
-                if (b < block) before[i] += n[i];
+                all[2 * i] += n[i] & 0xffff;
+                all[2 * i + 1] += n[i] >> 16;
+                mine[2 * i] += n[i] & mask & 0xffff;
+                mine[2 * i + 1] += (n[i] & mask) >> 16;
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (4 * q + i < a.E) {
-                atomicAdd(&s.total[4 * q + i], total[i]);
-                atomicAdd(&s.before[4 * q + i], before[i]);
-            }
+        for (int i = 0; i < 8; ++i) {
+            atomicAdd(&total[i * eights + q], all[i]);
+            atomicAdd(&before[i * eights + q], mine[i]);
+        }
+    }
+    __syncthreads();
+    for (int e = tid; e < a.E; e += kBlock) {
+        s.total[e] = total[e % 8 * eights + e / 8];
+        s.before[e] = before[e % 8 * eights + e / 8];
     }
     __syncthreads();
     scan_offsets(a, s, wave_sum);
@@ -467,22 +489,19 @@ template <bool F32> __global__ __launch_bounds__(256) void combine_kernel(Combin
 }
 
 // Tokens to a block, so that there are at most 256 blocks and 64 K counts (which every block of the second launch reads).
-constexpr int kOneLaunch = 128;                            // tokens that one block chooses for and sorts
 int most_blocks(int E) { return std::min(256, 65536 / E); }
 struct RoutePlan { int lpt, vpl, block_tokens, blocks; };
 RoutePlan route_plan(const RouteArgs &a) {
     RoutePlan p;
-    // 16 lanes to a token choose for four tokens in one wave; 64 where the experts, their groups or k need them, and for the
-    // few tokens of a decode step, which are a wave's latency whatever the others do
-    p.lpt = a.E > 256 || a.k > 16 || a.groups > 16 || a.T <= 16 ? 64 : 16;
+    // 16 lanes to a token choose for four tokens in one wave, which bounds long batches; 64 where the experts, their groups or k need
+    // them, and up to 4096 tokens, which 256 blocks take at once and where a token's own time counts
+    p.lpt = a.E > 256 || a.k > 16 || a.groups > 16 || a.T <= 4096 ? 64 : 16;
     p.vpl = 1;
     while (p.vpl * p.lpt < a.E) p.vpl *= 2;
-    const int most = most_blocks(a.E);
-    const int64_t pass = kBlock / p.lpt;
-    int64_t tokens = (a.T + most - 1) / most;
-    tokens = (tokens + pass - 1) / pass * pass;
-    if (a.T <= kOneLaunch) tokens = std::max<int64_t>(tokens, a.T);          // one launch: a second costs more than a longer block
-    p.block_tokens = (int)std::min<int64_t>(tokens, 1 << 30);
+    const int64_t pass = kBlock / p.lpt, most = most_blocks(a.E);
+    // one block chooses for and sorts what one launch can take: a second one costs more than its passes
+    const int64_t tokens = a.T <= kOneLaunch ? a.T : (a.T + most - 1) / most;
+    p.block_tokens = (int)((tokens + pass - 1) / pass * pass);
     p.blocks = (int)((a.T + p.block_tokens - 1) / p.block_tokens);
     return p;
 }
@@ -502,9 +521,9 @@ __global__ void no_rows_kernel(int *counts, int *offsets, int E) {
 
 }  // namespace
 
-size_t route_hist_words(const RouteArgs &a) {
+size_t route_hist_bytes(const RouteArgs &a) {
     // (of the most blocks, so that it does not fall as T grows)
-    return a.T > kOneLaunch ? (size_t)most_blocks(a.E) * ((a.E + 3) & ~3) : 0;
+    return a.T > kOneLaunch ? (size_t)most_blocks(a.E) * hist_stride(a.E) * sizeof(uint16_t) : 0;
 }
 
 void launch_route(RouteArgs a, hipStream_t st) {
@@ -515,7 +534,7 @@ void launch_route(RouteArgs a, hipStream_t st) {
     const RoutePlan p = route_plan(a);
     a.block_tokens = p.block_tokens;
     const bool grouped = a.top_groups < a.groups;
-    const size_t sort_words = 3 * (size_t)a.E + 1 + (size_t)kWaves * a.E;
+    const size_t sort_words = 3 * (size_t)a.E + 1 + (size_t)kWaves * hist_stride(a.E);
     // the keys of all tokens in hand (with groups), and the sort's words; in the launch that sorts too, one after the other
     a.lds_keys = a.E;
     const size_t key_words = a.E + (grouped ? (size_t)kBlock / p.lpt * a.E : 0);
