@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libssg.so")
 SOURCES = ["ssg_api.hip", "ssg_quant.hip", "ssg_gemm.hip", "ssg_gemm_bwd.hip", "ssg_gemm_skinny.hip", "ssg_adam.hip",
-           "ssg_route.hip", "ssg_i8_rows.hip", "ssg_i8_gemm.hip", "ssg_moe_api.hip"]
+           "ssg_route.hip", "ssg_i8_rows.hip", "ssg_i8_gemm.hip", "ssg_i8_token.hip", "ssg_moe_api.hip"]
 PROBE_LIB = os.path.join(HERE, "libssg_probe.so")
 PROBE_SOURCES = ["ssg_probe.hip"]
 

@@ -332,6 +332,35 @@ struct I8GemmArgs {
     int64_t rows_expected = 0;       // with offsets: rows that tokens fill, of M
 };
 void launch_i8_gemm(const I8GemmArgs &a, hipStream_t st);
+// Up to kTokenRows tokens, quantized where they are used (ssg_i8_token.hip); i8_token_ok and i8_mix_ok: whether their codes fit LDS.
+constexpr int kTokenRows = 4;
+constexpr int64_t kTokenLds = 64 << 10, kMixLds = 128 << 10;
+struct I8TokenArgs {
+    const void *src = nullptr;       // rows of K, `ld` elements apart
+    const uint8_t *B = nullptr, *B2 = nullptr;
+    const float *sb = nullptr, *sb2 = nullptr;
+    void *C = nullptr;
+    int64_t N = 0, K = 0, ld = 0, ldc = 0;
+    int rows = 1;                    // of src and C, without ids
+    int bf16 = 0, c_f32 = 0;
+    const int *ids = nullptr;        // [pairs]: row p of C is row p / k of src times the matrices of expert ids[p] (nothing: below zero)
+    int64_t pairs = 0;
+    int k = 1;
+};
+void launch_i8_token(const I8TokenArgs &a, hipStream_t st);
+struct I8MixArgs {
+    const void *h = nullptr;         // bf16 [T k, K]
+    const uint8_t *B = nullptr;
+    const float *sb = nullptr;
+    const int *ids = nullptr;        // [T, k]
+    const float *weights = nullptr;
+    void *y = nullptr;               // [T, N], fp32 (f32 = 1) or bf16
+    int64_t T = 0, N = 0, K = 0;
+    int k = 1, f32 = 0, split = 1;   // split: filled in by the launcher
+};
+void launch_i8_mix(I8MixArgs a, hipStream_t st);
+bool i8_token_ok(int64_t T, int64_t K);
+bool i8_mix_ok(int64_t T, int64_t d, int64_t f, int k);
 constexpr int kTagRoute = 48, kTagDispatch = 49, kTagRouteBwd = 50, kTagCombine = 51, kTagI8Rows = 52, kTagI8Gemm = 53, kTagI8Swiglu = 54;
 
 }  // namespace ssg

@@ -109,6 +109,9 @@ MoeLayout moe_layout(const ssg_moe_desc &d) {
     return L;
 }
 
+// Up to four tokens run without an order of dispatch: a token's experts are its own.
+bool few_tokens(const ssg_moe_desc &d) { return ssg::i8_mix_ok(d.route.T, d.d, d.f, d.route.k); }
+
 ssg_status check_moe(const ssg_moe_desc *d, const char *who) {
     if (!d) return fail(SSG_ERR_ARG, "%s: desc is NULL", who);
     SSG_CHECK(check_route(&d->route, who));
@@ -259,6 +262,13 @@ ssg_status ssg_i8_linear(const void *x, ssg_dtype x_dtype, int64_t M, int64_t K,
     SSG_CHECK(check_i8_buffer(who, "W", W, W_bytes, N, K));
     SSG_CHECK(check_i8_buffer(who, "workspace", workspace, workspace_bytes, M, K));
     SSG_CHECK(check_entry(who));
+    if (ssg::i8_token_ok(M, K)) {
+        ssg::I8TokenArgs k;
+        k.src = x; k.rows = (int)M; k.K = K; k.ld = ldx; k.bf16 = x_dtype == SSG_BF16;
+        k.B = static_cast<const uint8_t *>(W); k.sb = i8_scales(W, N, K); k.C = y; k.N = N; k.ldc = ldy; k.c_f32 = y_dtype == SSG_F32;
+        ssg::launch_i8_token(k, (hipStream_t)stream);
+        return check_launch(who);
+    }
     ssg::I8RowsArgs a;
     a.src = x; a.codes = static_cast<uint8_t *>(workspace); a.scales = const_cast<float *>(i8_scales(workspace, M, K));
     a.rows = M; a.K = K; a.ld = ldx; a.bf16 = x_dtype == SSG_BF16;
@@ -284,11 +294,18 @@ ssg_status ssg_moe_view_workspace(const ssg_moe_desc *desc, const void *workspac
     out->rows = L.rows;
     out->ids = reinterpret_cast<const int32_t *>(b + L.ids);
     out->weights = reinterpret_cast<const float *>(b + L.weights);
+    out->h = b + L.h;
+    out->counts = out->offsets = out->place = out->source = nullptr;
+    out->x_q = out->h_q = out->o = nullptr;
+    if (few_tokens(*desc)) {
+        out->rows = desc->route.T * desc->route.k;
+        return SSG_OK;
+    }
     out->counts = reinterpret_cast<const int32_t *>(b + L.counts);
     out->offsets = reinterpret_cast<const int32_t *>(b + L.offsets);
     out->place = reinterpret_cast<const int32_t *>(b + L.place);
     out->source = reinterpret_cast<const int32_t *>(b + L.source);
-    out->x_q = b + L.x_q; out->h = b + L.h; out->h_q = b + L.h_q; out->o = b + L.o;
+    out->x_q = b + L.x_q; out->h_q = b + L.h_q; out->o = b + L.o;
     return SSG_OK;
 }
 
@@ -320,6 +337,22 @@ ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logi
     a.counts = reinterpret_cast<int *>(b + L.counts); a.offsets = reinterpret_cast<int *>(b + L.offsets);
     a.place = reinterpret_cast<int *>(b + L.place); a.source = reinterpret_cast<int *>(b + L.source);
     a.hist = reinterpret_cast<uint16_t *>(b + L.hist);
+    if (few_tokens(*desc)) {
+        // h row t k + j for assignment (t, j): no order of dispatch, nothing quantized goes through memory
+        a.counts = a.offsets = a.place = a.source = nullptr;
+        ssg::launch_route(a, st);
+        ssg::I8TokenArgs u;
+        u.src = x; u.K = d; u.ld = d; u.bf16 = 1; u.ids = a.ids; u.pairs = r.T * r.k; u.k = r.k;
+        u.B = static_cast<const uint8_t *>(W1); u.sb = i8_scales(W1, E * f, d);
+        u.B2 = static_cast<const uint8_t *>(W2); u.sb2 = i8_scales(W2, E * f, d);
+        u.C = b + L.h; u.N = f; u.ldc = f;
+        ssg::launch_i8_token(u, st);
+        ssg::I8MixArgs m;
+        m.h = b + L.h; m.B = static_cast<const uint8_t *>(W3); m.sb = i8_scales(W3, E * d, f); m.ids = a.ids; m.weights = a.weights;
+        m.y = y; m.T = r.T; m.N = d; m.K = f; m.k = r.k; m.f32 = desc->y_dtype == SSG_F32;
+        ssg::launch_i8_mix(m, st);
+        return check_launch(who);
+    }
     ssg::launch_route(a, st);
 
     // x in the order of the experts, a scale for each token

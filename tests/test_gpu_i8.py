@@ -135,7 +135,7 @@ def test_largest_sums_stay_exact():
 
 @pytest.mark.parametrize("x_dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("y_dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("M,K,N", [(1, 64, 16), (1, 2736, 1040), (3, 4096, 528), (8, 11008, 256), (16, 1040, 272), (17, 80, 48), (33, 336, 272), (260, 1040, 784)])
+@pytest.mark.parametrize("M,K,N", [(1, 16, 16), (2, 528, 48), (4, 14352, 32), (4, 16384, 16), (1, 28672, 64), (1, 64, 16), (1, 2736, 1040), (3, 4096, 528), (8, 11008, 256), (16, 1040, 272), (17, 80, 48), (33, 336, 272), (260, 1040, 784)])
 def test_linear(x_dtype, y_dtype, M, K, N):
     x, W = rows_of(M, K + 8, x_dtype, M).to(DEV), rows_of(N, K, torch.bfloat16, N).to(DEV)
     x[M // 2] = 0

@@ -44,40 +44,50 @@ class Layer:
         E, k, d, f = self.E, self.k, self.d, self.f
         ids = read(self.work, v.ids, self.T * k, torch.int32).view(self.T, k).cpu().numpy()
         w = read(self.work, v.weights, self.T * k, torch.float32).view(self.T, k).cpu().numpy().astype(np.float64)
-        counts, offsets, place, source = route.dispatch(ids, E, 16, v.rows)
-        for name, ref, n in (("counts", counts, E), ("offsets", offsets, E + 1), ("place", place, self.T * k), ("source", source, v.rows)):
-            assert np.array_equal(read(self.work, getattr(v, name), n, torch.int32).cpu().numpy(), ref), name
-        live = int(offsets[-1])
-        real = source[:live] >= 0
+        if v.offsets is None:                                  # up to four tokens: no order of dispatch, nothing quantized is stored
+            assert self.T <= 4 and v.rows == self.T * k
+            live, flat = self.T * k, ids.reshape(-1)
+            place = np.where(flat >= 0, np.arange(live), -1)
+            rows_of = [np.nonzero(flat == e)[0] for e in range(E)]
+            source, real = np.arange(live), flat >= 0
+        else:
+            counts, offsets, place, source = route.dispatch(ids, E, 16, v.rows)
+            for name, ref, n in (("counts", counts, E), ("offsets", offsets, E + 1), ("place", place, self.T * k), ("source", source, v.rows)):
+                assert np.array_equal(read(self.work, getattr(v, name), n, torch.int32).cpu().numpy(), ref), name
+            live = int(offsets[-1])
+            rows_of = [np.arange(offsets[e], offsets[e] + counts[e]) for e in range(E)]
+            real = source[:live] >= 0
 
-        def quantized(ptr, K):
+        def quantized(ptr, K, want, name):
+            if ptr is None:
+                return
             wide, up = -(-K // 64) * 64, -(-v.rows // 16) * 16
             codes = read(self.work, ptr, live * wide, torch.uint8).cpu().numpy()
             at = -(-up * wide // 256) * 256
-            return codes, read(self.work, ptr + at, live, torch.float32).cpu().numpy()
+            scales = read(self.work, ptr + at, live, torch.float32).cpu().numpy()
+            assert np.array_equal(codes, i8.layout(want[0])) and np.array_equal(scales, want[1]), name
 
         x = f32(self.x)[np.maximum(source[:live], 0) // k] * real[:, None]
         xq, sx = i8.quantize(x)
-        got, s = quantized(v.x_q, d)
-        assert np.array_equal(got, i8.layout(xq)) and np.array_equal(s, sx), "quantized x"
+        quantized(v.x_q, d, (xq, sx), "quantized x")
         h = read(self.work, v.h, live * f, torch.bfloat16).view(live, f).float().cpu().numpy()
+        h[~real] = 0 if v.offsets is None else h[~real]        # (rows of no expert are not written)
         hq, sh = i8.quantize(h)
-        got, s = quantized(v.h_q, f)
-        assert np.array_equal(got, i8.layout(hq)) and np.array_equal(s, sh), "quantized h"
-        o = read(self.work, v.o, live * d, self.y_dtype).view(live, d).float().cpu().numpy()
-        for e in range(E):
-            r = slice(int(offsets[e]), int(offsets[e] + counts[e]))
-            if r.start == r.stop:
+        quantized(v.h_q, f, (hq, sh), "quantized h")
+        o = None if v.o is None else read(self.work, v.o, live * d, self.y_dtype).view(live, d).float().cpu().numpy()
+        expected = np.zeros((live, d))
+        for e, r in enumerate(rows_of):
+            if not len(r):
                 continue
             part = [(c[e * n:(e + 1) * n], t[e * n:(e + 1) * n]) for (_, c, t), n in ((self.W1, f), (self.W2, f), (self.W3, d))]
             u, g = (i8.matmul(xq[r], sx[r], *part[i]).astype(np.float64) for i in (0, 1))
             ref = u * g / (1 + np.exp(-g))
             # u and g are the GPU's own bits; their SwiGLU product is good to 6 ulp of binary32, then rounded to bf16
             assert (np.abs(h[r] - ref) <= bf16_ulp(ref) * (0.5 + 2.0 ** -12)).all()
-            want = torch.from_numpy(i8.matmul(hq[r], sh[r], *part[2])).to(self.y_dtype).float().numpy()
-            assert np.array_equal(o[r], want), f"results of expert {e}"
+            expected[r] = torch.from_numpy(i8.matmul(hq[r], sh[r], *part[2])).to(self.y_dtype).float().numpy()
+            assert o is None or np.array_equal(o[r], expected[r]), f"results of expert {e}"
         p = place.reshape(self.T, k)
-        terms = np.where((p >= 0)[:, :, None], w[:, :, None] * o.astype(np.float64)[np.maximum(p, 0)], 0.0) if live else np.zeros((self.T, k, d))
+        terms = np.where((p >= 0)[:, :, None], w[:, :, None] * expected[np.maximum(p, 0)], 0.0) if live else np.zeros((self.T, k, d))
         ref, size = terms.sum(1), np.abs(terms).sum(1)
         tol = k * 2.0 ** -24 * size + (0.5 * bf16_ulp(ref) if self.y_dtype == torch.bfloat16 else 0.0)
         assert (np.abs(f32(y) - ref) <= tol * (1 + 2.0 ** -10)).all()
@@ -136,6 +146,28 @@ def test_whole_against_binary64():
             ref[t] += weight * (part[2][0] @ hq[0]) * float(sh[0]) * part[2][1]
     # two roundings to bf16 of 2^-9 each, at most, in norm; a code's step is 1/127 of the row's largest in a sum of 336
     assert np.linalg.norm(y - ref) <= 2 * 2.0 ** -9 * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("E,k,d,f", [(1, 1, 64, 48), (9, 2, 1040, 528), (16, 4, 96, 2064), (24, 8, 272, 336), (20, 3, 64, 1040), (40, 20, 80, 64),
+                                     (33, 17, 64, 208), (6, 6, 8208, 16)])
+@pytest.mark.parametrize("y_dtype", [torch.bfloat16, torch.float32])
+def test_few_tokens(E, k, d, f, y_dtype):
+    for T in (1, 2, 4):
+        layer = Layer(T, E, k, d, f, y_dtype=y_dtype, seed=T)
+        if E > 8:
+            layer.logits[:, : E - k + 1] = -torch.inf           # the last choice of every token has no expert
+        layer.check(layer.run())
+
+
+@pytest.mark.parametrize("T", [5, 40, 300])
+@pytest.mark.parametrize("y_dtype", [torch.bfloat16, torch.float32])
+def test_a_token_does_not_depend_on_the_batch(T, y_dtype):
+    layer = Layer(T, 8, 3, 272, 208, y_dtype=y_dtype, score=ssg.SSG_ROUTE_SIGMOID, scale=1.5)
+    whole, x, z = layer.run(), layer.x, layer.logits
+    for first, n in ((0, 1), (3, 2), (T - 4, 4), (0, 5)):
+        part = Layer(n, 8, 3, 272, 208, y_dtype=y_dtype, score=ssg.SSG_ROUTE_SIGMOID, scale=1.5)
+        part.x, part.logits = x[first:first + n].contiguous(), z[first:first + n].contiguous()
+        assert torch.equal(part.run(), whole[first:first + n])
 
 
 def test_another_stream_and_a_graph():
