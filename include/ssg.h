@@ -411,7 +411,7 @@ ssg_status ssg_route_bwd(const ssg_route_desc *desc, const void *logits, const i
  * (scale at least 2^-126, with 2^126 as the factor there; a row of zeros has scale 0; one with a NaN or an infinity a NaN, and codes 0).
  * They live in a buffer of ssg_i8_bytes(rows, K) bytes, 256-byte aligned, in the layout that the products read: blocks of 16 rows by 64
  * codes, 1 KB each, code (r, k) at byte ((r / 16) * (Kp / 64) + k / 64) * 1024 + (k % 64 / 16) * 256 + r % 16 * 16 + k % 16
- * with Kp = K filled up to 64 by zeros; at the next multiple of 256 bytes the scales, rows filled up to 16.  rows up to 2^26, K a
+ * with Kp = K filled up to 128 by zeros; at the next multiple of 256 bytes the scales, rows filled up to 16.  rows up to 2^26, K a
  * multiple of 16 up to 131056 (sums stay exact in 32 bits for all codes from -128 to 127).
  * ssg_i8_quantize: from rows of src, ld elements apart, rows on 16 bytes.  ssg_i8_pack: from codes [rows,K] and scales [rows]
  * that a program has already; ssg_i8_unpack the way back. */

@@ -22,9 +22,9 @@ def quantize(x: np.ndarray):
 
 
 def layout(codes: np.ndarray) -> np.ndarray:
-    """The bytes of codes [rows, K] in blocks of 16 rows by 64 codes, 16 bytes of a row at a time."""
+    """The bytes of codes [rows, K] in blocks of 16 rows by 64 codes, 16 bytes of a row at a time, K filled up to 128."""
     rows, K = codes.shape
-    full = np.zeros((-(-rows // 16) * 16, -(-K // 64) * 64), np.int8)
+    full = np.zeros((-(-rows // 16) * 16, -(-K // 128) * 128), np.int8)
     full[:rows, :K] = codes
     r, k = full.shape[0] // 16, full.shape[1] // 64
     return full.reshape(r, 16, k, 4, 16).transpose(0, 2, 3, 1, 4).reshape(-1).view(np.uint8)

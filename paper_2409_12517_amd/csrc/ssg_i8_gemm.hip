@@ -23,8 +23,7 @@ struct I8Params {
     int64_t M, N, ldc;
     int KB;                      // blocks of 64 along K
     int c_f32;
-    const int *offsets;
-    int E;
+    const int4 *tiles;           // with experts: {tiles in all, ..}, then {first row, end, expert, first tile} of each row tile
     int tiles_n;
 };
 
@@ -37,64 +36,26 @@ __device__ __forceinline__ v4i_t mfma_i8(const v4i_t &w, const v4i_t &x, const v
 // Which rows and columns a workgroup has.
 struct I8Tile { int expert, row, row_end, col; };        // rows [row, row_end) of the expert, at most; column tile
 
-// Tiles of `edge` rows, column tiles of one row tile after the other in groups of four row tiles of one expert, and
-// eight contiguous ranges of that order for the eight XCDs (see map_tile).  False: no such tile.
-__device__ __forceinline__ bool find_tile(const I8Params &p, int edge, int vblock, I8Tile &tile) {
-    const int lane = threadIdx.x & 63;
-    int total = 0;                                       // row tiles
-    if (p.offsets) {
-        for (int e0 = 0; e0 < p.E; e0 += 64) {
-            const int e = e0 + lane;
-            int n = 0;
-            if (e < p.E) n = (p.offsets[e + 1] - p.offsets[e] + edge - 1) / edge;
-#pragma unroll
-            for (int d = 32; d > 0; d /= 2) n += __shfl_xor(n, d, 64);
-            total += n;
-        }
-    } else {
-        total = (int)((p.M + edge - 1) / edge);
-    }
-    const int all = total * p.tiles_n;
-    if (vblock >= all) return false;
-    const int full = all & ~7;
-    const int t = vblock < full ? (vblock & 7) * (full >> 3) + (vblock >> 3) : vblock;
-    int first = 0, tiles = total, lo = 0, hi = (int)((p.M + 15) & ~(int64_t)15), expert = 0;
-    if (p.offsets) {
-        const int want = t / p.tiles_n;                  // row tile in the order of experts
-        int before = 0;
-        for (int e0 = 0; e0 < p.E; e0 += 64) {
-            const int e = e0 + lane;
-            int a = 0, b = 0;
-            if (e < p.E) { a = p.offsets[e]; b = p.offsets[e + 1]; }
-            const int n = (b - a + edge - 1) / edge;
-            int inc = n;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const int o = __shfl_up(inc, d, 64);
-                if (lane >= d) inc += o;
-            }
-            const uint64_t hit = __ballot(want >= before + inc - n && want < before + inc);
-            if (hit) {
-                const int at = __ffsll((unsigned long long)hit) - 1;
-                first = before + __shfl(inc - n, at, 64);
-                tiles = __shfl(n, at, 64);
-                lo = __shfl(a, at, 64);
-                hi = __shfl(b, at, 64);
-                expert = e0 + at;
-                break;
-            }
-            before += __shfl(inc, 63, 64);
-        }
-    }
-    const int local = t - first * p.tiles_n;
+__device__ __forceinline__ int row_tiles(const I8Params &p, int edge) {
+    return p.tiles ? __builtin_amdgcn_readfirstlane(p.tiles[0].x) : (int)((p.M + edge - 1) / edge);
+}
+// Tile number v of row_tiles * tiles_n: the column tiles of one row tile after the other in groups of four row tiles of one
+// expert, and eight contiguous ranges of that order for the eight XCDs (see map_tile).
+__device__ __forceinline__ I8Tile find_tile(const I8Params &p, int edge, int rows, int v) {
+    const int all = rows * p.tiles_n, full = all & ~7;
+    const int t = v < full ? (v & 7) * (full >> 3) + (v >> 3) : v;
+    int4 e = make_int4(0, (int)((p.M + 15) & ~(int64_t)15), 0, 0);
+    if (p.tiles) e = p.tiles[1 + t / p.tiles_n];
+    const int local = t - e.w * p.tiles_n, tiles = (e.y - e.x + edge - 1) / edge;
     constexpr int kGroup = 4;
     const int group = local / (kGroup * p.tiles_n), in_group = local - group * (kGroup * p.tiles_n);
     const int height = tiles - group * kGroup < kGroup ? tiles - group * kGroup : kGroup;
-    tile.expert = __builtin_amdgcn_readfirstlane(expert);
+    I8Tile tile;
+    tile.expert = __builtin_amdgcn_readfirstlane(e.z);
     tile.col = __builtin_amdgcn_readfirstlane(in_group / height);
-    tile.row = __builtin_amdgcn_readfirstlane(lo + (group * kGroup + in_group % height) * edge);
-    tile.row_end = __builtin_amdgcn_readfirstlane(hi);
-    return true;
+    tile.row = __builtin_amdgcn_readfirstlane(e.x + (group * kGroup + in_group % height) * edge);
+    tile.row_end = __builtin_amdgcn_readfirstlane(e.y);
+    return tile;
 }
 
 // Four neighbouring columns of a row.
@@ -110,164 +71,257 @@ __device__ __forceinline__ void scaled4(const v4i_t &acc, float sa, const float4
     v[3] = __fmul_rn(__fmul_rn((float)acc[3], sa), sb.w);
 }
 
+// dma16_s where `no` is 0 (wave-uniform).  The branch is inside the statement: the code around it stays one block.
+__device__ __forceinline__ void dma16_unless(int no, const uint8_t *base_uniform, uint32_t lane_off, uint32_t lds_addr) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_cmp_lg_u32 %3, 0\n\ts_cbranch_scc1 1f\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n1:"
+                 :: "s"(lds_addr), "v"(lane_off), "s"(base_uniform), "s"(no) : "memory", "m0", "scc");
+#else
+    (void)no; (void)base_uniform; (void)lane_off; (void)lds_addr;
+#endif
+}
+
 // ---- tiles through LDS -----------------------------------------------------------------------------------
 // 4 waves as 2 x 2, RB x RB blocks of 16 x 16 each (RB = 8: 256 x 256, one workgroup to a compute unit; RB = 4: 128 x 128, two).
-// K advances in steps of 64 through a ring of five stages.  The fragments of a step are read while the step before it is
-// multiplied, so when all waves have passed the barrier at the start of step k the stage of step k is free, and k + 5 is loaded into it.
-constexpr int kI8Stages = 5;
+// K advances in steps of 64 through a ring of four stages.  The fragments of a step are read while the step before it is
+// multiplied, so when all waves have passed the barrier at the start of step k the stage of step k is free, and k + 4 is loaded into it.
+// A workgroup has several tiles one after the other and the ring runs on from one to the next: while a tile's last steps are
+// multiplied and its results stored, the first stages of the next are on their way.  A tile with no more rows than half (an expert's
+// last one) loads and multiplies half of them: 4 by 8 blocks to a wave.
+constexpr int kI8Stages = 4;
 template <int WB> constexpr int i8_stage_bytes() { return 8 * WB * 1024; }
 template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void i8_tile_kernel(I8Params p) {
-    constexpr int RB = 2 * WB, kEdge = 64 * WB, kCols = DUAL ? kEdge / 2 : kEdge;
-    constexpr int kStage = i8_stage_bytes<WB>();
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[kI8Stages * kStage];
-    I8Tile tile;
-    if (!find_tile(p, kEdge, blockIdx.x, tile)) return;
+    constexpr int RB = 2 * WB, kEdge = 64 * WB, kCols = DUAL ? kEdge / 2 : kEdge, kOut = DUAL ? RB / 2 : RB;
+    constexpr int kStage = i8_stage_bytes<WB>(), kRing = kI8Stages * kStage;
+    constexpr int kPatch = 16 * (64 * WB + 16);          // of a wave: 16 rows of 64 WB bytes
+    constexpr int kScales = 64 * WB * (DUAL ? 3 : 2) * 4;        // of a wave: its workgroup's rows' and columns'
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kRing + 4 * kPatch + 4 * kScales];
+    const int rows = row_tiles(p, kEdge), all = rows * p.tiles_n;
+    int v = blockIdx.x;
+    if (v >= all) return;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w >> 1, wn = w & 1;
-    int l = tid & 63;
+    const int lane_id = tid & 63;
     const int KB = p.KB, col_blocks = (int)(p.N / 16);
-    const int first_rb = tile.row / 16, last_rb = tile.row_end / 16 - 1;
-    const int first_cb = tile.col * (kCols / 16);
-    // the blocks this wave loads; beyond the matrix: its last one again (not stored)
-    uint32_t a_lane[WB], b_lane[WB];
-#pragma unroll
-    for (int j = 0; j < WB; ++j) {
-        const int rb = first_rb + w * WB + j;
-        a_lane[j] = (uint32_t)((rb < last_rb ? rb : last_rb) - first_rb) * (uint32_t)KB * 1024u + l * 16;
-        const int cb = first_cb + (DUAL ? (w & 1) * WB + j : w * WB + j);
-        b_lane[j] = (uint32_t)((cb < col_blocks ? cb : col_blocks - 1) - first_cb) * (uint32_t)KB * 1024u + l * 16;
-    }
-    const uint8_t *a_src = p.A + (int64_t)first_rb * KB * 1024;
-    const uint8_t *b_src = (DUAL && w >= 2 ? p.B2 : p.B) + ((int64_t)tile.expert * col_blocks + first_cb) * KB * 1024;
     const uint32_t smem_base = (uint32_t)(uintptr_t)(lds_void_ptr)smem;
-    const uint32_t a_dst = smem_base + w * WB * 1024u, b_dst = a_dst + 4 * WB * 1024u;
+    const uint32_t b_dst = smem_base + (4 * WB + w * WB) * 1024u;
+    // The blocks of a tile that this wave loads: where its first one begins and how far the others are, wave-uniform; beyond the
+    // matrix its last one again (not stored).
+    struct Source {
+        const uint8_t *a, *b;
+        uint32_t a_off[WB], b_off[WB], a_dst;
+        int half;
+    };
+    auto source = [&](const I8Tile &tile) {
+        Source s;
+        const int first_rb = tile.row / 16, last_rb = tile.row_end / 16 - 1, first_cb = tile.col * (kCols / 16);
+        s.half = (int)((uint32_t)(last_rb - first_rb - RB) >> 31);       // 1: no more than RB row blocks (a truth value would leave the scalar registers)
+        const int mine = (w * WB) >> s.half;             // the first row block of this wave's
+        s.a_dst = smem_base + mine * 1024u;
+        s.a = p.A + (int64_t)first_rb * KB * 1024;
+        s.b = (DUAL && w >= 2 ? p.B2 : p.B) + ((int64_t)tile.expert * col_blocks + first_cb) * KB * 1024;
+#pragma unroll
+        for (int j = 0; j < WB; ++j) {
+            const int rb = first_rb + mine + j, cb = first_cb + (DUAL ? (w & 1) * WB + j : w * WB + j);
+            s.a_off[j] = (uint32_t)((rb < last_rb ? rb : last_rb) - first_rb) * (uint32_t)KB * 1024u;
+            s.b_off[j] = (uint32_t)((cb < col_blocks ? cb : col_blocks - 1) - first_cb) * (uint32_t)KB * 1024u;
+        }
+        return s;
+    };
+    I8Tile tile = find_tile(p, kEdge, rows, v), next_tile = tile;
+    Source src = source(tile), next_src = src;
+    auto scalar = [](const Source &s) {
+        auto u32 = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+        auto ptr = [&](const uint8_t *x) {
+            const uint64_t u = (uint64_t)(uintptr_t)x;
+            return reinterpret_cast<const uint8_t *>((uintptr_t)((uint64_t)u32((uint32_t)(u >> 32)) << 32 | u32((uint32_t)u)));
+        };
+        Source r;
+        r.a = ptr(s.a);
+        r.b = ptr(s.b);
+#pragma unroll
+        for (int j = 0; j < WB; ++j) {
+            r.a_off[j] = u32(s.a_off[j]);
+            r.b_off[j] = u32(s.b_off[j]);
+        }
+        r.a_dst = u32(s.a_dst);
+        r.half = (int)u32((uint32_t)s.half);
+        return r;
+    };
+    const uint32_t lane = lane_id * 16;
+    // (opaque: what is computed from it for one tile is not kept for all, in registers that the main loop needs)
+    auto lane_now = [&]() {
+        int l = lane_id;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
     auto issue_one = [&](int j, uint32_t slot) {
-        if (j < WB) dma16_s(a_src, a_lane[j], a_dst + slot + j * 1024u);
-        else dma16_s(b_src, b_lane[j - WB], b_dst + slot + (j - WB) * 1024u);
+        if (j < WB / 2) dma16_s(src.a + src.a_off[j], lane, src.a_dst + slot + j * 1024u);
+        else if (j < WB) dma16_unless(src.half, src.a + src.a_off[j], lane, src.a_dst + slot + j * 1024u);
+        else dma16_s(src.b + src.b_off[j - WB], lane, b_dst + slot + (j - WB) * 1024u);
     };
-    // The sources stop at the last block of K: the loop issues loads in every step, the last ones into stages that nothing reads,
-    // so that it is one piece of code with one count of loads to wait for.
-    int loaded = 0;
-    auto advance = [&]() {
-        const int by = ++loaded < KB ? 1024 : 0;
-        a_src += by;
-        b_src += by;
-    };
-    constexpr int kLoads = 2 * WB;
+    constexpr int kLoads = 2 * WB, kFewest = kLoads - WB / 2;            // of a stage; where the tile is half of one
     static_assert(kLoads == RB, "a load to every column of blocks");
-    // Steps come in pairs; where their number is odd the first of a pair multiplies zeros, in the place of a step -1.
-    const int odd_steps = KB & 1;
+    // After the last stage of this tile come those of the next one (of the last tile's: the same again, which nothing reads).
+    // Their number is even, so that it is asked for after every second one.
+    int loaded = 0;
+    auto two_loaded = [&]() {
+        if ((loaded += 2) == KB) {
+            src = next_src;
+            loaded = 0;
+        }
+    };
+    // This tile's scales into the wave's own patch: 16 bytes to a lane, 64 WB rows and columns
+    uint8_t *patch = smem + kRing + w * kPatch;
+    const uint32_t scales = (uint32_t)(kRing + 4 * kPatch + w * kScales);
+    auto fetch_scales = [&]() {
+        const int l = lane_now();
+        if (l >= 16 * WB) return;
+        const int first_rb = tile.row / 16, last_rb = tile.row_end / 16 - 1, first_cb = tile.col * (kCols / 16);
+        const int rb = first_rb + l / 4, cb = first_cb + l / 4;
+        const float *sa = p.sa + (int64_t)(rb < last_rb ? rb : last_rb) * 16 + l % 4 * 4;
+        const int64_t col = (int64_t)tile.expert * p.N + (cb < col_blocks ? cb : col_blocks - 1) * 16 + l % 4 * 4;
+        dma16(reinterpret_cast<const uint8_t *>(sa), smem_base + scales);
+        dma16(reinterpret_cast<const uint8_t *>(p.sb + col), smem_base + scales + 256 * WB);
+        if (DUAL) dma16(reinterpret_cast<const uint8_t *>(p.sb2 + col), smem_base + scales + 512 * WB);
+    };
+    // the next tile, known before the loads come to it
+    auto look_ahead = [&]() {
+        const int n = v + (int)gridDim.x;
+        if (n < all) {
+            next_tile = find_tile(p, kEdge, rows, n);
+            next_src = source(next_tile);
+        } else {
+            next_src = source(tile);
+        }
+    };
+    look_ahead();
 #pragma unroll
     for (int s = 0; s < kI8Stages; ++s) {
-        if (s == kI8Stages - 1 && odd_steps) break;      // (step -1 loads it)
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) issue_one(j, s * kStage);
-        advance();
+        src.a += 1024;
+        src.b += 1024;
+        if (s % 2 == 1) two_loaded();
     }
-    v4i_t acc[RB][RB];
-#pragma unroll
-    for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int c = 0; c < RB; ++c) acc[r][c] = v4i_t{0, 0, 0, 0};
-    v4i_t fa[2][RB], fb[2][RB];
-    const uint8_t *a_frag = smem + wm * RB * 1024 + l * 16, *b_frag = smem + 4 * WB * 1024 + l * 16;
     // block c of this wave's columns; with two matrices the first half of them are W1's, the others W2's same columns
     auto col_block = [&](int c) { return DUAL ? (c / (RB / 2)) * (2 * WB) + wn * (RB / 2) + c % (RB / 2) : wn * RB + c; };
-    auto read_one = [&](int set, int i, uint32_t slot) {
-        if (i % 2 == 0) fa[set][i / 2] = *reinterpret_cast<const v4i_t *>(a_frag + slot + i / 2 * 1024);
-        else fb[set][i / 2] = *reinterpret_cast<const v4i_t *>(b_frag + slot + col_block(i / 2) * 1024);
-    };
-    wait_dma<(kI8Stages - 2) * kLoads>();                // (stage 0, and with an even number of steps stage 1)
+    uint32_t slot = 0;                                   // of this step's stage
+    wait_dma<(kI8Stages - 1) * kFewest>();               // stage 0
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < 2 * RB; ++i) read_one(0, i, 0);
-    if (odd_steps) {
-#pragma unroll
-        for (int i = 0; i < RB; ++i) fa[0][i] = v4i_t{0, 0, 0, 0};
-    }
-    uint32_t slot = odd_steps ? (kI8Stages - 1) * kStage : 0;        // of this step's stage
-    auto step = [&](auto parity) {
-        constexpr int set = decltype(parity)::value;
-        const uint32_t next = slot == (kI8Stages - 1) * kStage ? 0 : slot + kStage;
-        wait_dma<(kI8Stages - 2) * kLoads>();            // the next step's stage has landed
-        __builtin_amdgcn_s_waitcnt(0xC07F);              // this step's fragments are here
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        constexpr int kEvery = RB / 2;                   // MFMAs to a fragment read
-#pragma unroll
-        for (int t = 0; t < RB * RB; ++t) {
-            const int c = t / RB, r = c & 1 ? RB - 1 - t % RB : t % RB;
-            acc[r][c] = mfma_i8(fb[set][c], fa[set][r], acc[r][c]);
-            if (t % kEvery == 0) read_one(set ^ 1, t / kEvery, next);        // (after the last step: never used)
-            if (t % RB == RB / 4) issue_one(t / RB, slot);
+    // One tile, RA row blocks to a wave.
+    auto run_tile = [&](auto row_blocks) {
+        constexpr int RA = decltype(row_blocks)::value;
+        v4i_t acc[RA][RB];
+        v4i_t fa[2][RA], fb[2][RB];
+        const uint8_t *a_frag = smem + wm * RA * 1024 + lane, *b_frag = smem + 4 * WB * 1024 + lane;
+        // fragment i in the order of use: the first column's and the rows', then the other columns'
+        auto read_one = [&](int set, int i, uint32_t slot) {
+            if (i >= 1 && i <= RA) fa[set][i - 1] = *reinterpret_cast<const v4i_t *>(a_frag + slot + (i - 1) * 1024);
+            else fb[set][i == 0 ? 0 : i - RA] = *reinterpret_cast<const v4i_t *>(b_frag + slot + col_block(i == 0 ? 0 : i - RA) * 1024);
+        };
+        auto step = [&](auto parity) {
+            constexpr int set = decltype(parity)::value;
+            const uint32_t next = slot == (kI8Stages - 1) * kStage ? 0 : slot + kStage;
+            wait_dma<(kI8Stages - 2) * kFewest>();           // the next step's stage has landed
+            __builtin_amdgcn_s_waitcnt(0xC07F);              // this step's fragments are here
+            __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
-        }
-        advance();
-        slot = next;
-    };
+            constexpr int kEvery = RA * RB / (RA + RB);      // MFMAs to a fragment read
+#pragma unroll
+            for (int t = 0; t < RA * RB; ++t) {
+                const int c = t / RA, r = c & 1 ? RA - 1 - t % RA : t % RA;
+                acc[r][c] = mfma_i8(fb[set][c], fa[set][r], acc[r][c]);
+                if (t % kEvery == 0 && t / kEvery < RA + RB) read_one(set ^ 1, t / kEvery, next);
+                if (t % RA == RA / 4) issue_one(t / RA, slot);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            src.a += 1024;
+            src.b += 1024;
+            slot = next;
+        };
+        // 16 rows at a time go through the patch, so that rows leave in pieces of 16 bytes side by side (straight from the accumulators,
+        // 8 bytes of 16 rows in a store, the epilogue of the large tile took 9 us more)
+        auto store = [&](auto f32) {
+            const int l = lane_now();
+            constexpr bool F32 = decltype(f32)::value;
+            constexpr int kSize = F32 ? 4 : 2, kRowBytes = kOut * 16 * kSize < 64 * WB ? kOut * 16 * kSize : 64 * WB;
+            constexpr int kPitch = kRowBytes + 16, kPart = kRowBytes / (16 * kSize);             // column blocks at a time
+            constexpr int kLanes = kRowBytes / 16, kAtOnce = 64 / kLanes;        // lanes to a row, rows to a store
+            static_assert(16 * kPitch <= kPatch && kOut % kPart == 0, "a part of the columns fits the patch");
+            const int first_rb = tile.row / 16, last_rb = tile.row_end / 16 - 1;
+            const float *sc = reinterpret_cast<const float *>(smem + scales);
+#pragma unroll
+            for (int r = 0; r < RA; ++r) {
+                const int rb = first_rb + wm * RA + r;
+                if (rb > last_rb) break;
+                const float sa = sc[(wm * RA + r) * 16 + (l & 15)];
+#pragma unroll
+                for (int c0 = 0; c0 < kOut; c0 += kPart) {
+                    const int64_t col0 = (int64_t)tile.col * kCols + (wn * kOut + c0) * 16 + (l % kLanes) * (16 / kSize);
+#pragma unroll
+                    for (int c = c0; c < c0 + kPart; ++c) {
+                        const int at_col = (wn * kOut + c) * 16 + (l >> 4) * 4;
+                        float x[4];
+                        scaled4(acc[r][c], sa, *reinterpret_cast<const float4 *>(sc + 64 * WB + at_col), x);
+                        if (DUAL) {
+                            float g[4];
+                            scaled4(acc[r][c + RB / 2], sa, *reinterpret_cast<const float4 *>(sc + 128 * WB + at_col), g);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[i] = swiglu_f32(x[i], g[i]);
+                        }
+                        uint8_t *at = patch + (l & 15) * kPitch + ((c - c0) * 16 + (l >> 4) * 4) * kSize;
+                        if (F32) *reinterpret_cast<float4 *>(at) = make_float4(x[0], x[1], x[2], x[3]);
+                        else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16 / kAtOnce; ++i) {
+                        const int at = i * kAtOnce + l / kLanes;
+                        const uint4 x = *reinterpret_cast<const uint4 *>(patch + at * kPitch + l % kLanes * 16);
+                        const int64_t row = (int64_t)rb * 16 + at;
+                        if (row < p.M && col0 < p.N) *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.C) + (row * p.ldc + col0) * kSize) = x;
+                    }
+                }
+            }
+        };
+#pragma unroll
+        for (int r = 0; r < RA; ++r)
+#pragma unroll
+            for (int c = 0; c < RB; ++c) {
+                acc[r][c] = v4i_t{0, 0, 0, 0};
+                // (else the compiler knows the zeros, has them in both halves of the register file and moves half of the accumulators
+                // about in every step: 500 moves to 128 MFMAs)
+                if (WB == 4) asm volatile("" : "+a"(acc[r][c]));
+            }
+        // (read again, though the last step of the tile before has, so that no fragments are kept across the epilogue)
+#pragma unroll
+        for (int i = 0; i < RA + RB; ++i) read_one(0, i, slot);
 #pragma nounroll
-    for (int k = -odd_steps; k < KB; k += 2) {
-        step(std::integral_constant<int, 0>{});
-        step(std::integral_constant<int, 1>{});
+        for (int k = 0; k < KB; k += 2) {
+            step(std::integral_constant<int, 0>{});
+            step(std::integral_constant<int, 1>{});
+            two_loaded();
+        }
+        wait_dma<2 * kFewest>();                             // the scales are older than the loads of the last two steps
+        if (!DUAL && p.c_f32) store(std::true_type{});
+        else store(std::false_type{});
+    };
+    for (;;) {
+        // (what is the same in all lanes, said again where the two forms of a tile meet: the compiler loses sight of it)
+        src = scalar(src);
+        next_src = scalar(next_src);
+        slot = (uint32_t)__builtin_amdgcn_readfirstlane((int)slot);
+        loaded = __builtin_amdgcn_readfirstlane(loaded);
+        v = __builtin_amdgcn_readfirstlane(v);
+        fetch_scales();
+        if (__builtin_amdgcn_readfirstlane(tile.row_end - tile.row) <= kEdge / 2) run_tile(std::integral_constant<int, RB / 2>{});
+        else run_tile(std::integral_constant<int, RB>{});
+        v += (int)gridDim.x;
+        if (v >= all) break;
+        tile = next_tile;
+        look_ahead();
     }
     wait_dma<0>();                                       // (the workgroup's LDS is another's after it)
-    __syncthreads();                                     // the ring is free
-    asm volatile("" : "+v"(l));
-    // 16 rows at a time go through a patch of LDS of the wave's own, so that rows leave in pieces of 16 bytes side by side (straight from
-    // the accumulators, 8 bytes of 16 rows in a store, the epilogue of the large tile took 9 us more).  All scales are read
-    // before the first store: behind one the compiler would read them again.
-    constexpr int kOut = DUAL ? RB / 2 : RB;
-    const float *sb = p.sb + (int64_t)tile.expert * p.N, *sb2 = DUAL ? p.sb2 + (int64_t)tile.expert * p.N : nullptr;
-    float sa[RB];
-    float4 s1[kOut], s2[kOut];
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        const int rb = first_rb + wm * RB + r;
-        sa[r] = p.sa[(int64_t)(rb < last_rb ? rb : last_rb) * 16 + (l & 15)];
-    }
-#pragma unroll
-    for (int c = 0; c < kOut; ++c) {
-        const int cb = first_cb + wn * kOut + c;
-        const int64_t col = (int64_t)(cb < col_blocks ? cb : col_blocks - 1) * 16 + (l >> 4) * 4;
-        s1[c] = *reinterpret_cast<const float4 *>(sb + col);
-        if (DUAL) s2[c] = *reinterpret_cast<const float4 *>(sb2 + col);
-    }
-    auto store = [&](auto f32) {
-        constexpr bool F32 = decltype(f32)::value;
-        constexpr int kSize = F32 ? 4 : 2, kRowBytes = kOut * 16 * kSize, kPitch = kRowBytes + 16;
-        constexpr int kLanes = kRowBytes / 16, kAtOnce = 64 / kLanes;        // lanes to a row, rows to a store
-        static_assert(4 * 16 * kPitch <= kI8Stages * kStage, "the patches fit the ring");
-        uint8_t *patch = smem + w * 16 * kPitch;
-        const int64_t col0 = ((int64_t)first_cb + wn * kOut) * 16 + (l % kLanes) * (16 / kSize);
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const int rb = first_rb + wm * RB + r;
-            if (rb > last_rb) break;
-#pragma unroll
-            for (int c = 0; c < kOut; ++c) {
-                float v[4];
-                scaled4(acc[r][c], sa[r], s1[c], v);
-                if (DUAL) {
-                    float g[4];
-                    scaled4(acc[r][c + RB / 2], sa[r], s2[c], g);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = swiglu_f32(v[i], g[i]);
-                }
-                uint8_t *at = patch + (l & 15) * kPitch + (c * 16 + (l >> 4) * 4) * kSize;
-                if (F32) *reinterpret_cast<float4 *>(at) = make_float4(v[0], v[1], v[2], v[3]);
-                else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-            }
-#pragma unroll
-            for (int i = 0; i < 16 / kAtOnce; ++i) {
-                const int at = i * kAtOnce + l / kLanes;
-                const uint4 v = *reinterpret_cast<const uint4 *>(patch + at * kPitch + l % kLanes * 16);
-                const int64_t row = (int64_t)rb * 16 + at;
-                if (row < p.M && col0 < p.N) *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.C) + (row * p.ldc + col0) * kSize) = v;
-            }
-        }
-    };
-    if (!DUAL && p.c_f32) store(std::true_type{});
-    else store(std::false_type{});
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------
@@ -276,8 +330,9 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
 template <int RB, int CB, int WAVES, bool DUAL> __global__ __launch_bounds__(64 * WAVES) void i8_few_kernel(I8Params p) {
     constexpr int NB = DUAL ? 2 * CB : CB;
     __shared__ v4i_t part[WAVES][RB * NB][64];
-    I8Tile tile;
-    if (!find_tile(p, 16 * RB, blockIdx.x, tile)) return;
+    const int rows = row_tiles(p, 16 * RB);
+    if ((int)blockIdx.x >= rows * p.tiles_n) return;
+    const I8Tile tile = find_tile(p, 16 * RB, rows, blockIdx.x);
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int KB = p.KB, col_blocks = (int)(p.N / 16);
     const int first_rb = tile.row / 16, last_rb = tile.row_end / 16 - 1, first_cb = tile.col * CB;
@@ -350,13 +405,6 @@ template <int RB, int CB, int WAVES, bool DUAL> __global__ __launch_bounds__(64 
     }
 }
 
-// Row tiles of `edge` rows that the experts can have between them.
-int64_t row_tiles_bound(const I8GemmArgs &a, int edge) {
-    if (!a.offsets) return (a.M + edge - 1) / edge;
-    const int64_t active = std::min<int64_t>(a.E, a.rows_expected);
-    return (a.M + active * (edge - 16)) / edge;
-}
-
 // Which kernel, from the extents alone.
 // One matrix.  Up to 16 and up to 32 rows the blocks that fit them.  Then 64 x 32 where 128 x 128 tiles would leave three quarters
 // of the chip idle (4096 x 11008 by 128 rows 20 us and 49 in 32 tiles; 1040 x 2736 by 333 8 and 12; with 96 tiles, 4096 x 4096 by 333,
@@ -369,9 +417,9 @@ int64_t row_tiles_bound(const I8GemmArgs &a, int edge) {
 // 241, at 2048 161 and 141.  Over 98 products 3 % above the better one on average, at most 14 %.)
 enum I8Form { FEW_16, FEW_16_EXPERTS, FEW_32, FEW_64, TILE_128, TILE_256 };
 I8Form choose_form(const I8GemmArgs &a, bool dual) {
-    const double KB = (double)((a.K + 63) / 64), small_step = .52 * KB + 4, small_alone = .28 * KB + 4, large_step = .70 * KB + 9;
+    const double KB = (double)(i8_width(a.K) / 64), small_step = .52 * KB + 4, small_alone = .28 * KB + 4, large_step = .70 * KB + 9;
     const int64_t cols = dual ? 2 * a.N : a.N, cols128 = (cols + 127) / 128, cols256 = (cols + 255) / 256;
-    if (!a.offsets) {
+    if (a.E == 0) {
         const int64_t tiles128 = (a.M + 127) / 128 * cols128, tiles256 = (a.M + 255) / 256 * cols256;
         if (a.M <= 16) return FEW_16;
         if (a.M <= 32) return FEW_32;
@@ -382,33 +430,47 @@ I8Form choose_form(const I8GemmArgs &a, bool dual) {
     }
     const double active = (double)std::min<int64_t>(a.E, a.rows_expected), rows = (double)a.rows_expected / active;
     if (rows <= 12) return FEW_16_EXPERTS;
-    const double small = active * std::max(1.0, rows / 128 + .5) * cols128 / 512 * small_step;
-    const double large = std::ceil(active * std::max(1.0, rows / 256 + .5) * cols256 / 256) * large_step;
+    const double small = active * std::max(.6, rows / 128 + .3) * cols128 / 512 * small_step;
+    const double large = std::ceil(active * std::max(.6, rows / 256 + .3) * cols256 / 256) * large_step;
     return large < small ? TILE_256 : TILE_128;
 }
 
+int form_edge(I8Form f) { return f == TILE_256 ? 256 : f == TILE_128 ? 128 : f == FEW_64 ? 64 : f == FEW_32 ? 32 : 16; }
+
 template <bool DUAL> void launch_form(const I8GemmArgs &a, hipStream_t st) {
+    const I8Form form = choose_form(a, DUAL);
+    const I8RowTiles rows = i8_row_tiles(a);
     I8Params p;
     p.A = a.A; p.B = a.B; p.B2 = a.B2; p.sa = a.sa; p.sb = a.sb; p.sb2 = a.sb2; p.C = a.C;
-    p.M = a.M; p.N = a.N; p.ldc = a.ldc; p.KB = (int)((a.K + 63) / 64); p.c_f32 = a.c_f32; p.offsets = a.offsets; p.E = a.E;
-    auto go = [&](auto kernel, int edge, int cols, int threads) {
+    p.M = a.M; p.N = a.N; p.ldc = a.ldc; p.KB = (int)(i8_width(a.K) / 64); p.c_f32 = a.c_f32; p.tiles = reinterpret_cast<const int4 *>(a.tiles);
+    auto go = [&](auto kernel, int cols, int threads, int64_t most) {
         p.tiles_n = (int)((a.N + cols - 1) / cols);
-        const int64_t blocks = row_tiles_bound(a, edge) * p.tiles_n;
+        const int64_t blocks = std::min(rows.most * p.tiles_n, most);
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, st, p);
     };
+    // the tiles' workgroups stay, one or two to a compute unit; a tile of no more steps than the ring has stages is a workgroup's only one
+    // (its loads would run two tiles ahead)
+    constexpr int64_t kAll = (int64_t)1 << 31;
+    const int64_t units = p.KB > kI8Stages ? 256 : kAll;
     profile_before(DUAL ? kTagI8Swiglu : kTagI8Gemm, st);
-    switch (choose_form(a, DUAL)) {
-        case FEW_16: go(i8_few_kernel<1, 1, 8, DUAL>, 16, 16, 512); break;
-        case FEW_16_EXPERTS: go(i8_few_kernel<1, 1, 4, DUAL>, 16, 16, 256); break;
-        case FEW_32: go(i8_few_kernel<2, 1, 4, DUAL>, 32, 16, 256); break;
-        case FEW_64: go(i8_few_kernel<4, 2, 8, DUAL>, 64, 32, 512); break;
-        case TILE_128: go(i8_tile_kernel<2, DUAL>, 128, DUAL ? 64 : 128, 256); break;
-        case TILE_256: go(i8_tile_kernel<4, DUAL>, 256, DUAL ? 128 : 256, 256); break;
+    switch (form) {
+        case FEW_16: go(i8_few_kernel<1, 1, 8, DUAL>, 16, 512, kAll); break;
+        case FEW_16_EXPERTS: go(i8_few_kernel<1, 1, 4, DUAL>, 16, 256, kAll); break;
+        case FEW_32: go(i8_few_kernel<2, 1, 4, DUAL>, 16, 256, kAll); break;
+        case FEW_64: go(i8_few_kernel<4, 2, 8, DUAL>, 32, 512, kAll); break;
+        case TILE_128: go(i8_tile_kernel<2, DUAL>, DUAL ? 64 : 128, 256, 2 * units); break;
+        case TILE_256: go(i8_tile_kernel<4, DUAL>, DUAL ? 128 : 256, 256, units); break;
     }
     profile_after(st);
 }
 
 }  // namespace
+
+I8RowTiles i8_row_tiles(const I8GemmArgs &a) {
+    const int edge = form_edge(choose_form(a, a.B2 != nullptr));
+    if (a.E == 0) return {edge, (a.M + edge - 1) / edge};
+    return {edge, (a.M + std::min<int64_t>(a.E, a.rows_expected) * (edge - 16)) / edge};
+}
 
 void launch_i8_gemm(const I8GemmArgs &a, hipStream_t st) {
     if (a.M == 0) return;

@@ -17,18 +17,44 @@ namespace {
 // that a wave reads 8 rows x 128 elements and writes pieces of 128 bytes.  The first HELD runs of a thread stay in registers between the
 // maximum and the codes; what a row has beyond them is read again, out of the L2.
 constexpr int kRows = 8;
+// The list of row tiles, by one wave.
+__device__ __forceinline__ void list_tiles(const int *offsets, int E, int *list, int edge) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+        const int e = e0 + lane;
+        int lo = 0, hi = 0;
+        if (e < E) { lo = offsets[e]; hi = offsets[e + 1]; }
+        const int n = (hi - lo + edge - 1) / edge;
+        int inc = n;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(inc, d, 64);
+            if (lane >= d) inc += o;
+        }
+        const int first = before + inc - n;
+        for (int i = 0; i < n; ++i) *reinterpret_cast<int4 *>(list + 4 + 4 * (first + i)) = make_int4(lo, hi, e, first);
+        before += __shfl(inc, 63, 64);
+    }
+    if (lane == 0) *reinterpret_cast<int4 *>(list) = make_int4(before, 0, 0, 0);
+}
+
 template <bool BF16, int THREADS, int HELD> __global__ __launch_bounds__(THREADS) void i8_rows_kernel(I8RowsArgs a) {
     constexpr int kCols = THREADS / kRows, kWaves = THREADS / 64;
     __shared__ uint32_t maxima[kWaves][kRows];
     const int tid = threadIdx.x, r = tid % kRows, c0 = tid / kRows;
     const int64_t row = (int64_t)blockIdx.x * kRows + r;
+    if (a.E > 0 && blockIdx.x == gridDim.x - 1) {       // (the block behind those of the rows)
+        if (tid < 128 && a.tiles[tid >> 6].edge) list_tiles(a.offsets, a.E, a.tiles[tid >> 6].list, a.tiles[tid >> 6].edge);
+        return;
+    }
     if (a.live_rows && (int64_t)blockIdx.x * kRows >= *a.live_rows) return;
     int64_t from = row < a.rows ? row : -1;
     if (a.source && from >= 0) {
         const int s = a.source[row];
         from = s >= 0 ? s / a.k : -1;
     }
-    const int runs = (int)(a.K / 16), padded = (int)(i8_up(a.K, 64) / 16);
+    const int runs = (int)(a.K / 16), padded = (int)(i8_width(a.K) / 16);
     const uint8_t *src = static_cast<const uint8_t *>(a.src) + (from >= 0 ? from : 0) * a.ld * (BF16 ? 2 : 4);
     I8Run<BF16> held[HELD];
     uint32_t top = 0;
@@ -72,8 +98,8 @@ template <bool BF16, int THREADS, int HELD> __global__ __launch_bounds__(THREADS
 }
 
 template <bool BF16> void launch_rows(const I8RowsArgs &a, hipStream_t st) {
-    const unsigned blocks = (unsigned)(i8_up(a.rows, 16) / kRows);
-    const int runs = (int)(i8_up(a.K, 64) / 16);
+    const unsigned blocks = (unsigned)(i8_up(a.rows, 16) / kRows) + (a.E > 0);
+    const int runs = (int)(i8_width(a.K) / 16);
     // the smallest block whose registers hold the rows: 88 registers of values are 11 runs of bf16, 80 5 of fp32
     auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, st, a); };
     constexpr int kFew = BF16 ? 4 : 2, kMost = BF16 ? 11 : 5;
@@ -86,7 +112,7 @@ template <bool BF16> void launch_rows(const I8RowsArgs &a, hipStream_t st) {
 // Row-major codes and scales into the layout and back, 16 bytes to a thread.
 __global__ void i8_pack_kernel(const int8_t *codes, const float *scales, int64_t rows, int64_t K, uint8_t *out, float *out_scales) {
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    const int64_t padded = i8_up(K, 64) / 16, up = i8_up(rows, 16);
+    const int64_t padded = i8_width(K) / 16, up = i8_up(rows, 16);
     if (i < up) out_scales[i] = i < rows ? scales[i] : 0.0f;
     if (i >= up * padded) return;
     const int64_t r = i / (16 * padded) * 16 + (i & 15), c = i % (16 * padded) / 16;
@@ -96,7 +122,7 @@ __global__ void i8_pack_kernel(const int8_t *codes, const float *scales, int64_t
 }
 __global__ void i8_unpack_kernel(const uint8_t *in, const float *in_scales, int64_t rows, int64_t K, int8_t *codes, float *scales) {
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    const int64_t padded = i8_up(K, 64) / 16, up = i8_up(rows, 16);
+    const int64_t padded = i8_width(K) / 16, up = i8_up(rows, 16);
     if (i < rows) scales[i] = in_scales[i];
     if (i >= up * padded) return;
     const int64_t r = i / (16 * padded) * 16 + (i & 15), c = i % (16 * padded) / 16;

@@ -48,7 +48,7 @@ template <bool BF16, bool DUAL, int WAVES> __global__ __launch_bounds__(64 * WAV
     __shared__ v4i_t part[WAVES][NB][64];
     __shared__ uint32_t maxima[WAVES][kRows];
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col_blocks = (int)(a.N / 16), KB = (int)((a.K + 63) / 64), Kp = KB * 64;
+    const int col_blocks = (int)(a.N / 16), KB = (int)(i8_width(a.K) / 64), Kp = KB * 64;
     const int pair = a.ids ? blockIdx.x / col_blocks : 0, cb = blockIdx.x % col_blocks;
     const int expert = a.ids ? __builtin_amdgcn_readfirstlane(a.ids[pair]) : 0;
     if (expert < 0) return;
@@ -149,7 +149,7 @@ template <bool F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_ker
     __shared__ v4i_t part[kMixWaves][4];
     __shared__ float result[kMaxChosen][16];
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col_blocks = (int)(a.N / 16), KB = (int)((a.K + 63) / 64);
+    const int col_blocks = (int)(a.N / 16), KB = (int)(i8_width(a.K) / 64);
     const int t = blockIdx.x / col_blocks, cb = blockIdx.x % col_blocks;
     const int split = a.split, share = (KB + split - 1) / split, at_once = kMixWaves / split;
     const int runs = (int)(a.K / 16);
@@ -219,7 +219,7 @@ template <bool F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_ker
 void launch_i8_token(const I8TokenArgs &a, hipStream_t st) {
     const bool dual = a.B2 != nullptr;
     const unsigned blocks = (unsigned)((a.ids ? a.pairs : 1) * (a.N / 16));
-    const unsigned lds = (unsigned)(a.rows * i8_up(a.K, 64));
+    const unsigned lds = (unsigned)(a.rows * i8_width(a.K));
     profile_before(dual ? kTagI8Swiglu : kTagI8Gemm, st);
     // one matrix has few workgroups, which take more waves each
     if (dual) hipLaunchKernelGGL((i8_token_kernel<true, true, 4>), dim3(blocks), dim3(256), lds, st, a);
@@ -234,10 +234,10 @@ static int mix_split(int k) {
     while (2 * split * k <= kMixWaves) split *= 2;
     return split;
 }
-static int64_t mix_lds(int64_t K, int k) { const int64_t KB = (K + 63) / 64, s = mix_split(k); return kMixWaves * ((KB + s - 1) / s) * 64; }
+static int64_t mix_lds(int64_t K, int k) { const int64_t KB = i8_width(K) / 64, s = mix_split(k); return kMixWaves * ((KB + s - 1) / s) * 64; }
 
-bool i8_token_ok(int64_t T, int64_t K) { return T <= kTokenRows && T * i8_up(K, 64) <= kTokenLds; }
-bool i8_mix_ok(int64_t T, int64_t d, int64_t f, int k) { return T <= kTokenRows && i8_up(d, 64) <= kTokenLds && mix_lds(f, k) <= kMixLds; }
+bool i8_token_ok(int64_t T, int64_t K) { return T <= kTokenRows && T * i8_width(K) <= kTokenLds; }
+bool i8_mix_ok(int64_t T, int64_t d, int64_t f, int k) { return T <= kTokenRows && i8_width(d) <= kTokenLds && mix_lds(f, k) <= kMixLds; }
 
 void launch_i8_mix(I8MixArgs a, hipStream_t st) {
     a.split = mix_split(a.k);

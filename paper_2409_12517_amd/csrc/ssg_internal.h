@@ -302,12 +302,13 @@ void launch_route_bwd(const RouteBwdArgs &a, hipStream_t st);
 void launch_combine(const CombineArgs &a, hipStream_t st);
 
 // ---- products in 8-bit integers (ssg_i8_rows.hip, ssg_i8_gemm.hip) --------------------
-// Codes lie in blocks of 16 rows by 64 codes of K, 1 KB each, a row of blocks after the other, K filled up with zeros to 64:
-// code (r, k) at ((r / 16) * (Kp / 64) + k / 64) * 1024 + (k % 64 / 16) * 256 + (r % 16) * 16 + k % 16, which is the order in which
+// Codes lie in blocks of 16 rows by 64 codes of K, 1 KB each, a row of blocks after the other, K filled up with zeros to 128, an even
+// number of blocks (the tiles' steps come in pairs): code (r, k) at ((r / 16) * (Kp / 64) + k / 64) * 1024 + (k % 64 / 16) * 256 + (r % 16) * 16 + k % 16, which is the order in which
 // the 64 lanes of a wave hold the operand of v_mfma_i32_16x16x64_i8, 16 bytes each.  Behind them the rows' scales, one float each, for
 // the rows filled up to 16.
 constexpr int64_t i8_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
-constexpr int64_t i8_code_bytes(int64_t rows, int64_t K) { return i8_up(rows, 16) * i8_up(K, 64); }
+constexpr int64_t i8_width(int64_t K) { return i8_up(K, 128); }
+constexpr int64_t i8_code_bytes(int64_t rows, int64_t K) { return i8_up(rows, 16) * i8_width(K); }
 struct I8RowsArgs {
     const void *src = nullptr;       // rows of K, `ld` elements apart
     uint8_t *codes = nullptr;
@@ -317,7 +318,14 @@ struct I8RowsArgs {
     const int *source = nullptr;     // row r is src row source[r] / k, or zeros where source[r] < 0; null: row r
     const int *live_rows = nullptr;  // device: rows from here on are left alone; null: all rows
     int k = 1;
+    // with experts: lists of their row tiles for the products to come, written on the side (see I8RowTiles); edge 0: none
+    const int *offsets = nullptr;    // [E + 1]
+    int E = 0;
+    struct { int *list = nullptr; int edge = 0; } tiles[2];
 };
+// A list of row tiles of `edge` rows: four words {tiles in all, 0, 0, 0}, then four for each tile, {its expert's first row, its expert's end,
+// the expert, the number of the expert's first tile}.
+inline size_t i8_tile_list_words(int64_t tiles) { return 4 + 4 * (size_t)tiles; }
 void launch_i8_quantize(const I8RowsArgs &a, hipStream_t st);
 void launch_i8_pack(const int8_t *codes, const float *scales, int64_t rows, int64_t K, uint8_t *out, float *out_scales, hipStream_t st);
 void launch_i8_unpack(const uint8_t *in, const float *in_scales, int64_t rows, int64_t K, int8_t *codes, float *scales, hipStream_t st);
@@ -327,10 +335,13 @@ struct I8GemmArgs {
     void *C = nullptr;
     int64_t M = 0, N = 0, K = 0, ldc = 0;     // N: columns of the result (of one expert)
     int c_f32 = 0;
-    const int *offsets = nullptr;    // device [E + 1], multiples of 16: expert e's rows; its weights are rows e N .. of B.  null: one expert
-    int E = 1;
-    int64_t rows_expected = 0;       // with offsets: rows that tokens fill, of M
+    // With experts: expert e's rows start at a multiple of 16, its weights are rows e N .. of B
+    int E = 0;                       // 0: one matrix
+    int64_t rows_expected = 0;       // rows that tokens fill, of M
+    const int *tiles = nullptr;      // device: the list of row tiles of i8_row_tiles().edge rows
 };
+struct I8RowTiles { int edge; int64_t most; };     // rows of a tile; tiles that the experts can have between them
+I8RowTiles i8_row_tiles(const I8GemmArgs &a);
 void launch_i8_gemm(const I8GemmArgs &a, hipStream_t st);
 // Up to kTokenRows tokens, quantized where they are used (ssg_i8_token.hip); i8_token_ok and i8_mix_ok: whether their codes fit LDS.
 constexpr int kTokenRows = 4;

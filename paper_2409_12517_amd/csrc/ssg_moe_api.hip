@@ -91,7 +91,9 @@ ssg_status check_i8_product(const char *who, int64_t rows, int64_t experts, int6
     return SSG_OK;
 }
 
-struct MoeLayout { size_t ids, weights, counts, offsets, place, source, hist, x_q, h, h_q, o, total; int64_t rows; };
+struct MoeLayout { size_t ids, weights, counts, offsets, place, source, hist, tiles, x_q, h, h_q, o, total; int64_t rows; };
+// words of a list of row tiles, whichever products run (no tile has fewer than 16 rows)
+size_t moe_list_words(int64_t rows) { return (ssg::i8_tile_list_words(rows / 16) + 63) / 64 * 64; }
 MoeLayout moe_layout(const ssg_moe_desc &d) {
     MoeLayout L;
     const ssg_route_desc &r = d.route;
@@ -101,6 +103,7 @@ MoeLayout moe_layout(const ssg_moe_desc &d) {
     auto take = [&](size_t bytes) { size_t at = o; o += align256(bytes); return at; };
     L.ids = take(n * 4); L.weights = take(n * 4); L.counts = take((size_t)r.E * 4); L.offsets = take(((size_t)r.E + 1) * 4);
     L.place = take(n * 4); L.source = take((size_t)L.rows * 4); L.hist = take(ssg::route_hist_bytes(route_args(r)));
+    L.tiles = take(2 * moe_list_words(L.rows) * 4);
     L.x_q = take(i8_bytes(L.rows, d.d));
     L.h = take((size_t)L.rows * d.f * 2);
     L.h_q = take(i8_bytes(L.rows, d.f));
@@ -359,25 +362,34 @@ ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logi
     ssg::I8RowsArgs q;
     q.src = x; q.codes = b + L.x_q; q.scales = const_cast<float *>(i8_scales(b + L.x_q, L.rows, d));
     q.rows = L.rows; q.K = d; q.ld = d; q.bf16 = 1; q.source = a.source; q.live_rows = a.offsets + E; q.k = r.k;
-    ssg::launch_i8_quantize(q, st);
 
     // h = u Swish(g) in bf16
     ssg::I8GemmArgs g;
-    g.A = q.codes; g.sa = q.scales; g.M = L.rows; g.offsets = a.offsets; g.E = (int)E; g.rows_expected = r.T * r.k;
+    g.A = q.codes; g.sa = q.scales; g.M = L.rows; g.E = (int)E; g.rows_expected = r.T * r.k;
     g.B = static_cast<const uint8_t *>(W1); g.sb = i8_scales(W1, E * f, d);
     g.B2 = static_cast<const uint8_t *>(W2); g.sb2 = i8_scales(W2, E * f, d);
     g.C = b + L.h; g.N = f; g.K = d; g.ldc = f;
-    ssg::launch_i8_gemm(g, st);
 
     ssg::I8RowsArgs hq;
     hq.src = b + L.h; hq.codes = b + L.h_q; hq.scales = const_cast<float *>(i8_scales(b + L.h_q, L.rows, f));
     hq.rows = L.rows; hq.K = f; hq.ld = f; hq.bf16 = 1; hq.live_rows = a.offsets + E;
-    ssg::launch_i8_quantize(hq, st);
 
     // the experts' results, in y's type
     ssg::I8GemmArgs o = g;
     o.A = hq.codes; o.sa = hq.scales; o.B = static_cast<const uint8_t *>(W3); o.sb = i8_scales(W3, E * d, f); o.B2 = nullptr; o.sb2 = nullptr;
     o.C = b + L.o; o.N = d; o.K = f; o.ldc = d; o.c_f32 = desc->y_dtype == SSG_F32;
+
+    // the launch that quantizes x lists the row tiles of both products on the side
+    int *lists = reinterpret_cast<int *>(b + L.tiles);
+    const int up = ssg::i8_row_tiles(g).edge, down = ssg::i8_row_tiles(o).edge;
+    q.offsets = a.offsets; q.E = (int)E;
+    q.tiles[0].list = lists; q.tiles[0].edge = up;
+    if (down != up) { q.tiles[1].list = lists + moe_list_words(L.rows); q.tiles[1].edge = down; }
+    g.tiles = lists;
+    o.tiles = down != up ? q.tiles[1].list : lists;
+    ssg::launch_i8_quantize(q, st);
+    ssg::launch_i8_gemm(g, st);
+    ssg::launch_i8_quantize(hq, st);
     ssg::launch_i8_gemm(o, st);
 
     ssg::CombineArgs c;

@@ -304,7 +304,8 @@ __global__ __launch_bounds__(kBlock) void dispatch_kernel(RouteArgs a, int block
     const SortLds s = sort_lds(lds, a.E);
     const int tid = threadIdx.x, block = blockIdx.x;
     // sums of expert 8 q + i lie at i * eights + q meanwhile, so that neighbouring lanes are in neighbouring banks
-    const int eights = hist_stride(a.E) / 8, parts = kBlock / eights;          // E <= 1024: at least eight parts
+    // (few parts where there are few experts: their sums meet in the same words)
+    const int eights = hist_stride(a.E) / 8, parts = min(kBlock / eights, min(blocks, 64));          // E <= 1024: eight threads to eight experts
     uint32_t *total = s.wave_count, *before = total + 8 * eights;
     for (int i = tid; i < 16 * eights; i += kBlock) total[i] = 0;
     __syncthreads();

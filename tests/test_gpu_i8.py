@@ -23,7 +23,7 @@ def rows_of(rows, K, dtype, seed):
 
 def parts(q, rows, K):
     """codes in the layout, scales, of a buffer."""
-    up, wide = -(-rows // 16) * 16, -(-K // 64) * 64
+    up, wide = -(-rows // 16) * 16, -(-K // 128) * 128
     raw = q.cpu().numpy()
     at = -(-up * wide // 256) * 256
     return raw[:up * wide], raw[at:at + 4 * up].view(np.float32)
@@ -112,6 +112,13 @@ def test_product_over_steps_of_k(M, K):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_product_large(M, N, K, dtype):
     product(M, N, K, dtype, 3)
+
+
+@pytest.mark.parametrize("M,N,K", [(4096, 4096, 336), (4200, 4080, 400), (4330, 4096, 656), (4090, 4112, 784), (3970, 4096, 1040), (9000, 2064, 272)])
+def test_product_in_large_tiles(M, N, K):
+    """Whole tiles, tiles with more and with no more than half of their rows, a last column tile of one block; several tiles to a workgroup."""
+    product(M, N, K, torch.bfloat16, M)
+    product(M, N, K, torch.float32, K)
 
 
 def test_product_strided_result_and_the_lowest_code():

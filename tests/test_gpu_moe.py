@@ -61,7 +61,7 @@ class Layer:
         def quantized(ptr, K, want, name):
             if ptr is None:
                 return
-            wide, up = -(-K // 64) * 64, -(-v.rows // 16) * 16
+            wide, up = -(-K // 128) * 128, -(-v.rows // 16) * 16
             codes = read(self.work, ptr, live * wide, torch.uint8).cpu().numpy()
             at = -(-up * wide // 256) * 256
             scales = read(self.work, ptr + at, live, torch.float32).cpu().numpy()
@@ -104,6 +104,13 @@ def test_stages(T, E, k, d, f):
 @pytest.mark.parametrize("y_dtype", [torch.bfloat16, torch.float32])
 def test_stages_larger(T, E, k, d, f, y_dtype):
     layer = Layer(T, E, k, d, f, y_dtype=y_dtype, logits_dtype=torch.bfloat16)
+    layer.check(layer.run())
+
+
+@pytest.mark.parametrize("T,E,k,d,f", [(3700, 2, 1, 528, 2064), (2500, 5, 2, 400, 1552), (900, 6, 2, 1040, 784)])
+def test_stages_with_many_rows(T, E, k, d, f):
+    layer = Layer(T, E, k, d, f)
+    layer.logits[:, 0] += 0.7                                   # rows of every remainder, one expert with more
     layer.check(layer.run())
 
 
