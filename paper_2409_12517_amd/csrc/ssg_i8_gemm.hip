@@ -71,13 +71,31 @@ __device__ __forceinline__ void scaled4(const v4i_t &acc, float sa, const float4
     v[3] = __fmul_rn(__fmul_rn((float)acc[3], sa), sb.w);
 }
 
-// dma16_s where `no` is 0 (wave-uniform).  The branch is inside the statement: the code around it stays one block.
-__device__ __forceinline__ void dma16_unless(int no, const uint8_t *base_uniform, uint32_t lane_off, uint32_t lds_addr) {
+// f(0) to f(N - 1), the numbers as constants
+template <int N, int I = 0, class F> __device__ __forceinline__ void each(F &&f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, I + 1>(f);
+    }
+}
+
+// A load of 16 bytes a lane to LDS in two statements, with an MFMA or two between them, which hide one or two other instructions each and
+// no more: where in LDS (M0, which nothing else here uses), then the load, from a wave-uniform base and 32-bit offsets.  `no`: not if it
+// is 1 (wave-uniform; the branch is inside the statement, so that the code around it stays one block).
+template <int OFF> __device__ __forceinline__ void dma_to(uint32_t lds_addr) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_cmp_lg_u32 %3, 0\n\ts_cbranch_scc1 1f\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n1:"
-                 :: "s"(lds_addr), "v"(lane_off), "s"(base_uniform), "s"(no) : "memory", "m0", "scc");
-#else
-    (void)no; (void)base_uniform; (void)lane_off; (void)lds_addr;
+    asm volatile("s_add_u32 m0, %0, %1" :: "s"(lds_addr), "n"(OFF) : "m0", "scc");
+#endif
+}
+__device__ __forceinline__ void dma_from(const uint8_t *base_uniform, uint32_t lane_off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("global_load_lds_dwordx4 %0, %1" :: "v"(lane_off), "s"(base_uniform) : "memory");
+#endif
+}
+__device__ __forceinline__ void dma_from_unless(int no, const uint8_t *base_uniform, uint32_t lane_off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_cmp_lg_u32 %2, 0\n\ts_cbranch_scc1 1f\n\tglobal_load_lds_dwordx4 %0, %1\n1:"
+                 :: "v"(lane_off), "s"(base_uniform), "s"(no) : "memory", "scc");
 #endif
 }
 
@@ -154,10 +172,26 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
         asm volatile("" : "+v"(l));
         return l;
     };
-    auto issue_one = [&](int j, uint32_t slot) {
-        if (j < WB / 2) dma16_s(src.a + src.a_off[j], lane, src.a_dst + slot + j * 1024u);
-        else if (j < WB) dma16_unless(src.half, src.a + src.a_off[j], lane, src.a_dst + slot + j * 1024u);
-        else dma16_s(src.b + src.b_off[j - WB], lane, b_dst + slot + (j - WB) * 1024u);
+    uint32_t a_lane[WB], b_lane[WB];                     // lane offsets of the blocks of `src`
+    auto take_lanes = [&]() {
+#pragma unroll
+        for (int j = 0; j < WB; ++j) {
+            a_lane[j] = lane + src.a_off[j];
+            b_lane[j] = lane + src.b_off[j];
+        }
+    };
+    take_lanes();
+    // load j of a stage into `slot`: where to, and the load
+    auto issue_to = [&](auto which, uint32_t slot) {
+        constexpr int j = decltype(which)::value;
+        if (j < WB) dma_to<j * 1024>(src.a_dst + slot);
+        else dma_to<(j - WB) * 1024>(b_dst + slot);
+    };
+    auto issue_from = [&](auto which) {
+        constexpr int j = decltype(which)::value;
+        if constexpr (j < WB / 2) dma_from(src.a, a_lane[j]);
+        else if constexpr (j < WB) dma_from_unless(src.half, src.a, a_lane[j]);
+        else dma_from(src.b, b_lane[j - WB]);
     };
     constexpr int kLoads = 2 * WB, kFewest = kLoads - WB / 2;            // of a stage; where the tile is half of one
     static_assert(kLoads == RB, "a load to every column of blocks");
@@ -167,6 +201,7 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
     auto two_loaded = [&]() {
         if ((loaded += 2) == KB) {
             src = next_src;
+            take_lanes();
             loaded = 0;
         }
     };
@@ -197,8 +232,11 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
     look_ahead();
 #pragma unroll
     for (int s = 0; s < kI8Stages; ++s) {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) issue_one(j, s * kStage);
+        each<kLoads>([&](auto j) {
+            issue_to(j, s * kStage);
+            asm volatile("s_nop 0");
+            issue_from(j);
+        });
         src.a += 1024;
         src.b += 1024;
         if (s % 2 == 1) two_loaded();
@@ -228,14 +266,14 @@ template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) 
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
             constexpr int kEvery = RA * RB / (RA + RB);      // MFMAs to a fragment read
-#pragma unroll
-            for (int t = 0; t < RA * RB; ++t) {
-                const int c = t / RA, r = c & 1 ? RA - 1 - t % RA : t % RA;
+            each<RA * RB>([&](auto at) {
+                constexpr int t = decltype(at)::value, c = t / RA, r = c & 1 ? RA - 1 - t % RA : t % RA;
                 acc[r][c] = mfma_i8(fb[set][c], fa[set][r], acc[r][c]);
                 if (t % kEvery == 0 && t / kEvery < RA + RB) read_one(set ^ 1, t / kEvery, next);
-                if (t % RA == RA / 4) issue_one(t / RA, slot);
+                if (t % RA == (RA > 4 ? 1 : 0)) issue_to(std::integral_constant<int, t / RA>{}, slot);
+                if (t % RA == (RA > 4 ? 2 : 1)) issue_from(std::integral_constant<int, t / RA>{});
                 __builtin_amdgcn_sched_barrier(0);
-            }
+            });
             src.a += 1024;
             src.b += 1024;
             slot = next;
@@ -418,19 +456,21 @@ template <int RB, int CB, int WAVES, bool DUAL> __global__ __launch_bounds__(64 
 enum I8Form { FEW_16, FEW_16_EXPERTS, FEW_32, FEW_64, TILE_128, TILE_256 };
 I8Form choose_form(const I8GemmArgs &a, bool dual) {
     const double KB = (double)(i8_width(a.K) / 64), small_step = .52 * KB + 4, small_alone = .28 * KB + 4, large_step = .70 * KB + 9;
+    auto small_time = [&](double tiles) {                // rounds of two to a compute unit, the last one perhaps of one
+        const double rounds = std::floor(tiles / 512), rest = tiles - 512 * rounds;
+        return rounds * small_step + (rest <= 0 ? 0 : rest <= 256 ? small_alone : small_step);
+    };
     const int64_t cols = dual ? 2 * a.N : a.N, cols128 = (cols + 127) / 128, cols256 = (cols + 255) / 256;
     if (a.E == 0) {
         const int64_t tiles128 = (a.M + 127) / 128 * cols128, tiles256 = (a.M + 255) / 256 * cols256;
         if (a.M <= 16) return FEW_16;
         if (a.M <= 32) return FEW_32;
         if (a.M <= 64 || tiles128 <= 64) return FEW_64;
-        const int64_t rounds = tiles128 / 512, rest = tiles128 % 512;
-        const double small = rounds * small_step + (rest == 0 ? 0 : rest <= 256 ? small_alone : small_step);
-        return (double)((tiles256 + 255) / 256) * large_step < small ? TILE_256 : TILE_128;
+        return (double)((tiles256 + 255) / 256) * large_step < small_time((double)tiles128) ? TILE_256 : TILE_128;
     }
     const double active = (double)std::min<int64_t>(a.E, a.rows_expected), rows = (double)a.rows_expected / active;
     if (rows <= 12) return FEW_16_EXPERTS;
-    const double small = active * std::max(.6, rows / 128 + .3) * cols128 / 512 * small_step;
+    const double small = small_time(active * std::max(.6, rows / 128 + .3) * cols128);
     const double large = std::ceil(active * std::max(.6, rows / 256 + .3) * cols256 / 256) * large_step;
     return large < small ? TILE_256 : TILE_128;
 }
