@@ -39,7 +39,7 @@ EXPORTS = [
     "ssg_infer_noalloc_max_bytes", "ssg_infer_fwd_noalloc",
     "ssg_adam_state_bytes", "ssg_adam_init", "ssg_adam_step", "ssg_adam_step_wait", "ssg_adam_view_state",
     "ssg_route_workspace_bytes", "ssg_route_rows", "ssg_route", "ssg_route_bwd",
-    "ssg_i8_bytes", "ssg_i8_quantize", "ssg_i8_pack", "ssg_i8_unpack", "ssg_i8_gemm", "ssg_i8_linear_workspace_bytes", "ssg_i8_linear",
+    "ssg_i8_bytes", "ssg_i8_quantize", "ssg_i8_pack", "ssg_i8_unpack", "ssg_i8_gemm", "ssg_i8_gemm_plan", "ssg_i8_linear_workspace_bytes", "ssg_i8_linear",
     "ssg_moe_workspace_bytes", "ssg_moe_fwd", "ssg_moe_view_workspace",
     "ssg_profile_enable", "ssg_profile_select", "ssg_profile_read",
 ]
@@ -164,6 +164,7 @@ _lib.ssg_i8_quantize.argtypes = [c_void_p, c_int, c_int64, c_int64, c_int64, c_v
 _lib.ssg_i8_pack.argtypes = [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_size_t, c_void_p]
 _lib.ssg_i8_unpack.argtypes = [c_void_p, c_size_t, c_int64, c_int64, c_void_p, c_void_p, c_void_p]
 _lib.ssg_i8_gemm.argtypes = [c_void_p, c_size_t, c_int64, c_void_p, c_size_t, c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p]
+_lib.ssg_i8_gemm_plan.argtypes = [c_int64, c_int64, c_int64, c_int32, c_int, POINTER(ssg_gemm_plan)]
 _lib.ssg_i8_linear_workspace_bytes.argtypes = [c_int64, c_int64]
 _lib.ssg_i8_linear_workspace_bytes.restype = c_size_t
 _lib.ssg_i8_linear.argtypes = [c_void_p, c_int, c_int64, c_int64, c_int64, c_void_p, c_size_t, c_int64, c_void_p, c_int, c_int64,
@@ -467,6 +468,12 @@ def ssg_i8_unpack(q, rows, K, codes, scales, stream=None, q_bytes=None) -> None:
 
 def ssg_i8_gemm(A, M, B, N, K, C, c_dtype, ldc, stream=None, A_bytes=None, B_bytes=None) -> None:
     _check(_lib.ssg_i8_gemm(_ptr(A), _nbytes(A, A_bytes), M, _ptr(B), _nbytes(B, B_bytes), N, K, _ptr(C), c_dtype, ldc, _stream(stream)))
+
+
+def ssg_i8_gemm_plan(M, N, K, experts=0, swiglu=0) -> ssg_gemm_plan:
+    p = ssg_gemm_plan()
+    _check(_lib.ssg_i8_gemm_plan(M, N, K, experts, swiglu, ctypes.byref(p)))
+    return p
 
 
 def ssg_i8_linear_workspace_bytes(M: int, K: int) -> int:

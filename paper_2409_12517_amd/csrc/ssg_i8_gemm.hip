@@ -512,6 +512,13 @@ I8RowTiles i8_row_tiles(const I8GemmArgs &a) {
     return {edge, (a.M + std::min<int64_t>(a.E, a.rows_expected) * (edge - 16)) / edge};
 }
 
+I8Plan i8_gemm_plan(const I8GemmArgs &a) {
+    const I8Form form = choose_form(a, a.B2 != nullptr);
+    const int edge = form_edge(form);
+    if (form == TILE_256 || form == TILE_128) return {edge, edge, a.B2 ? edge / 2 : edge};
+    return {0, edge, form == FEW_64 ? 32 : 16};
+}
+
 void launch_i8_gemm(const I8GemmArgs &a, hipStream_t st) {
     if (a.M == 0) return;
     if (a.B2) launch_form<true>(a, st);

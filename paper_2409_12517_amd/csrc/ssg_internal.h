@@ -342,6 +342,8 @@ struct I8GemmArgs {
 };
 struct I8RowTiles { int edge; int64_t most; };     // rows of a tile; tiles that the experts can have between them
 I8RowTiles i8_row_tiles(const I8GemmArgs &a);
+struct I8Plan { int tile, rows, cols; };           // edge of the tiles, or 0 and the rows and columns of a workgroup
+I8Plan i8_gemm_plan(const I8GemmArgs &a);
 void launch_i8_gemm(const I8GemmArgs &a, hipStream_t st);
 // Up to kTokenRows tokens, quantized where they are used (ssg_i8_token.hip); i8_token_ok and i8_mix_ok: whether their codes fit LDS.
 constexpr int kTokenRows = 4;

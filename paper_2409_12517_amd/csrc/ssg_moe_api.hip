@@ -249,6 +249,22 @@ ssg_status ssg_i8_gemm(const void *A, size_t A_bytes, int64_t M, const void *B, 
     return check_launch(who);
 }
 
+ssg_status ssg_i8_gemm_plan(int64_t M, int64_t N, int64_t K, int32_t experts, int swiglu, ssg_gemm_plan *out) {
+    const char *who = "ssg_i8_gemm_plan";
+    SSG_CHECK(check_i8_shape(who, M, K));
+    if (experts < 0 || experts > ssg::kMaxExperts) return fail(SSG_ERR_SHAPE, "%s: %d experts (0 to %d)", who, experts, ssg::kMaxExperts);
+    if (swiglu != 0 && swiglu != 1) return fail(SSG_ERR_ARG, "%s: swiglu %d (0 or 1)", who, swiglu);
+    SSG_CHECK(check_i8_product(who, M, std::max(experts, 1), N));
+    if (M == 0) return fail(SSG_ERR_SHAPE, "%s: no rows, no kernel", who);
+    if (!out) return fail(SSG_ERR_ARG, "%s: out is NULL", who);
+    ssg::I8GemmArgs g;
+    static const uint8_t some = 0;
+    g.M = M; g.N = N; g.K = K; g.E = experts; g.rows_expected = M; g.B2 = swiglu ? &some : nullptr;
+    const ssg::I8Plan p = ssg::i8_gemm_plan(g);
+    *out = ssg_gemm_plan{p.tile, p.tile ? 4 : 0, 0, p.tile ? 0 : p.rows, p.tile ? 0 : p.cols, 1};
+    return SSG_OK;
+}
+
 size_t ssg_i8_linear_workspace_bytes(int64_t M, int64_t K) {
     if (check_i8_shape("ssg_i8_linear_workspace_bytes", M, K) != SSG_OK) return 0;
     return i8_bytes(M, K);

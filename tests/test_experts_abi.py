@@ -98,6 +98,23 @@ def test_moe_refusals():
     refused(ssg.SSG_ERR_ARG, "reserved", ssg.ssg_moe_fwd, desc, *[4096] * 8, **sizes)
 
 
+def test_plan():
+    """Host logic only: which kernel a product runs in."""
+    def plan(*args):
+        p = ssg.ssg_i8_gemm_plan(*args)
+        return (p.tile, p.rows, p.cols)
+
+    assert [plan(M, 4096, 4096) for M in (1, 16, 17, 32, 33, 64)] == [(0, 16, 16)] * 2 + [(0, 32, 16)] * 2 + [(0, 64, 32)] * 2
+    assert plan(256, 4096, 4096) == (0, 64, 32) and plan(257, 4096, 4096) == (128, 0, 0)          # 64 and 96 tiles of 128
+    assert plan(4096, 4096, 11008) == (256, 0, 0) and plan(2048, 4096, 11008) == (128, 0, 0)
+    # experts: 12 rows each on average, and one more
+    assert plan(64 * 12, 1376, 2048, 64, 1) == (0, 16, 16) and plan(64 * 12 + 64, 1376, 2048, 64, 1) == (128, 0, 0)
+    assert plan(4096 * 8, 1376, 2048, 64, 1) == (256, 0, 0) == plan(4096 * 8, 2048, 1376, 64, 0)
+    for args in ((0, 16, 16), (16, 20, 16), (16, 16, 16, -1), (16, 16, 16, 2000), (16, 16, 16, 4, 2)):
+        with pytest.raises(ssg.SsgError):
+            ssg.ssg_i8_gemm_plan(*args)
+
+
 def test_workspaces_do_not_shrink_with_more_tokens():
     last = 0
     for T in list(range(0, 300)) + [1000, 1 << 14]:

@@ -114,9 +114,11 @@ def test_product_large(M, N, K, dtype):
     product(M, N, K, dtype, 3)
 
 
-@pytest.mark.parametrize("M,N,K", [(4096, 4096, 336), (4200, 4080, 400), (4330, 4096, 656), (4090, 4112, 784), (3970, 4096, 1040), (9000, 2064, 272)])
-def test_product_in_large_tiles(M, N, K):
+@pytest.mark.parametrize("tile,M,N,K", [(256, 4096, 4096, 336), (256, 3970, 4096, 1040), (256, 3900, 4080, 656), (256, 7960, 4080, 784), (256, 8030, 4096, 400),
+                                        (128, 4200, 4080, 400), (128, 9000, 2064, 272), (128, 4170, 4112, 784), (128, 1290, 2064, 1040)])
+def test_product_in_tiles(tile, M, N, K):
     """Whole tiles, tiles with more and with no more than half of their rows, a last column tile of one block; several tiles to a workgroup."""
+    assert ssg.ssg_i8_gemm_plan(M, N, K).tile == tile
     product(M, N, K, torch.bfloat16, M)
     product(M, N, K, torch.float32, K)
 

@@ -107,11 +107,23 @@ def test_stages_larger(T, E, k, d, f, y_dtype):
     layer.check(layer.run())
 
 
-@pytest.mark.parametrize("T,E,k,d,f", [(3700, 2, 1, 528, 2064), (2500, 5, 2, 400, 1552), (900, 6, 2, 1040, 784)])
-def test_stages_with_many_rows(T, E, k, d, f):
+@pytest.mark.parametrize("up,down,T,E,k,d,f", [(256, 128, 3700, 2, 1, 528, 2064), (128, 256, 3700, 2, 1, 4096, 528), (128, 128, 2500, 5, 2, 400, 1552),
+                                               (128, 128, 900, 6, 2, 1040, 784), (0, 0, 90, 40, 5, 272, 336)])
+def test_stages_in_every_kernel(up, down, T, E, k, d, f):
+    assert ssg.ssg_i8_gemm_plan(T * k, f, d, E, 1).tile == up and ssg.ssg_i8_gemm_plan(T * k, d, f, E, 0).tile == down
     layer = Layer(T, E, k, d, f)
     layer.logits[:, 0] += 0.7                                   # rows of every remainder, one expert with more
     layer.check(layer.run())
+
+
+def test_a_token_that_is_not_finite_stays_its_own():
+    for T in (3, 60):
+        layer = Layer(T, 6, 2, 64, 48)
+        clean = layer.run().clone()
+        layer.x[1, 5] = torch.nan
+        y = layer.run()
+        others = torch.arange(T, device=DEV) != 1
+        assert torch.isnan(y[1]).all() and torch.equal(y[others], clean[others])
 
 
 def test_groups_bias_and_padding_tokens():
