@@ -275,7 +275,7 @@ struct RouteArgs {
     int64_t T = 0, ld = 0, rows = 0;
     int E = 0, k = 0, bf16 = 0, score = 0, groups = 1, top_groups = 1, group_top = 1, renorm = 0, align = 1;
     float scale = 1.0f;
-    int block_tokens = 0, lds_keys = 0;     // filled in by the launcher
+    int block_tokens = 0, lds_keys = 0, key_stride = 0;     // filled in by the launcher
 };
 struct RouteBwdArgs {
     const void *logits = nullptr;

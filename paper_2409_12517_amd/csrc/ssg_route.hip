@@ -65,7 +65,27 @@ __device__ __forceinline__ float held(float z) { return fminf(z, 3.402823466e+38
 
 constexpr float kTiny = 1e-38f;                           // what a sum of scores is held above where it divides
 
-// The experts of token t: lane j of the group returns the j-th (or -1) in id, its weight in w.  `keys`: E words of LDS of the
+// The k largest keys of the group's lanes, key i of lane l in slot l + i LPT: lane j returns the slot of the j-th, -1 if there is none.
+template <int LPT, int VPL> __device__ __forceinline__ int pick(uint32_t (&key)[VPL], int k) {
+    const int g0 = threadIdx.x & (LPT - 1);
+    int slot = -1;
+    for (int j = 0; j < k; ++j) {
+        uint32_t best = 0, e = 0xffffffffu;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i)
+            if (key[i] > best) { best = key[i]; e = (uint32_t)(g0 + i * LPT); }
+        const uint32_t all = reduce_max<LPT>(best);
+        e = reduce_min<LPT>(best == all ? e : 0xffffffffu);
+        if (all == 0) e = 0xffffffffu;
+        if (g0 == j) slot = (int)e;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i)
+            if (e == (uint32_t)(g0 + i * LPT)) key[i] = 0;
+    }
+    return slot;
+}
+
+// The experts of token t: lane j of the group returns the j-th (or -1) in id, its weight in w.  `keys`: a.key_stride words of LDS of the
 // group's own (used with groups only).  All lanes of a wave come here together; `live` says whether the group has a token.
 template <int LPT, int VPL, bool BF16>
 __device__ __forceinline__ void choose(const RouteArgs &a, int64_t t, bool live, uint32_t *keys, int &id, float &w) {
@@ -116,14 +136,18 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t t, bool live,
         }
         __builtin_amdgcn_wave_barrier();
         __threadfence_block();
-        const int group = g0 / L, sub = g0 % L;
+        const int group = g0 / L, sub = g0 % L, count = (size + L - 1) / L;
         uint32_t first = 0, second = 0;
         if (group < a.groups) {
+            // (each group from another place on, since those of the same size begin in the same bank)
+            int n = group % count;
 #pragma unroll 4
-            for (int i = sub; i < size; i += L) {
-                const uint32_t u = keys[group * size + i];
+            for (int i = 0; i < count; ++i) {
+                const int x = sub + n * L;
+                const uint32_t u = x < size ? keys[group * size + x] : 0;
                 second = u > first ? first : (u > second ? u : second);
                 first = u > first ? u : first;
+                n = n + 1 == count ? 0 : n + 1;
             }
         }
         for (int step = 1; step < L; step *= 2) {
@@ -137,32 +161,45 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t t, bool live,
         if (a.group_top == 2 && first && second) mine = ordered(from_ordered(first) + from_ordered(second));
         int ahead = 0;
         const int lane0 = (threadIdx.x & 63) - g0;
+#pragma unroll 4
         for (int g = 0; g < a.groups; ++g) {
             const uint32_t other = (uint32_t)__shfl((int)mine, lane0 + g * L, 64);
             ahead += other > mine || (other == mine && g < group);
         }
-        const uint64_t kept = __ballot(group < a.groups && ahead < a.top_groups) >> lane0;
-        const uint32_t inv = ((1u << 20) + size - 1) / size;          // e * inv >> 20 = e / size for e, size up to 1024
+        // The experts of the groups that stay, in their order, are what is chosen from: slot s is number s % size of the group that
+        // is number s / size among them.
+        const bool stays = group < a.groups && sub == 0 && ahead < a.top_groups;
+        const uint64_t kept = __ballot(stays) >> lane0;
+        uint32_t *starts = keys + a.E;
+        if (stays) starts[__popcll(kept & ((1ull << g0) - 1))] = (uint32_t)(group * size);
+        if (a.group_top == 2 && !biased) {                 // (by their scores until now)
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            const uint32_t g = ((uint32_t)(g0 + i * LPT) * inv) >> 20;
-            if (g < (uint32_t)a.groups && !(kept >> (g * L) & 1)) key[i] = 0;
+            for (int i = 0; i < VPL; ++i)
+                if (g0 + i * LPT < a.E) keys[g0 + i * LPT] = key[i];
         }
         __builtin_amdgcn_wave_barrier();
-    }
-    id = -1;
-    for (int j = 0; j < a.k; ++j) {
-        uint32_t best = 0, e = 0xffffffffu;
+        __threadfence_block();
+        const int slots = a.top_groups * size;
+        const uint32_t inv = ((1u << 20) + size - 1) / size;          // s * inv >> 20 = s / size for s, size up to 1024
+        auto expert = [&](int s) {
+            const uint32_t nth = (uint32_t)s * inv >> 20;
+            return starts[nth] + (uint32_t)s - nth * size;
+        };
+        auto pick_kept = [&](auto values) {
+            uint32_t k2[decltype(values)::value];
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (key[i] > best) { best = key[i]; e = (uint32_t)(g0 + i * LPT); }
-        const uint32_t all = reduce_max<LPT>(best);
-        e = reduce_min<LPT>(best == all ? e : 0xffffffffu);
-        if (all == 0) e = 0xffffffffu;
-        if (g0 == j) id = (int)e;
-#pragma unroll
-        for (int i = 0; i < VPL; ++i)
-            if (e == (uint32_t)(g0 + i * LPT)) key[i] = 0;
+            for (int i = 0; i < decltype(values)::value; ++i) {
+                const int s = g0 + i * LPT;
+                k2[i] = live && s < slots ? keys[expert(s)] : 0u;
+            }
+            return pick<LPT>(k2, a.k);
+        };
+        constexpr int kHalf = VPL > 1 ? VPL / 2 : 1;
+        id = slots <= kHalf * LPT ? pick_kept(std::integral_constant<int, kHalf>{}) : pick_kept(std::integral_constant<int, VPL>{});
+        if (id >= 0) id = (int)expert(id);
+        __builtin_amdgcn_wave_barrier();
+    } else {
+        id = pick<LPT>(key, a.k);
     }
     w = 0.0f;
     if (id >= 0) {
@@ -266,7 +303,7 @@ template <int LPT, int VPL, bool BF16> __global__ __launch_bounds__(kBlock) void
     if (a.place)
         for (int e = tid; e < a.E; e += kBlock) hist[e] = 0;
     __syncthreads();
-    uint32_t *keys = lds + a.lds_keys + (size_t)(tid / LPT) * a.E;
+    uint32_t *keys = lds + a.lds_keys + (size_t)(tid / LPT) * a.key_stride;
     const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
     const int64_t t1 = t0 + a.block_tokens < a.T ? t0 + a.block_tokens : a.T;
     constexpr int kAtOnce = kBlock / LPT;
@@ -538,7 +575,9 @@ void launch_route(RouteArgs a, hipStream_t st) {
     const size_t sort_words = 3 * (size_t)a.E + 1 + (size_t)kWaves * hist_stride(a.E);
     // the keys of all tokens in hand (with groups), and the sort's words; in the launch that sorts too, one after the other
     a.lds_keys = a.E;
-    const size_t key_words = a.E + (grouped ? (size_t)kBlock / p.lpt * a.E : 0);
+    // (with groups a token's keys and where its groups that stay begin; the tokens of a wave 16 banks apart)
+    a.key_stride = (a.E + a.groups + 47) / 64 * 64 + 16;
+    const size_t key_words = a.E + (grouped ? (size_t)kBlock / p.lpt * a.key_stride : 0);
     const size_t words = a.place && p.blocks == 1 ? std::max(sort_words, key_words) : key_words;
     const double bytes = (double)a.T * a.E * (a.bf16 ? 2 : 4) + 8.0 * a.T * a.k;
     profile_before(kTagRoute, st, bytes);
