@@ -424,7 +424,7 @@ ssg_status ssg_i8_unpack(const void *q, size_t q_bytes, int64_t rows, int64_t K,
 ssg_status ssg_i8_gemm(const void *A, size_t A_bytes, int64_t M, const void *B, size_t B_bytes, int64_t N, int64_t K, void *C,
                        ssg_dtype c_dtype, int64_t ldc, void *stream);
 /* Which kernel such a product runs in, for tests and reports (host logic; nothing is launched): with experts > 0 that of a mixture's
- * products, M the assignments (tokens times k) and N the columns of one expert, swiglu = 1 the gate/up form.  tile: 256 or 128, the edge of
+ * products, M the assignments (tokens times k) and N the columns of one expert; swiglu = 1 the gate/up form, with experts only.  tile: 256 or 128, the edge of
  * the tiles; 0: rows x cols of the result to a workgroup that shares K out among its waves. */
 ssg_status ssg_i8_gemm_plan(int64_t M, int64_t N, int64_t K, int32_t experts, int swiglu, ssg_gemm_plan *out);
 /* y = x W^T with x quantized in the call, a scale for each token: ssg_i8_quantize and ssg_i8_gemm.  W: N rows of K. */

@@ -5,8 +5,8 @@
 //
 // Both operands lie in blocks of 16 rows by 64 codes in the order in which a wave holds them (see I8RowsArgs), so a block
 // is one 1 KB load, to LDS or straight to registers, with nothing to permute and no LDS bank conflicts.
-// With experts the rows of C are sorted by expert and every expert's start at a multiple of 16; a workgroup finds its expert from the
-// offsets on the device, so that nothing waits for the host.
+// With experts the rows of C are sorted by expert and every expert starts at a multiple of 16; the row tiles of all of them are listed
+// on the device (see I8RowsArgs), so that nothing waits for the host, which launches for the most there can be.
 #include <cmath>
 
 #include "ssg_gemm_tile.h"
@@ -444,15 +444,18 @@ template <int RB, int CB, int WAVES, bool DUAL> __global__ __launch_bounds__(64 
 }
 
 // Which kernel, from the extents alone.
-// One matrix.  Up to 16 and up to 32 rows the blocks that fit them.  Then 64 x 32 where 128 x 128 tiles would leave three quarters
-// of the chip idle (4096 x 11008 by 128 rows 20 us and 49 in 32 tiles; 1040 x 2736 by 333 8 and 12; with 96 tiles, 4096 x 4096 by 333,
-// 22 and 17), and up to 64 rows always (11008 x 4096 17.5 and 19.6).
-// Experts: blocks of 16 rows while an expert has no more on average than 12, which reads weights at 6.0 TB/s (64 experts, d = 2048,
-// f = 1376, 64 tokens of 8: gate/up 60 us, 69 in 128 x 128 tiles; with 16 rows on average 74 and 72, with 32 120 and 77).
+// One matrix.  The smallest blocks whose workgroups the chip holds at once, one to a compute unit, since their waves share K out: 16 x 16
+// (512 x 11008 by 64 rows 7.8 us, 11.3 in 32 x 16 and 19.1 in 64 x 32; 4096 x 11008 by 17 rows, where there are 512 of them, 15.6 and 13.6)
+// and 32 x 16 (512 x 11008 by 256 rows 11.9, 17.4 in 64 x 32; 4096 x 4096 by 33 rows 8.8 and 8.6); up to 16 and up to 32 rows always.
+// Then 64 x 32 where 128 x 128 tiles would leave three quarters of the chip idle (4096 x 11008 by 128 rows 20 us and 49 in 32 tiles;
+// 1040 x 2736 by 333 7.6 and 11.6; with 96 tiles, 4096 x 4096 by 333, 21.5 and 15.6), and up to 64 rows always (11008 x 4096 17.3 and 18.2).
+// Experts: blocks of 16 rows while an expert has no more on average than 12 (64 experts, d = 2048, f = 1376, 64 tokens of 8: gate/up
+// 60 us, 67 in 128 x 128 tiles; with 16 rows on average 77 and 69, with 32 110 and 70).
 // Between the tiles: estimated times, where a step of 64 along K takes a compute unit .52 us with two small tiles on it, .28 with
 // one, .70 with a large one, and a tile 4 and 9 us beside its steps; with experts half a tile each beyond their average
-// rows.  (4096 x 4096 x 11008 133 us in large and 176 in small tiles, 2048 rows 102 and 92; the 64 experts at 4096 tokens 223 and
-// 241, at 2048 161 and 141.  Over 98 products 3 % above the better one on average, at most 14 %.)
+// rows, and a twentieth more for the large ones.  (4096 x 4096 x 11008 131 us in large and 176 in small tiles, 2048 rows 101 and 93; gate/up of
+// the 64 experts at 4096 tokens 222 and 233, at 2048 155 and 136.  Of 46 products with experts the choice takes .7 % longer on average than
+// the better of the two, at most 14 %.)
 enum I8Form { FEW_16, FEW_16_EXPERTS, FEW_32, FEW_64, TILE_128, TILE_256 };
 I8Form choose_form(const I8GemmArgs &a, bool dual) {
     const double KB = (double)(i8_width(a.K) / 64), small_step = .52 * KB + 4, small_alone = .28 * KB + 4, large_step = .70 * KB + 9;
@@ -463,15 +466,16 @@ I8Form choose_form(const I8GemmArgs &a, bool dual) {
     const int64_t cols = dual ? 2 * a.N : a.N, cols128 = (cols + 127) / 128, cols256 = (cols + 255) / 256;
     if (a.E == 0) {
         const int64_t tiles128 = (a.M + 127) / 128 * cols128, tiles256 = (a.M + 255) / 256 * cols256;
-        if (a.M <= 16) return FEW_16;
-        if (a.M <= 32) return FEW_32;
+        const int64_t cols16 = (a.N + 15) / 16;
+        if (a.M <= 16 || (a.M + 15) / 16 * cols16 <= 256) return FEW_16;
+        if (a.M <= 32 || (a.M + 31) / 32 * cols16 <= 256) return FEW_32;
         if (a.M <= 64 || tiles128 <= 64) return FEW_64;
         return (double)((tiles256 + 255) / 256) * large_step < small_time((double)tiles128) ? TILE_256 : TILE_128;
     }
     const double active = (double)std::min<int64_t>(a.E, a.rows_expected), rows = (double)a.rows_expected / active;
     if (rows <= 12) return FEW_16_EXPERTS;
-    const double small = small_time(active * std::max(.6, rows / 128 + .3) * cols128);
-    const double large = std::ceil(active * std::max(.6, rows / 256 + .3) * cols256 / 256) * large_step;
+    const double small = small_time(active * std::max(.6, rows / 128 + .5) * cols128);
+    const double large = std::ceil(active * std::max(.6, rows / 256 + .5) * cols256 / 256) * 1.05 * large_step;
     return large < small ? TILE_256 : TILE_128;
 }
 
@@ -493,13 +497,13 @@ template <bool DUAL> void launch_form(const I8GemmArgs &a, hipStream_t st) {
     constexpr int64_t kAll = (int64_t)1 << 31;
     const int64_t units = p.KB > kI8Stages ? 256 : kAll;
     profile_before(DUAL ? kTagI8Swiglu : kTagI8Gemm, st);
-    switch (form) {
-        case FEW_16: go(i8_few_kernel<1, 1, 8, DUAL>, 16, 512, kAll); break;
-        case FEW_16_EXPERTS: go(i8_few_kernel<1, 1, 4, DUAL>, 16, 256, kAll); break;
-        case FEW_32: go(i8_few_kernel<2, 1, 4, DUAL>, 16, 256, kAll); break;
-        case FEW_64: go(i8_few_kernel<4, 2, 8, DUAL>, 32, 512, kAll); break;
-        case TILE_128: go(i8_tile_kernel<2, DUAL>, DUAL ? 64 : 128, 256, 2 * units); break;
-        case TILE_256: go(i8_tile_kernel<4, DUAL>, DUAL ? 128 : 256, 256, units); break;
+    if (form == TILE_128) go(i8_tile_kernel<2, DUAL>, DUAL ? 64 : 128, 256, 2 * units);
+    else if (form == TILE_256) go(i8_tile_kernel<4, DUAL>, DUAL ? 128 : 256, 256, units);
+    else if (form == FEW_16_EXPERTS) go(i8_few_kernel<1, 1, 4, DUAL>, 16, 256, kAll);
+    else if constexpr (!DUAL) {                          // (two matrices only with experts)
+        if (form == FEW_16) go(i8_few_kernel<1, 1, 8, false>, 16, 512, kAll);
+        else if (form == FEW_32) go(i8_few_kernel<2, 1, 4, false>, 16, 256, kAll);
+        else go(i8_few_kernel<4, 2, 8, false>, 32, 512, kAll);
     }
     profile_after(st);
 }

@@ -254,6 +254,7 @@ ssg_status ssg_i8_gemm_plan(int64_t M, int64_t N, int64_t K, int32_t experts, in
     SSG_CHECK(check_i8_shape(who, M, K));
     if (experts < 0 || experts > ssg::kMaxExperts) return fail(SSG_ERR_SHAPE, "%s: %d experts (0 to %d)", who, experts, ssg::kMaxExperts);
     if (swiglu != 0 && swiglu != 1) return fail(SSG_ERR_ARG, "%s: swiglu %d (0 or 1)", who, swiglu);
+    if (swiglu && experts == 0) return fail(SSG_ERR_UNSUPPORTED, "%s: the gate/up form is a mixture's (experts > 0)", who);
     SSG_CHECK(check_i8_product(who, M, std::max(experts, 1), N));
     if (M == 0) return fail(SSG_ERR_SHAPE, "%s: no rows, no kernel", who);
     if (!out) return fail(SSG_ERR_ARG, "%s: out is NULL", who);

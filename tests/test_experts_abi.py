@@ -105,12 +105,14 @@ def test_plan():
         return (p.tile, p.rows, p.cols)
 
     assert [plan(M, 4096, 4096) for M in (1, 16, 17, 32, 33, 64)] == [(0, 16, 16)] * 2 + [(0, 32, 16)] * 2 + [(0, 64, 32)] * 2
+    # few columns: the smallest blocks whose workgroups the chip holds at once
+    assert plan(128, 512, 11008) == (0, 16, 16) and plan(129, 512, 11008) == (0, 32, 16) and plan(257, 512, 11008) == (0, 64, 32)
     assert plan(256, 4096, 4096) == (0, 64, 32) and plan(257, 4096, 4096) == (128, 0, 0)          # 64 and 96 tiles of 128
     assert plan(4096, 4096, 11008) == (256, 0, 0) and plan(2048, 4096, 11008) == (128, 0, 0)
     # experts: 12 rows each on average, and one more
     assert plan(64 * 12, 1376, 2048, 64, 1) == (0, 16, 16) and plan(64 * 12 + 64, 1376, 2048, 64, 1) == (128, 0, 0)
     assert plan(4096 * 8, 1376, 2048, 64, 1) == (256, 0, 0) == plan(4096 * 8, 2048, 1376, 64, 0)
-    for args in ((0, 16, 16), (16, 20, 16), (16, 16, 16, -1), (16, 16, 16, 2000), (16, 16, 16, 4, 2)):
+    for args in ((0, 16, 16), (16, 20, 16), (16, 16, 16, -1), (16, 16, 16, 2000), (16, 16, 16, 4, 2), (16, 16, 16, 0, 1)):
         with pytest.raises(ssg.SsgError):
             ssg.ssg_i8_gemm_plan(*args)
 

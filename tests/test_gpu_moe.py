@@ -107,7 +107,7 @@ def test_stages_larger(T, E, k, d, f, y_dtype):
     layer.check(layer.run())
 
 
-@pytest.mark.parametrize("up,down,T,E,k,d,f", [(256, 128, 3700, 2, 1, 528, 2064), (128, 256, 3700, 2, 1, 4096, 528), (128, 128, 2500, 5, 2, 400, 1552),
+@pytest.mark.parametrize("up,down,T,E,k,d,f", [(256, 128, 3100, 2, 1, 528, 2064), (128, 128, 3700, 2, 1, 528, 2064), (128, 256, 3700, 2, 1, 4096, 528), (128, 128, 2500, 5, 2, 400, 1552),
                                                (128, 128, 900, 6, 2, 1040, 784), (0, 0, 90, 40, 5, 272, 336)])
 def test_stages_in_every_kernel(up, down, T, E, k, d, f):
     assert ssg.ssg_i8_gemm_plan(T * k, f, d, E, 1).tile == up and ssg.ssg_i8_gemm_plan(T * k, d, f, E, 0).tile == down
