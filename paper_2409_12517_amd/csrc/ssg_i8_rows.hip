@@ -13,7 +13,8 @@ namespace ssg {
 
 namespace {
 
-// Bound by memory.  A block owns 8 rows, half of one of the layout's: thread t has row t % 8 and every (threads / 8)-th run of 16 codes, so
+// Bound by memory: 4096 rows of 11008 bf16 (135 MB) 30 us, 4.5 TB/s; 4096 tokens of 2048 gathered into 32768 rows (17 MB read eight
+// times, out of the caches, 67 MB written) 28 us.  A block owns 8 rows, half of one of the layout's: thread t has row t % 8 and every (threads / 8)-th run of 16 codes, so
 // that a wave reads 8 rows x 128 elements and writes pieces of 128 bytes.  The first HELD runs of a thread stay in registers between the
 // maximum and the codes; what a row has beyond them is read again, out of the L2.
 constexpr int kRows = 8;

@@ -6,6 +6,9 @@
 //   i8_token_kernel   up to four rows by 16 columns of one matrix, or one row by 16 columns of the two matrices of the expert that
 //                     an assignment (token, choice) names, with the SwiGLU product; waves share K out
 //   i8_mix_kernel     16 columns of a token's result: its experts side by side, a few waves each, and their weighted sum
+// One token: 11008 x 4096 10.6 us, 4.2 TB/s (15.4 with the rows quantized in a launch before); 8 experts of d = 2048, f = 1376
+// 9.9 + 11.3 us for 45 + 23 MB (43 us a call in five launches, 27 in three).  What bounds them now is the start and the end of a single
+// round of workgroups: x and the first weights from memory, two barriers, the sums in LDS.
 #include "ssg_gemm_tile.h"
 #include "ssg_i8.h"
 

@@ -9,6 +9,9 @@
 // A group of LPT lanes owns a token, expert e in lane e % LPT, so that a wave of 16-lane groups chooses for four tokens at once.
 // Keys are compared as integers that order like the floats; 0 is "closed" or "already taken".  Each of the k rounds is a scan of the
 // lane's own keys and two reductions over the group (largest key, lowest expert that has it) in DPP steps.
+// Long batches are bound by the vector ALU: 16384 tokens, 256 experts, sigmoid and bias, 8 of 4 groups of 8: 16 us (21 with the keys of
+// all groups in every round and the groups read in step, from the same banks), half the time with k = 1; 17 MB would take 3.3.  Short ones
+// by latency: 331 tokens 8.5 us.  The order of the rows is a second launch (5 to 9 us), whose blocks each need the counts of all.
 #include "ssg_device.h"
 #include "ssg_internal.h"
 
@@ -383,7 +386,8 @@ __global__ __launch_bounds__(kBlock) void dispatch_kernel(RouteArgs a, int block
 // With q_j = ds/dw of the chosen: (scale dw_j - sum_i w_i dw_i) / S where renormalised (S the sum of the chosen scores), else scale dw_j;
 //   sigmoid: dz_j = q_j s_j (1 - s_j)        softmax: dz_e = s_e ([e chosen] q_e - sum_j q_j s_j)
 // and with renormalised softmax weights the last sum is zero and s_j / S = w_j / scale: only the chosen experts' logits have one.
-// A block forms the rows of its tokens in LDS, 16 lanes to a token, and streams them out.
+// A block forms the rows of its tokens in LDS, 16 lanes to a token, and streams them out: 16384 x 256 fp32 (17 MB written, 1.5 read)
+// 6.9 us, which is the writes and a launch.  Without renormalisation the row's logits are read too.
 constexpr int kBwdThreads = 256, kBwdTokens = kBwdThreads / 16;
 template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_kernel(RouteBwdArgs a) {
     extern __shared__ float rows[];
@@ -489,7 +493,8 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
 }
 
 // ---- the weighted sum of the experts' rows -------------------------------------------------------------------
-// y[t] = sum_j w[t,j] o[place[t,j]], in the order of j, in fp32.  A thread owns 8 columns of a token.
+// y[t] = sum_j w[t,j] o[place[t,j]], in the order of j, in fp32.  A thread owns 8 columns of a token.  At the rate of a copy: 4096
+// tokens of 8 rows of 2048 bf16 (151 MB) 28.5 us, 5.3 TB/s.
 template <bool F32> __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     const int per_row = (int)(a.d / 8);
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
