@@ -11,7 +11,7 @@
 // lane's own keys and two reductions over the group (largest key, lowest expert that has it) in DPP steps.
 // Long batches are bound by the vector ALU: 16384 tokens, 256 experts, sigmoid and bias, 8 of 4 groups of 8: 16 us (21 with the keys of
 // all groups in every round and the groups read in step, from the same banks), half the time with k = 1; 17 MB would take 3.3.  Short ones
-// by latency: 331 tokens 8.5 us.  The order of the rows is a second launch (5 to 9 us), whose blocks each need the counts of all.
+// by latency: 331 tokens 6.6 us.  The order of the rows is a second launch (5 to 9 us), whose blocks each need the counts of all.
 #include "ssg_device.h"
 #include "ssg_internal.h"
 
@@ -19,8 +19,9 @@ namespace ssg {
 
 namespace {
 
-constexpr int kOneLaunch = 64;                            // tokens that one block chooses for and sorts
-constexpr int kBlock = 1024;                              // threads of the kernels that choose and sort
+constexpr int kOneLaunch = 16;                            // tokens that one block chooses for and sorts
+constexpr int kBlock = 1024;                              // threads of a block that sorts, and the most of one that chooses
+constexpr int kLeast = 256;                               // the fewest of one that chooses
 constexpr int kWaves = kBlock / 64;
 
 // float -> integer in the same order; -0 counts as +0
@@ -269,6 +270,7 @@ __device__ __forceinline__ void scatter(const RouteArgs &a, const SortLds &s, in
         } else if (at < last) {
             a.place[at] = -1;
         }
+        if (base + kBlock >= last) break;
         __syncthreads();
         for (int x = tid; x < a.E; x += kBlock) {
             uint32_t n = 0;
@@ -297,20 +299,19 @@ __device__ __forceinline__ SortLds sort_lds(uint32_t *lds, int E) { return SortL
 // Counts of a block: at most its tokens, since a token takes an expert once; 16 bits each, rows of 16 bytes.
 __host__ __device__ constexpr int hist_stride(int E) { return (E + 7) & ~7; }
 
-// One block per a.block_tokens tokens.  With one block in all it sorts too; otherwise it leaves its experts' counts.
+// One block per a.block_tokens tokens.  With one block in all it sorts too (and has kBlock threads); otherwise it leaves its experts' counts.
 template <int LPT, int VPL, bool BF16> __global__ __launch_bounds__(kBlock) void route_kernel(RouteArgs a) {
     extern __shared__ uint32_t lds[];
     __shared__ uint32_t wave_sum[kWaves];
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, threads = blockDim.x;
     uint32_t *hist = lds;                                  // = the totals of the sort
     if (a.place)
-        for (int e = tid; e < a.E; e += kBlock) hist[e] = 0;
+        for (int e = tid; e < a.E; e += threads) hist[e] = 0;
     __syncthreads();
     uint32_t *keys = lds + a.lds_keys + (size_t)(tid / LPT) * a.key_stride;
     const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
     const int64_t t1 = t0 + a.block_tokens < a.T ? t0 + a.block_tokens : a.T;
-    constexpr int kAtOnce = kBlock / LPT;
-    for (int64_t t = t0 + tid / LPT; t - tid / LPT < t1; t += kAtOnce) {
+    for (int64_t t = t0 + tid / LPT; t - tid / LPT < t1; t += threads / LPT) {
         const int64_t wave_first = t - (tid & 63) / LPT;
         if (wave_first >= t1) continue;                    // the whole wave is beyond
         int id;
@@ -327,7 +328,7 @@ template <int LPT, int VPL, bool BF16> __global__ __launch_bounds__(kBlock) void
     __syncthreads();                                       // (also: this block's ids are visible to it)
     if (gridDim.x > 1) {
         const int stride = hist_stride(a.E);
-        for (int e = tid; e < stride; e += kBlock) a.hist[(size_t)blockIdx.x * stride + e] = (uint16_t)(e < a.E ? hist[e] : 0);
+        for (int e = tid; e < stride; e += threads) a.hist[(size_t)blockIdx.x * stride + e] = (uint16_t)(e < a.E ? hist[e] : 0);
         return;
     }
     const SortLds s = sort_lds(lds, a.E);
@@ -494,32 +495,47 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
 
 // ---- the weighted sum of the experts' rows -------------------------------------------------------------------
 // y[t] = sum_j w[t,j] o[place[t,j]], in the order of j, in fp32.  A thread owns 8 columns of a token.  At the rate of a copy: 4096
-// tokens of 8 rows of 2048 bf16 (151 MB) 28.5 us, 5.3 TB/s.
-template <bool F32> __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
+// tokens of 8 rows of 2048 bf16 (151 MB) 23.8 us, 6.3 TB/s, part of them still in the memory-side cache.
+template <bool F32, int AT_ONCE> __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     const int per_row = (int)(a.d / 8);
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= a.T * per_row) return;
     const int64_t t = i / per_row;
     const int64_t c = (i - t * per_row) * 8;
     float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll 4
-    for (int j = 0; j < a.k; ++j) {
-        const int row = a.place[t * a.k + j];
-        if (row < 0) continue;
-        const float w = a.weights[t * a.k + j];
-        float v[8];
-        if (F32) {
-            const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(a.o) + (int64_t)row * a.d + c);
-            const float4 x = p[0], y = p[1];
-            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-        } else {
-            const uint4 x = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.o) + (int64_t)row * a.d + c);
-            const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+    // AT_ONCE rows are on their way together; one that there is not is the first row, and left out of the sum
+    for (int j0 = 0; j0 < a.k; j0 += AT_ONCE) {
+        int row[AT_ONCE];
+        float w[AT_ONCE];
+        uint4 x[AT_ONCE][F32 ? 2 : 1];
 #pragma unroll
-            for (int b = 0; b < 4; ++b) { v[2 * b] = __uint_as_float(u[b] << 16); v[2 * b + 1] = __uint_as_float(u[b] & 0xffff0000u); }
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int j = j0 + u < a.k ? j0 + u : a.k - 1;
+            row[u] = a.place[t * a.k + j];
+            w[u] = a.weights[t * a.k + j];
+            if (j0 + u >= a.k) row[u] = -1;
         }
 #pragma unroll
-        for (int b = 0; b < 8; ++b) acc[b] = __fmaf_rn(w, v[b], acc[b]);
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(a.o) + ((int64_t)(row[u] < 0 ? 0 : row[u]) * a.d + c) * (F32 ? 4 : 2));
+#pragma unroll
+            for (int b = 0; b < (F32 ? 2 : 1); ++b) x[u][b] = p[b];
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            float v[8];
+#pragma unroll
+            for (int b = 0; b < (F32 ? 2 : 1); ++b) {
+                const uint32_t words[4] = {x[u][b].x, x[u][b].y, x[u][b].z, x[u][b].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (F32) v[4 * b + q] = __uint_as_float(words[q]);
+                    else { v[2 * q] = __uint_as_float(words[q] << 16); v[2 * q + 1] = __uint_as_float(words[q] & 0xffff0000u); }
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < 8; ++b) acc[b] = row[u] < 0 ? acc[b] : __fmaf_rn(w[u], v[b], acc[b]);
+        }
     }
     if (F32) {
         float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(a.y) + t * a.d + c);
@@ -533,7 +549,7 @@ template <bool F32> __global__ __launch_bounds__(256) void combine_kernel(Combin
 
 // Tokens to a block, so that there are at most 256 blocks and 64 K counts (which every block of the second launch reads).
 int most_blocks(int E) { return std::min(256, 65536 / E); }
-struct RoutePlan { int lpt, vpl, block_tokens, blocks; };
+struct RoutePlan { int lpt, vpl, block_tokens, blocks, threads; };
 RoutePlan route_plan(const RouteArgs &a) {
     RoutePlan p;
     // 16 lanes to a token choose for four tokens in one wave, which bounds long batches; 64 where the experts, their groups or k need
@@ -541,17 +557,23 @@ RoutePlan route_plan(const RouteArgs &a) {
     p.lpt = a.E > 256 || a.k > 16 || a.groups > 16 || a.T <= 4096 ? 64 : 16;
     p.vpl = 1;
     while (p.vpl * p.lpt < a.E) p.vpl *= 2;
-    const int64_t pass = kBlock / p.lpt, most = most_blocks(a.E);
-    // one block chooses for and sorts what one launch can take: a second one costs more than its passes
-    const int64_t tokens = a.T <= kOneLaunch ? a.T : (a.T + most - 1) / most;
+    // One block chooses and sorts what it can take at once (64 tokens in four passes took 26 us, in two launches 17 with the events around
+    // them).  Otherwise as many blocks as there may be, so that a compute unit has few waves that choose.
+    const bool one = a.place && a.T <= kOneLaunch;
+    const int64_t tokens = one ? a.T : (a.T + most_blocks(a.E) - 1) / most_blocks(a.E);
+    const int64_t least = kLeast / p.lpt, most = kBlock / p.lpt;
+    if (one) p.threads = kBlock;
+    else p.threads = (int)std::min(std::max(tokens, least), most) * p.lpt;
+    p.threads = (p.threads + 63) / 64 * 64;
+    const int64_t pass = p.threads / p.lpt;
     p.block_tokens = (int)((tokens + pass - 1) / pass * pass);
     p.blocks = (int)((a.T + p.block_tokens - 1) / p.block_tokens);
     return p;
 }
 
-template <int LPT, int VPL> void launch_route_as(const RouteArgs &a, int blocks, size_t lds, hipStream_t st) {
-    if (a.bf16) hipLaunchKernelGGL((route_kernel<LPT, VPL, true>), dim3(blocks), dim3(kBlock), lds, st, a);
-    else hipLaunchKernelGGL((route_kernel<LPT, VPL, false>), dim3(blocks), dim3(kBlock), lds, st, a);
+template <int LPT, int VPL> void launch_route_as(const RouteArgs &a, const RoutePlan &p, size_t lds, hipStream_t st) {
+    if (a.bf16) hipLaunchKernelGGL((route_kernel<LPT, VPL, true>), dim3(p.blocks), dim3(p.threads), lds, st, a);
+    else hipLaunchKernelGGL((route_kernel<LPT, VPL, false>), dim3(p.blocks), dim3(p.threads), lds, st, a);
 }
 
 // T = 0: no expert has a row
@@ -582,26 +604,26 @@ void launch_route(RouteArgs a, hipStream_t st) {
     a.lds_keys = a.E;
     // (with groups a token's keys and where its groups that stay begin; the tokens of a wave 16 banks apart)
     a.key_stride = (a.E + a.groups + 47) / 64 * 64 + 16;
-    const size_t key_words = a.E + (grouped ? (size_t)kBlock / p.lpt * a.key_stride : 0);
+    const size_t key_words = a.E + (grouped ? (size_t)p.threads / p.lpt * a.key_stride : 0);
     const size_t words = a.place && p.blocks == 1 ? std::max(sort_words, key_words) : key_words;
     const double bytes = (double)a.T * a.E * (a.bf16 ? 2 : 4) + 8.0 * a.T * a.k;
     profile_before(kTagRoute, st, bytes);
     const size_t lds = words * 4;
     if (p.lpt == 16) {
         switch (p.vpl) {
-            case 1: launch_route_as<16, 1>(a, p.blocks, lds, st); break;
-            case 2: launch_route_as<16, 2>(a, p.blocks, lds, st); break;
-            case 4: launch_route_as<16, 4>(a, p.blocks, lds, st); break;
-            case 8: launch_route_as<16, 8>(a, p.blocks, lds, st); break;
-            default: launch_route_as<16, 16>(a, p.blocks, lds, st); break;
+            case 1: launch_route_as<16, 1>(a, p, lds, st); break;
+            case 2: launch_route_as<16, 2>(a, p, lds, st); break;
+            case 4: launch_route_as<16, 4>(a, p, lds, st); break;
+            case 8: launch_route_as<16, 8>(a, p, lds, st); break;
+            default: launch_route_as<16, 16>(a, p, lds, st); break;
         }
     } else {
         switch (p.vpl) {
-            case 1: launch_route_as<64, 1>(a, p.blocks, lds, st); break;
-            case 2: launch_route_as<64, 2>(a, p.blocks, lds, st); break;
-            case 4: launch_route_as<64, 4>(a, p.blocks, lds, st); break;
-            case 8: launch_route_as<64, 8>(a, p.blocks, lds, st); break;
-            default: launch_route_as<64, 16>(a, p.blocks, lds, st); break;
+            case 1: launch_route_as<64, 1>(a, p, lds, st); break;
+            case 2: launch_route_as<64, 2>(a, p, lds, st); break;
+            case 4: launch_route_as<64, 4>(a, p, lds, st); break;
+            case 8: launch_route_as<64, 8>(a, p, lds, st); break;
+            default: launch_route_as<64, 16>(a, p, lds, st); break;
         }
     }
     profile_after(st);
@@ -626,8 +648,17 @@ void launch_combine(const CombineArgs &a, hipStream_t st) {
     const int64_t blocks = (a.T * (a.d / 8) + 255) / 256;
     const double size = a.f32 ? 4 : 2;
     profile_before(kTagCombine, st, (a.k + 1.0) * size * a.T * a.d);
-    if (a.f32) hipLaunchKernelGGL(combine_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(combine_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    // as many rows at once as there are, up to 128 bytes a thread (k = 8: one at a time 29.4 us, eight 23.9; k = 2, 1041 tokens of 4096: two
+    // 7.0, eight 8.7)
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a); };
+    if (a.f32) {
+        if (a.k <= 2) go(combine_kernel<true, 2>);
+        else go(combine_kernel<true, 4>);
+    } else {
+        if (a.k <= 2) go(combine_kernel<false, 2>);
+        else if (a.k <= 4) go(combine_kernel<false, 4>);
+        else go(combine_kernel<false, 8>);
+    }
     profile_after(st);
 }
 
