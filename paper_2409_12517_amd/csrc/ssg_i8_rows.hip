@@ -14,10 +14,10 @@ namespace ssg {
 namespace {
 
 // Bound by memory: 4096 rows of 11008 bf16 (135 MB) 30 us, 4.5 TB/s; 4096 tokens of 2048 gathered into 32768 rows (17 MB read eight
-// times, out of the caches, 67 MB written) 28 us.  A block owns 8 rows, half of one of the layout's: thread t has row t % 8 and every (threads / 8)-th run of 16 codes, so
-// that a wave reads 8 rows x 128 elements and writes pieces of 128 bytes.  The first HELD runs of a thread stay in registers between the
+// times, out of the caches, 67 MB written) 28 us.  A block owns ROWS rows, up to half of a row of
+// the layout's blocks: thread t has row t % ROWS and every (threads / ROWS)-th run of 16 codes, so that with eight a wave reads 8 rows x 128
+// elements and writes pieces of 128 bytes.  The first HELD runs of a thread stay in registers between the
 // maximum and the codes; what a row has beyond them is read again, out of the L2.
-constexpr int kRows = 8;
 // The list of row tiles, by one wave.
 __device__ __forceinline__ void list_tiles(const int *offsets, int E, int *list, int edge) {
     const int lane = threadIdx.x & 63;
@@ -40,16 +40,16 @@ __device__ __forceinline__ void list_tiles(const int *offsets, int E, int *list,
     if (lane == 0) *reinterpret_cast<int4 *>(list) = make_int4(before, 0, 0, 0);
 }
 
-template <bool BF16, int THREADS, int HELD> __global__ __launch_bounds__(THREADS) void i8_rows_kernel(I8RowsArgs a) {
-    constexpr int kCols = THREADS / kRows, kWaves = THREADS / 64;
-    __shared__ uint32_t maxima[kWaves][kRows];
-    const int tid = threadIdx.x, r = tid % kRows, c0 = tid / kRows;
-    const int64_t row = (int64_t)blockIdx.x * kRows + r;
+template <bool BF16, int THREADS, int HELD, int ROWS> __global__ __launch_bounds__(THREADS) void i8_rows_kernel(I8RowsArgs a) {
+    constexpr int kCols = THREADS / ROWS, kWaves = THREADS / 64;
+    __shared__ uint32_t maxima[kWaves][ROWS];
+    const int tid = threadIdx.x, r = tid % ROWS, c0 = tid / ROWS;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + r;
     if (a.E > 0 && blockIdx.x == gridDim.x - 1) {       // (the block behind those of the rows)
         if (tid < 128 && a.tiles[tid >> 6].edge) list_tiles(a.offsets, a.E, a.tiles[tid >> 6].list, a.tiles[tid >> 6].edge);
         return;
     }
-    if (a.live_rows && (int64_t)blockIdx.x * kRows >= *a.live_rows) return;
+    if (a.live_rows && (int64_t)blockIdx.x * ROWS >= *a.live_rows) return;
     int64_t from = row < a.rows ? row : -1;
     if (a.source && from >= 0) {
         const int s = a.source[row];
@@ -76,13 +76,13 @@ template <bool BF16, int THREADS, int HELD> __global__ __launch_bounds__(THREADS
     top = I8Run<BF16>::as_f32_bits(top);
     auto larger = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
 #pragma unroll
-    for (int d = kRows; d < 64; d *= 2) top = larger(top, (uint32_t)__shfl_xor((int)top, d, 64));
-    if ((tid & 63) < kRows) maxima[tid >> 6][r] = top;
+    for (int d = ROWS; d < 64; d *= 2) top = larger(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    if ((tid & 63) < ROWS) maxima[tid >> 6][r] = top;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) top = larger(top, maxima[i][r]);
     const I8Scale s = i8_scale(top);
-    if (tid < kRows) a.scales[row] = s.scale;
+    if (tid < ROWS) a.scales[row] = s.scale;
     uint8_t *out = a.codes + (row / 16 * padded * 16 + row % 16) * 16;
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
@@ -98,16 +98,24 @@ template <bool BF16, int THREADS, int HELD> __global__ __launch_bounds__(THREADS
     }
 }
 
-template <bool BF16> void launch_rows(const I8RowsArgs &a, hipStream_t st) {
-    const unsigned blocks = (unsigned)(i8_up(a.rows, 16) / kRows) + (a.E > 0);
+template <bool BF16, int ROWS> void launch_rows_as(const I8RowsArgs &a, hipStream_t st) {
+    const unsigned blocks = (unsigned)(i8_up(a.rows, 16) / ROWS) + (a.E > 0);
     const int runs = (int)(i8_width(a.K) / 16);
     // the smallest block whose registers hold the rows: 88 registers of values are 11 runs of bf16, 80 5 of fp32
     auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, st, a); };
-    constexpr int kFew = BF16 ? 4 : 2, kMost = BF16 ? 11 : 5;
-    if (runs <= 32 * kFew) go(i8_rows_kernel<BF16, 256, kFew>, 256);
-    else if (runs <= 32 * kMost) go(i8_rows_kernel<BF16, 256, kMost>, 256);
-    else if (runs <= 64 * kMost) go(i8_rows_kernel<BF16, 512, kMost>, 512);
-    else go(i8_rows_kernel<BF16, 1024, kMost>, 1024);
+    constexpr int kFew = BF16 ? 4 : 2, kMost = BF16 ? 11 : 5, kCols = 256 / ROWS;
+    if (runs <= kCols * kFew) go(i8_rows_kernel<BF16, 256, kFew, ROWS>, 256);
+    else if (runs <= kCols * kMost) go(i8_rows_kernel<BF16, 256, kMost, ROWS>, 256);
+    else if (runs <= 2 * kCols * kMost) go(i8_rows_kernel<BF16, 512, kMost, ROWS>, 512);
+    else go(i8_rows_kernel<BF16, 1024, kMost, ROWS>, 1024);
+}
+// Few rows in smaller blocks, so that they are more compute units' work (11008 bf16 a row, cold, with the events around the launch: 333 rows
+// 12.1 us in blocks of eight, 11.4 of four, 9.1 of two; 1024 rows of 4096 9.8, 7.4 and 7.7); many in blocks of eight, whose pieces fill cache
+// lines (4096 rows of 11008 37, 40 and 47).
+template <bool BF16> void launch_rows(const I8RowsArgs &a, hipStream_t st) {
+    if (a.rows <= 512) launch_rows_as<BF16, 2>(a, st);
+    else if (a.rows <= 2048) launch_rows_as<BF16, 4>(a, st);
+    else launch_rows_as<BF16, 8>(a, st);
 }
 
 // Row-major codes and scales into the layout and back, 16 bytes to a thread.
