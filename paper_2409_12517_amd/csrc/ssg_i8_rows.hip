@@ -16,7 +16,8 @@ namespace {
 // Bound by memory: 4096 rows of 11008 bf16 (135 MB) 30 us, 4.5 TB/s; 4096 tokens of 2048 gathered into 32768 rows (17 MB read eight
 // times, out of the caches, 67 MB written) 28 us.  A block owns ROWS rows, up to half of a row of
 // the layout's blocks: thread t has row t % ROWS and every (threads / ROWS)-th run of 16 codes, so that with eight a wave reads 8 rows x 128
-// elements and writes pieces of 128 bytes.  The first HELD runs of a thread stay in registers between the
+// elements and writes pieces of 128 bytes; at most 128 registers, since one more halves the blocks on a compute unit (2304 rows of 11008
+// 25 us, 30 then).  The first HELD runs of a thread stay in registers between the
 // maximum and the codes; what a row has beyond them is read again, out of the L2.
 // The list of row tiles, by one wave.
 __device__ __forceinline__ void list_tiles(const int *offsets, int E, int *list, int edge) {
@@ -40,7 +41,7 @@ __device__ __forceinline__ void list_tiles(const int *offsets, int E, int *list,
     if (lane == 0) *reinterpret_cast<int4 *>(list) = make_int4(before, 0, 0, 0);
 }
 
-template <bool BF16, int THREADS, int HELD, int ROWS> __global__ __launch_bounds__(THREADS) void i8_rows_kernel(I8RowsArgs a) {
+template <bool BF16, int THREADS, int HELD, int ROWS> __global__ __launch_bounds__(THREADS, 4) void i8_rows_kernel(I8RowsArgs a) {
     constexpr int kCols = THREADS / ROWS, kWaves = THREADS / 64;
     __shared__ uint32_t maxima[kWaves][ROWS];
     const int tid = threadIdx.x, r = tid % ROWS, c0 = tid / ROWS;
@@ -110,11 +111,11 @@ template <bool BF16, int ROWS> void launch_rows_as(const I8RowsArgs &a, hipStrea
     else go(i8_rows_kernel<BF16, 1024, kMost, ROWS>, 1024);
 }
 // Few rows in smaller blocks, so that they are more compute units' work (11008 bf16 a row, cold, with the events around the launch: 333 rows
-// 12.1 us in blocks of eight, 11.4 of four, 9.1 of two; 1024 rows of 4096 9.8, 7.4 and 7.7); many in blocks of eight, whose pieces fill cache
-// lines (4096 rows of 11008 37, 40 and 47).
+// 12.1 us in blocks of eight, 11.4 of four, 9.1 of two; 2304 rows of 4096 12.7, 10.2 and 11.1); many in blocks of eight, whose pieces fill cache
+// lines (4096 rows of 11008 34, 37 and 46).
 template <bool BF16> void launch_rows(const I8RowsArgs &a, hipStream_t st) {
     if (a.rows <= 512) launch_rows_as<BF16, 2>(a, st);
-    else if (a.rows <= 2048) launch_rows_as<BF16, 4>(a, st);
+    else if (a.rows <= 2560) launch_rows_as<BF16, 4>(a, st);
     else launch_rows_as<BF16, 8>(a, st);
 }
 
