@@ -20,6 +20,13 @@ if not os.path.exists(LIB_PATH):
         f"{LIB_PATH} is missing: build it with `python paper_2409_12517_amd/build.py` "
         "(hipcc, --offload-arch=gfx950). There is no CPU fallback.")
 
+# torch brings a HIP runtime of its own.  Loaded after it the library takes that one; loaded before it, it would bring in the installed
+# one, and the process would have two, of which the library's sees no device.
+try:
+    import torch  # noqa: F401
+except ImportError:
+    pass                       # (without torch there is one runtime, and pointers are passed as integers)
+
 _lib = ctypes.CDLL(LIB_PATH)
 
 # enums of ssg.h
