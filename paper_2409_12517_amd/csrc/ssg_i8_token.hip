@@ -17,7 +17,6 @@ namespace ssg {
 namespace {
 
 typedef int v4i_t __attribute__((ext_vector_type(4)));
-constexpr int kRows = kTokenRows;
 constexpr int kAtOnce = 8;                     // steps of 64 whose weights a wave loads before it multiplies
 
 // The products of this wave's steps [k0, k1) of 64 along K: weights from `b` (1 KB a step), codes of lane l & 15's row from LDS at
@@ -45,11 +44,11 @@ template <int NB> struct Stream {
     }
 };
 
-template <bool BF16, bool DUAL, int WAVES> __global__ __launch_bounds__(64 * WAVES) void i8_token_kernel(I8TokenArgs a) {
+template <bool BF16, bool DUAL, int WAVES, int ROWS> __global__ __launch_bounds__(64 * WAVES) void i8_token_kernel(I8TokenArgs a) {
     constexpr int NB = DUAL ? 2 : 1, kThreads = 64 * WAVES;
     extern __shared__ __attribute__((aligned(16))) uint8_t codes[];          // rows of Kp
     __shared__ v4i_t part[WAVES][NB][64];
-    __shared__ uint32_t maxima[WAVES][kRows];
+    __shared__ uint32_t maxima[WAVES][ROWS];
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col_blocks = (int)(a.N / 16), KB = (int)(i8_width(a.K) / 64), Kp = KB * 64;
     const int pair = a.ids ? blockIdx.x / col_blocks : 0, cb = blockIdx.x % col_blocks;
@@ -67,15 +66,15 @@ template <bool BF16, bool DUAL, int WAVES> __global__ __launch_bounds__(64 * WAV
     const int runs = (int)(a.K / 16), padded = Kp / 16;
     const uint8_t *src = static_cast<const uint8_t *>(a.src) + from * a.ld * (BF16 ? 2 : 4);
     const int64_t row_bytes = a.ld * (BF16 ? 2 : 4);
-    uint32_t top[kRows] = {};
-    I8Run<BF16> held[kRows];                            // this thread's first run of each row
+    uint32_t top[ROWS] = {};
+    I8Run<BF16> held[ROWS];                            // this thread's first run of each row
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
+    for (int r = 0; r < ROWS; ++r) {
         held[r].clear();
         if (r < a.rows && tid < runs) held[r].load(src + r * row_bytes, tid);
     }
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
+    for (int r = 0; r < ROWS; ++r) {
         top[r] = held[r].max_bits(0);
         if (r < a.rows)
             for (int c = tid + kThreads; c < runs; c += kThreads) {
@@ -87,9 +86,9 @@ template <bool BF16, bool DUAL, int WAVES> __global__ __launch_bounds__(64 * WAV
         if (l == 0) maxima[w][r] = top[r];
     }
     __syncthreads();
-    float scale[kRows];
+    float scale[ROWS];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
+    for (int r = 0; r < ROWS; ++r) {
         uint32_t m = 0;
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) m = m > maxima[i][r] ? m : maxima[i][r];
@@ -130,7 +129,7 @@ template <bool BF16, bool DUAL, int WAVES> __global__ __launch_bounds__(64 * WAV
     const int64_t col = (int64_t)cb * 16 + (l >> 4) * 4, row = a.ids ? pair : l & 15;
     float sa = scale[0];
 #pragma unroll
-    for (int r = 1; r < kRows; ++r) sa = (l & 15) == r ? scale[r] : sa;
+    for (int r = 1; r < ROWS; ++r) sa = (l & 15) == r ? scale[r] : sa;
     const float4 s1 = *reinterpret_cast<const float4 *>(a.sb + (int64_t)expert * a.N + col);
     float v[4] = {(float)sum[0][0] * sa * s1.x, (float)sum[0][1] * sa * s1.y, (float)sum[0][2] * sa * s1.z, (float)sum[0][3] * sa * s1.w};
     if (DUAL) {
@@ -225,9 +224,15 @@ void launch_i8_token(const I8TokenArgs &a, hipStream_t st) {
     const unsigned lds = (unsigned)(a.rows * i8_width(a.K));
     profile_before(dual ? kTagI8Swiglu : kTagI8Gemm, st);
     // one matrix has few workgroups, which take more waves each
-    if (dual) hipLaunchKernelGGL((i8_token_kernel<true, true, 4>), dim3(blocks), dim3(256), lds, st, a);
-    else if (a.bf16) hipLaunchKernelGGL((i8_token_kernel<true, false, 8>), dim3(blocks), dim3(512), lds, st, a);
-    else hipLaunchKernelGGL((i8_token_kernel<false, false, 8>), dim3(blocks), dim3(512), lds, st, a);
+    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, st, a); };
+    auto rows = [&](auto count) {
+        constexpr int ROWS = decltype(count)::value;
+        if (a.bf16) go(i8_token_kernel<true, false, 8, ROWS>, 512);
+        else go(i8_token_kernel<false, false, 8, ROWS>, 512);
+    };
+    if (dual) go(i8_token_kernel<true, true, 4, 1>, 256);
+    else if (a.rows == 1) rows(std::integral_constant<int, 1>{});
+    else rows(std::integral_constant<int, kTokenRows>{});
     profile_after(st);
 }
 
@@ -239,7 +244,12 @@ static int mix_split(int k) {
 }
 static int64_t mix_lds(int64_t K, int k) { const int64_t KB = i8_width(K) / 64, s = mix_split(k); return kMixWaves * ((KB + s - 1) / s) * 64; }
 
-bool i8_token_ok(int64_t T, int64_t K) { return T <= kTokenRows && T * i8_width(K) <= kTokenLds; }
+// One token always.  More where every compute unit has one workgroup to quantize them for, and K enough that the launch saved is not spent
+// on it: 4 tokens, 4096 x 11008 14.7 us and 15.4 in two launches, 1040 x 2736 6.6 and 7.2; 2752 x 1024 6.5 and 6.0, 11008 x 4096 17.2 and 13.7
+// (2 tokens there 13.5 and 13.6, in fp32 18.7 and 14.1; 8 tokens of 4096 x 4096 11.0 and 8.5).
+bool i8_token_ok(int64_t T, int64_t N, int64_t K) {
+    return T * i8_width(K) <= kTokenLds && (T == 1 || (T <= kTokenRows && N <= 4096 && K >= 2048));
+}
 bool i8_mix_ok(int64_t T, int64_t d, int64_t f, int k) { return T <= kTokenRows && i8_width(d) <= kTokenLds && mix_lds(f, k) <= kMixLds; }
 
 void launch_i8_mix(I8MixArgs a, hipStream_t st) {

@@ -372,7 +372,7 @@ struct I8MixArgs {
     int k = 1, f32 = 0, split = 1;   // split: filled in by the launcher
 };
 void launch_i8_mix(I8MixArgs a, hipStream_t st);
-bool i8_token_ok(int64_t T, int64_t K);
+bool i8_token_ok(int64_t T, int64_t N, int64_t K);
 bool i8_mix_ok(int64_t T, int64_t d, int64_t f, int k);
 constexpr int kTagRoute = 48, kTagDispatch = 49, kTagRouteBwd = 50, kTagCombine = 51, kTagI8Rows = 52, kTagI8Gemm = 53, kTagI8Swiglu = 54;
 

@@ -282,7 +282,7 @@ ssg_status ssg_i8_linear(const void *x, ssg_dtype x_dtype, int64_t M, int64_t K,
     SSG_CHECK(check_i8_buffer(who, "W", W, W_bytes, N, K));
     SSG_CHECK(check_i8_buffer(who, "workspace", workspace, workspace_bytes, M, K));
     SSG_CHECK(check_entry(who));
-    if (ssg::i8_token_ok(M, K)) {
+    if (ssg::i8_token_ok(M, N, K)) {
         ssg::I8TokenArgs k;
         k.src = x; k.rows = (int)M; k.K = K; k.ld = ldx; k.bf16 = x_dtype == SSG_BF16;
         k.B = static_cast<const uint8_t *>(W); k.sb = i8_scales(W, N, K); k.C = y; k.N = N; k.ldc = ldy; k.c_f32 = y_dtype == SSG_F32;
