@@ -6,8 +6,8 @@
 //   i8_token_kernel   up to four rows by 16 columns of one matrix, or one row by 16 columns of the two matrices of the expert that
 //                     an assignment (token, choice) names, with the SwiGLU product; waves share K out
 //   i8_mix_kernel     16 columns of a token's result: its experts side by side, a few waves each, and their weighted sum
-// One token: 11008 x 4096 10.6 us, 4.2 TB/s (15.4 with the rows quantized in a launch before); 8 experts of d = 2048, f = 1376
-// 9.9 + 11.3 us for 45 + 23 MB (43 us a call in five launches, 27 in three).  What bounds them now is the start and the end of a single
+// One token: 11008 x 4096 9.4 us, 4.8 TB/s (13.6 in two launches); 8 experts of d = 2048, f = 1376 9 to 11 and 10.5 us for 45 and
+// 23 MB (43 us a call in five launches, 25 in three).  What bounds them now is the start and the end of a single
 // round of workgroups: x and the first weights from memory, two barriers, the sums in LDS.
 #include "ssg_gemm_tile.h"
 #include "ssg_i8.h"
@@ -21,13 +21,13 @@ constexpr int kAtOnce = 8;                     // steps of 64 whose weights a wa
 
 // The products of this wave's steps [k0, k1) of 64 along K: weights from `b` (1 KB a step), codes of lane l & 15's row from LDS at
 // `codes`, where step k0 lies first.  `first` holds the first kAtOnce steps' weights; beyond the end the last step again, times zero.
-template <int NB> struct Stream {
+template <int NB, int AT_ONCE> struct Stream {
     const uint8_t *b[NB];
     int k0, k1;
-    v4i_t w[kAtOnce][NB];
+    v4i_t w[AT_ONCE][NB];
     __device__ __forceinline__ void load(int k) {
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
+        for (int u = 0; u < AT_ONCE; ++u) {
             const int at = k + u < k1 ? k + u : (k1 > 0 ? k1 - 1 : 0);
 #pragma unroll
             for (int c = 0; c < NB; ++c) w[u][c] = __builtin_nontemporal_load(reinterpret_cast<const v4i_t *>(b[c] + (int64_t)at * 1024));
@@ -35,7 +35,7 @@ template <int NB> struct Stream {
     }
     __device__ __forceinline__ void multiply(int k, const uint8_t *codes, v4i_t (&acc)[NB]) {
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
+        for (int u = 0; u < AT_ONCE; ++u) {
             const bool in = k + u < k1;
             const v4i_t x = *reinterpret_cast<const v4i_t *>(codes + (in ? k + u - k0 : 0) * 64) & (in ? -1 : 0);
 #pragma unroll
@@ -56,7 +56,7 @@ template <bool BF16, bool DUAL, int WAVES, int ROWS> __global__ __launch_bounds_
     if (expert < 0) return;
     const int64_t from = a.ids ? pair / a.k : 0;
     const int share = (KB + WAVES - 1) / WAVES;
-    Stream<NB> s;
+    Stream<NB, kAtOnce> s;
     s.k0 = w * share < KB ? w * share : KB;
     s.k1 = s.k0 + share < KB ? s.k0 + share : KB;
 #pragma unroll
@@ -145,29 +145,37 @@ template <bool BF16, bool DUAL, int WAVES, int ROWS> __global__ __launch_bounds_
 }
 
 // y[t, 16 columns]: kMixWaves waves, `split` of them to an expert, each with a share of K; h row t k + j is the expert's input.
-constexpr int kMixWaves = 16;
+constexpr int kMixWaves = 16, kMixAtOnce = 12;        // (a share of f = 1376 is 11 steps; with 8 at once 12.3 us for 11.3, with 16 12.4)
 template <bool F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_kernel(I8MixArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t codes[];          // kMixWaves shares
     __shared__ v4i_t part[kMixWaves][4];
-    __shared__ float result[kMaxChosen][16];
+    __shared__ float result[kMaxChosen][16], weight[kMaxChosen];
+    __shared__ int chosen[kMaxChosen];
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col_blocks = (int)(a.N / 16), KB = (int)(i8_width(a.K) / 64);
     const int t = blockIdx.x / col_blocks, cb = blockIdx.x % col_blocks;
     const int split = a.split, share = (KB + split - 1) / split, at_once = kMixWaves / split;
     const int runs = (int)(a.K / 16);
     uint8_t *mine = codes + w * share * 64;
+    if (tid < a.k) {
+        chosen[tid] = a.ids[t * a.k + tid];
+        weight[tid] = a.weights[t * a.k + tid];
+    }
     for (int j0 = 0; j0 < a.k; j0 += at_once) {
         const int j = j0 + w / split;
         const int expert = w / split < at_once && j < a.k ? __builtin_amdgcn_readfirstlane(a.ids[t * a.k + j]) : -1;
         float scale = 0.0f;
         if (expert >= 0) {
-            Stream<1> s;
+            Stream<1, kMixAtOnce> s;
             s.k0 = w % split * share < KB ? w % split * share : KB;
             s.k1 = s.k0 + share < KB ? s.k0 + share : KB;
             s.b[0] = a.B + ((int64_t)expert * col_blocks + cb) * KB * 1024 + l * 16;
             s.load(s.k0);
             const uint8_t *src = static_cast<const uint8_t *>(a.h) + ((int64_t)t * a.k + j) * a.K * 2;
-            // the whole row's maximum in every wave, its own share's codes
+            // the whole row's maximum in every wave, its own share's codes, of which the first run of each lane stays
+            I8Run<true> held;
+            held.clear();
+            if (s.k0 * 4 + l < s.k1 * 4 && s.k0 * 4 + l < runs) held.load(src, s.k0 * 4 + l);
             uint32_t top = 0;
             for (int c = l; c < runs; c += 64) {
                 I8Run<true> run;
@@ -176,7 +184,9 @@ template <bool F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_ker
             }
             const I8Scale q = i8_scale(wave_max_u32(I8Run<true>::as_f32_bits(top)));
             scale = q.scale;
-            for (int c = s.k0 * 4 + l; c < s.k1 * 4; c += 64) {
+            held.opaque();
+            if (s.k0 * 4 + l < s.k1 * 4) *reinterpret_cast<uint4 *>(mine + l * 16) = held.codes(q.factor);
+            for (int c = s.k0 * 4 + l + 64; c < s.k1 * 4; c += 64) {
                 I8Run<true> run;
                 run.clear();
                 if (c < runs) run.load(src, c);
@@ -188,7 +198,7 @@ template <bool F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_ker
             const uint8_t *x = mine + (l >> 4) * 16;    // (all 16 rows the same: only one is used)
             if (s.k0 < s.k1) {
                 s.multiply(s.k0, x, acc);
-                for (int k = s.k0 + kAtOnce; k < s.k1; k += kAtOnce) {
+                for (int k = s.k0 + kMixAtOnce; k < s.k1; k += kMixAtOnce) {
                     s.load(k);
                     s.multiply(k, x, acc);
                 }
@@ -210,7 +220,7 @@ template <bool F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_ker
     if (tid >= 16) return;
     float y = 0.0f;
     for (int j = 0; j < a.k; ++j)
-        if (a.ids[t * a.k + j] >= 0) y = __fmaf_rn(a.weights[t * a.k + j], result[j][tid], y);
+        if (chosen[j] >= 0) y = __fmaf_rn(weight[j], result[j][tid], y);
     const int64_t at = (int64_t)t * a.N + cb * 16 + tid;
     if (F32) static_cast<float *>(a.y)[at] = y;
     else static_cast<uint16_t *>(a.y)[at] = (uint16_t)f32_to_bf16_bits(y);
