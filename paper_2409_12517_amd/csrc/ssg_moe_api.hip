@@ -392,7 +392,7 @@ ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logi
     hq.rows = L.rows; hq.K = f; hq.ld = f; hq.bf16 = 1; hq.live_rows = a.offsets + E;
 
     // the experts' results, in y's type: bf16 is half the bytes for the product to write and the sum to read (23.8 us at 4096 tokens of 8
-    // rows of 2048); y is then 2.3e-3 to 2.5e-3 from the sums in 64 bits, 1.6e-3 to 1.9e-3 in a plain form that keeps results in fp32
+    // rows of 2048); y is then 2.3e-3 to 2.9e-3 from the sums in 64 bits, 1.6e-3 to 2.4e-3 in a plain form that keeps results in fp32
     ssg::I8GemmArgs o = g;
     o.A = hq.codes; o.sa = hq.scales; o.B = static_cast<const uint8_t *>(W3); o.sb = i8_scales(W3, E * d, f); o.B2 = nullptr; o.sb2 = nullptr;
     o.C = b + L.o; o.N = d; o.K = f; o.ldc = d; o.c_f32 = desc->y_dtype == SSG_F32;
