@@ -433,15 +433,18 @@ ssg_status ssg_i8_linear(const void *x, ssg_dtype x_dtype, int64_t M, int64_t K,
                          void *y, ssg_dtype y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
 
 /* The mixture's forward: routing, then with every expert's own W1, W2 [f,d] and W3 [d,f] in 8-bit integers
- *     h = (x w1)(Swish(x w2)) in bf16, quantized with a scale for each token;  o = h w3^T in y's type
- *     y_t = sum_j weights[t,j] o[place[t,j]]  in fp32, in the order of j
+ *     h = (x w1)(Swish(x w2)) in bf16, quantized with a scale for each token;  o = h w3^T
+ *     y_t = sum_j weights[t,j] o[place[t,j]]  in fp32, in the order of j, rounded to y's type
+ * o is rounded to y's type before the sum, or stays in fp32 with f32_terms = 1: a bf16 y then holds one rounding to bf16 and not two, for
+ * twice the bytes of o in the workspace, written and read (fp32 y: no difference).
  * W1, W2: buffers of E*f rows of K = d, expert e's rows from e*f; W3: E*d rows of K = f.  x [T,d] bf16; y [T,d] of y_dtype.  d, f
  * multiples of 16.  A token without an open expert gets zeros.  Inference only: the integer products have no gradient. */
 typedef struct {
     ssg_route_desc route;    /* row_align must be 16 */
     int64_t d, f;
     int32_t y_dtype;
-    int32_t reserved[3];     /* must be 0 */
+    int32_t f32_terms;       /* 0 or 1 */
+    int32_t reserved[2];     /* must be 0 */
 } ssg_moe_desc;
 size_t ssg_moe_workspace_bytes(const ssg_moe_desc *desc);
 ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logits, const float *bias, const void *W1, size_t W1_bytes,
@@ -456,7 +459,7 @@ typedef struct {
     const int32_t *counts, *offsets, *place, *source;
     const void *x_q, *h_q;               /* quantized rows of K = d and K = f */
     const void *h;                       /* bf16 [rows, f] */
-    const void *o;                       /* [rows, d] of y_dtype */
+    const void *o;                       /* [rows, d] of y_dtype, of fp32 with f32_terms */
 } ssg_moe_workspace_view;
 ssg_status ssg_moe_view_workspace(const ssg_moe_desc *desc, const void *workspace, ssg_moe_workspace_view *out);
 

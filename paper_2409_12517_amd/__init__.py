@@ -93,7 +93,7 @@ class ssg_route_desc(Structure):
 
 
 class ssg_moe_desc(Structure):
-    _fields_ = [("route", ssg_route_desc), ("d", c_int64), ("f", c_int64), ("y_dtype", c_int32), ("reserved", c_int32 * 3)]
+    _fields_ = [("route", ssg_route_desc), ("d", c_int64), ("f", c_int64), ("y_dtype", c_int32), ("f32_terms", c_int32), ("reserved", c_int32 * 2)]
 
 
 class ssg_moe_workspace_view(Structure):
@@ -492,8 +492,8 @@ def ssg_i8_linear(x, x_dtype, M, K, ldx, W, N, y, y_dtype, ldy, workspace, strea
                               _nbytes(workspace, workspace_bytes), _stream(stream)))
 
 
-def make_moe_desc(route: ssg_route_desc, d: int, f: int, y_dtype: int = SSG_BF16) -> ssg_moe_desc:
-    return ssg_moe_desc(route, d, f, y_dtype, (c_int32 * 3)(0, 0, 0))
+def make_moe_desc(route: ssg_route_desc, d: int, f: int, y_dtype: int = SSG_BF16, f32_terms: int = 0) -> ssg_moe_desc:
+    return ssg_moe_desc(route, d, f, y_dtype, f32_terms, (c_int32 * 2)(0, 0))
 
 
 def ssg_moe_workspace_bytes(desc) -> int:

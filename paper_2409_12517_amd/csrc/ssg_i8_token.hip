@@ -146,7 +146,7 @@ template <bool BF16, bool DUAL, int WAVES, int ROWS> __global__ __launch_bounds_
 
 // y[t, 16 columns]: kMixWaves waves, `split` of them to an expert, each with a share of K; h row t k + j is the expert's input.
 constexpr int kMixWaves = 16, kMixAtOnce = 12;        // (a share of f = 1376 is 11 steps; with 8 at once 12.3 us for 11.3, with 16 12.4)
-template <bool F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_kernel(I8MixArgs a) {
+template <bool O_F32, bool Y_F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_kernel(I8MixArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t codes[];          // kMixWaves shares
     __shared__ v4i_t part[kMixWaves][4];
     __shared__ float result[kMaxChosen][16], weight[kMaxChosen];
@@ -212,8 +212,8 @@ template <bool F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_ker
             const float4 sb = *reinterpret_cast<const float4 *>(a.sb + (int64_t)expert * a.N + cb * 16 + (l >> 4) * 4);
             float v[4] = {(float)sum[0] * scale * sb.x, (float)sum[1] * scale * sb.y, (float)sum[2] * scale * sb.z, (float)sum[3] * scale * sb.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i)                 // in y's type, as it is where it goes through memory
-                result[j][(l >> 4) * 4 + i] = F32 ? v[i] : bf16_bits_to_f32(f32_to_bf16_bits(v[i]));
+            for (int i = 0; i < 4; ++i)                 // in the type that it has where it goes through memory: a token's bits do not depend on its batch
+                result[j][(l >> 4) * 4 + i] = O_F32 ? v[i] : bf16_bits_to_f32(f32_to_bf16_bits(v[i]));
         }
         __syncthreads();
     }
@@ -222,7 +222,7 @@ template <bool F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_ker
     for (int j = 0; j < a.k; ++j)
         if (chosen[j] >= 0) y = __fmaf_rn(weight[j], result[j][tid], y);
     const int64_t at = (int64_t)t * a.N + cb * 16 + tid;
-    if (F32) static_cast<float *>(a.y)[at] = y;
+    if (Y_F32) static_cast<float *>(a.y)[at] = y;
     else static_cast<uint16_t *>(a.y)[at] = (uint16_t)f32_to_bf16_bits(y);
 }
 
@@ -266,8 +266,10 @@ void launch_i8_mix(I8MixArgs a, hipStream_t st) {
     a.split = mix_split(a.k);
     const unsigned blocks = (unsigned)(a.T * (a.N / 16)), lds = (unsigned)mix_lds(a.K, a.k);
     profile_before(kTagI8Gemm, st);
-    if (a.f32) hipLaunchKernelGGL(i8_mix_kernel<true>, dim3(blocks), dim3(64 * kMixWaves), lds, st, a);
-    else hipLaunchKernelGGL(i8_mix_kernel<false>, dim3(blocks), dim3(64 * kMixWaves), lds, st, a);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64 * kMixWaves), lds, st, a); };
+    if (a.y_f32) go(i8_mix_kernel<true, true>);
+    else if (a.o_f32) go(i8_mix_kernel<true, false>);
+    else go(i8_mix_kernel<false, false>);
     profile_after(st);
 }
 

@@ -287,12 +287,12 @@ struct RouteBwdArgs {
     float scale = 1.0f;
 };
 struct CombineArgs {
-    const void *o = nullptr;         // rows of d, fp32 (f32 = 1) or bf16
-    void *y = nullptr;               // [T, d] of the same type
+    const void *o = nullptr;         // rows of d, fp32 (o_f32 = 1) or bf16
+    void *y = nullptr;               // [T, d], fp32 (y_f32 = 1, with o_f32 = 1 only) or bf16
     const int *place = nullptr;      // [T, k]
     const float *weights = nullptr;
     int64_t T = 0, d = 0;
-    int k = 0, f32 = 0;
+    int k = 0, o_f32 = 0, y_f32 = 0;
 };
 constexpr int kMaxExperts = 1024, kMaxChosen = 32, kMaxGroups = 64;
 constexpr int64_t kMaxTokens = ((int64_t)1 << 22) - 1024;     // a block of 64 for 1024 experts counts them in 16 bits
@@ -367,9 +367,11 @@ struct I8MixArgs {
     const float *sb = nullptr;
     const int *ids = nullptr;        // [T, k]
     const float *weights = nullptr;
-    void *y = nullptr;               // [T, N], fp32 (f32 = 1) or bf16
+    void *y = nullptr;               // [T, N], fp32 (y_f32 = 1) or bf16
     int64_t T = 0, N = 0, K = 0;
-    int k = 1, f32 = 0, split = 1;   // split: filled in by the launcher
+    int k = 1, y_f32 = 0;
+    int o_f32 = 0;                   // experts' results stay in fp32; 0, with bf16 y only: they are rounded to bf16
+    int split = 1;                   // filled in by the launcher
 };
 void launch_i8_mix(I8MixArgs a, hipStream_t st);
 bool i8_token_ok(int64_t T, int64_t N, int64_t K);

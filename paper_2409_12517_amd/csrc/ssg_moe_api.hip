@@ -91,6 +91,9 @@ ssg_status check_i8_product(const char *who, int64_t rows, int64_t experts, int6
     return SSG_OK;
 }
 
+// whether the experts' results, the terms of the weighted sum, are fp32
+bool f32_results(const ssg_moe_desc &d) { return d.y_dtype == SSG_F32 || d.f32_terms; }
+
 struct MoeLayout { size_t ids, weights, counts, offsets, place, source, hist, tiles, x_q, h, h_q, o, total; int64_t rows; };
 // words of a list of row tiles, whichever products run (no tile has fewer than 16 rows)
 size_t moe_list_words(int64_t rows) { return (ssg::i8_tile_list_words(rows / 16) + 63) / 64 * 64; }
@@ -107,7 +110,7 @@ MoeLayout moe_layout(const ssg_moe_desc &d) {
     L.x_q = take(i8_bytes(L.rows, d.d));
     L.h = take((size_t)L.rows * d.f * 2);
     L.h_q = take(i8_bytes(L.rows, d.f));
-    L.o = take((size_t)L.rows * d.d * (d.y_dtype == SSG_F32 ? 4 : 2));
+    L.o = take((size_t)L.rows * d.d * (f32_results(d) ? 4 : 2));
     L.total = o;
     return L;
 }
@@ -120,6 +123,7 @@ ssg_status check_moe(const ssg_moe_desc *d, const char *who) {
     SSG_CHECK(check_route(&d->route, who));
     if (d->route.row_align != kI8Align) return fail(SSG_ERR_ARG, "%s: route.row_align %d (the products take %d)", who, d->route.row_align, kI8Align);
     if (!dtype_ok(d->y_dtype)) return fail(SSG_ERR_ARG, "%s: y_dtype %d", who, d->y_dtype);
+    if (d->f32_terms != 0 && d->f32_terms != 1) return fail(SSG_ERR_ARG, "%s: f32_terms %d (0 or 1)", who, d->f32_terms);
     for (int r : d->reserved)
         if (r) return fail(SSG_ERR_ARG, "%s: reserved fields must be zero", who);
     const int64_t rows = route_rows(d->route);
@@ -369,7 +373,7 @@ ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logi
         ssg::launch_i8_token(u, st);
         ssg::I8MixArgs m;
         m.h = b + L.h; m.B = static_cast<const uint8_t *>(W3); m.sb = i8_scales(W3, E * d, f); m.ids = a.ids; m.weights = a.weights;
-        m.y = y; m.T = r.T; m.N = d; m.K = f; m.k = r.k; m.f32 = desc->y_dtype == SSG_F32;
+        m.y = y; m.T = r.T; m.N = d; m.K = f; m.k = r.k; m.y_f32 = desc->y_dtype == SSG_F32; m.o_f32 = f32_results(*desc);
         ssg::launch_i8_mix(m, st);
         return check_launch(who);
     }
@@ -391,11 +395,11 @@ ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logi
     hq.src = b + L.h; hq.codes = b + L.h_q; hq.scales = const_cast<float *>(i8_scales(b + L.h_q, L.rows, f));
     hq.rows = L.rows; hq.K = f; hq.ld = f; hq.bf16 = 1; hq.live_rows = a.offsets + E;
 
-    // the experts' results, in y's type: bf16 is half the bytes for the product to write and the sum to read (23.8 us at 4096 tokens of 8
-    // rows of 2048); y is then 2.3e-3 to 2.9e-3 from the sums in 64 bits, 1.6e-3 to 2.4e-3 in a plain form that keeps results in fp32
+    // the experts' results, in y's type unless the caller wants them in fp32: bf16 is half the bytes for the product to write and the sum to
+    // read (23.8 us at 4096 tokens of 8 rows of 2048); y is then 2.3e-3 to 2.9e-3 from the sums in 64 bits, 1.6e-3 to 2.4e-3 with fp32 terms
     ssg::I8GemmArgs o = g;
     o.A = hq.codes; o.sa = hq.scales; o.B = static_cast<const uint8_t *>(W3); o.sb = i8_scales(W3, E * d, f); o.B2 = nullptr; o.sb2 = nullptr;
-    o.C = b + L.o; o.N = d; o.K = f; o.ldc = d; o.c_f32 = desc->y_dtype == SSG_F32;
+    o.C = b + L.o; o.N = d; o.K = f; o.ldc = d; o.c_f32 = f32_results(*desc);
 
     // the launch that quantizes x lists the row tiles of both products on the side
     int *lists = reinterpret_cast<int *>(b + L.tiles);
@@ -411,7 +415,7 @@ ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logi
     ssg::launch_i8_gemm(o, st);
 
     ssg::CombineArgs c;
-    c.o = b + L.o; c.y = y; c.place = a.place; c.weights = a.weights; c.T = r.T; c.d = d; c.k = r.k; c.f32 = desc->y_dtype == SSG_F32;
+    c.o = b + L.o; c.y = y; c.place = a.place; c.weights = a.weights; c.T = r.T; c.d = d; c.k = r.k; c.y_f32 = desc->y_dtype == SSG_F32; c.o_f32 = f32_results(*desc);
     ssg::launch_combine(c, st);
     return check_launch(who);
 }

@@ -496,7 +496,8 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
 // ---- the weighted sum of the experts' rows -------------------------------------------------------------------
 // y[t] = sum_j w[t,j] o[place[t,j]], in the order of j, in fp32.  A thread owns 8 columns of a token.  At the rate of a copy: 4096
 // tokens of 8 rows of 2048 bf16 (151 MB) 23.8 us, 6.3 TB/s, part of them still in the memory-side cache.
-template <bool F32, int AT_ONCE> __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
+// F32: the rows' type, Y_F32: y's.
+template <bool F32, bool Y_F32, int AT_ONCE> __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     const int per_row = (int)(a.d / 8);
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= a.T * per_row) return;
@@ -537,7 +538,7 @@ template <bool F32, int AT_ONCE> __global__ __launch_bounds__(256) void combine_
             for (int b = 0; b < 8; ++b) acc[b] = row[u] < 0 ? acc[b] : __fmaf_rn(w[u], v[b], acc[b]);
         }
     }
-    if (F32) {
+    if (Y_F32) {
         float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(a.y) + t * a.d + c);
         p[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
         p[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
@@ -646,18 +647,20 @@ void launch_route_bwd(const RouteBwdArgs &a, hipStream_t st) {
 void launch_combine(const CombineArgs &a, hipStream_t st) {
     if (a.T == 0) return;
     const int64_t blocks = (a.T * (a.d / 8) + 255) / 256;
-    const double size = a.f32 ? 4 : 2;
-    profile_before(kTagCombine, st, (a.k + 1.0) * size * a.T * a.d);
+    profile_before(kTagCombine, st, (a.k * (a.o_f32 ? 4.0 : 2.0) + (a.y_f32 ? 4.0 : 2.0)) * a.T * a.d);
     // as many rows at once as there are, up to 128 bytes a thread (k = 8: one at a time 29.4 us, eight 23.9; k = 2, 1041 tokens of 4096: two
     // 7.0, eight 8.7)
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a); };
-    if (a.f32) {
-        if (a.k <= 2) go(combine_kernel<true, 2>);
-        else go(combine_kernel<true, 4>);
+    if (a.y_f32) {
+        if (a.k <= 2) go(combine_kernel<true, true, 2>);
+        else go(combine_kernel<true, true, 4>);
+    } else if (a.o_f32) {
+        if (a.k <= 2) go(combine_kernel<true, false, 2>);
+        else go(combine_kernel<true, false, 4>);
     } else {
-        if (a.k <= 2) go(combine_kernel<false, 2>);
-        else if (a.k <= 4) go(combine_kernel<false, 4>);
-        else go(combine_kernel<false, 8>);
+        if (a.k <= 2) go(combine_kernel<false, false, 2>);
+        else if (a.k <= 4) go(combine_kernel<false, false, 4>);
+        else go(combine_kernel<false, false, 8>);
     }
     profile_after(st);
 }
