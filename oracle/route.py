@@ -92,5 +92,6 @@ def gradient(z, ids, dw, score=SOFTMAX, renorm=True, scale=1.0):
             if chosen[t, j]:
                 ds[t, ids[t, j]] += dw[t, j]
     if score == SIGMOID:
-        return ds * s * (1.0 - s)
+        with np.errstate(over="ignore"):
+            return ds * s / (1.0 + np.exp(np.where(open_, z, -np.inf)))          # 1 - s without the difference
     return s * (ds - (ds * s).sum(-1, keepdims=True))

@@ -468,7 +468,8 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
 #pragma unroll
     for (int i = 0; i < 2; ++i)
         if (id[i] >= 0) {
-            const float d = softmax ? q[i] * s[i] : q[i] * s[i] * (1.0f - s[i]);
+            // (1 - s from the logit: as a difference it has no bits left where s is close to 1, a quarter of the value at z = 16)
+            const float d = softmax ? q[i] * s[i] : q[i] * s[i] * sigmoid_f32(-z[i]);
             if (dense) mine[id[i]] += d;
             else mine[id[i]] = d;
         }

@@ -1,0 +1,42 @@
+"""Routing where scores are next to 0 or 1: weights and gradients with errors relative to themselves, from references without differences of
+nearly equal numbers."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2409_12517_amd as ssg
+from gpu_util import DEV, f32
+
+pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -24
+SOFTMAX, SIGMOID = ssg.SSG_ROUTE_SOFTMAX, ssg.SSG_ROUTE_SIGMOID
+
+
+def desc_of(z, k, **more):
+    return ssg.make_route_desc(z.shape[0], z.shape[1], k, logits_dtype=ssg.SSG_BF16 if z.dtype == torch.bfloat16 else ssg.SSG_F32, **more)
+
+
+def route(desc, z, bias=None):
+    ids, w = torch.full((desc.T, desc.k), -77, dtype=torch.int32, device=DEV), torch.full((desc.T, desc.k), -77.0, device=DEV)
+    ssg.ssg_route(desc, z.to(DEV), bias, ids, w, None, None, None, None, None)
+    return ids, w
+
+
+def gradient(desc, z, ids, w, dw):
+    dz = torch.full((desc.T, desc.E), -5.0, dtype=z.dtype, device=DEV)
+    ssg.ssg_route_bwd(desc, z.to(DEV), ids, w, dw, dz)
+    return f32(dz).astype(np.float64)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sigmoid_gradient_of_confident_choices(dtype):
+    """s (1 - s) of logits from 0 to 80, on both sides: two sigmoids good to 6 ulp, three products, one rounding to the logits' type."""
+    at = torch.arange(0, 80, 0.375)
+    z = torch.cat([at, -at])[:, None].to(dtype)
+    desc = desc_of(z, 1, score=SIGMOID, renorm=0, scale=2.5)
+    ids, w = route(desc, z)
+    dw = torch.randn(z.shape[0], 1, generator=torch.Generator().manual_seed(1)).to(DEV)
+    zz = f32(z).astype(np.float64)
+    ref = 2.5 * f32(dw).astype(np.float64) / (1 + np.exp(-zz)) / (1 + np.exp(zz))
+    tol = (2 * 12 + 4) * EPS + (2.0 ** -8 if dtype == torch.bfloat16 else 0.0)
+    assert (np.abs(gradient(desc, z, ids, w, dw) - ref) <= tol * np.abs(ref)).all()
