@@ -67,6 +67,13 @@ template <bool BF16> __device__ __forceinline__ float load_logit(const void *p, 
 __device__ __forceinline__ bool is_open(float z) { return z > -INFINITY; }            // false for NaN
 __device__ __forceinline__ float held(float z) { return fminf(z, 3.402823466e+38f); } // +inf: the largest finite number
 
+// The sigmoid of every logit: sigmoid_f32 stays at e^-88 below -88; where 1 + e^z is 1 to 35 digits this is e^z itself, down to the smallest number.
+__device__ __forceinline__ float score_sigmoid(float z) {
+    float s = sigmoid_f32(z);
+    if (__builtin_expect(z < -80.0f, 0)) s = expf(z);
+    return s;
+}
+
 constexpr float kTiny = 1e-38f;                           // what a sum of scores is held above where it divides
 
 // The k largest keys of the group's lanes, key i of lane l in slot l + i LPT: lane j returns the slot of the j-th, -1 if there is none.
@@ -120,7 +127,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t t, bool live,
             sum = fmaxf(reduce_sum<LPT>(sum), kTiny);
         }
     }
-    auto score = [&](float v) { return softmax ? expf(held(v) - top) / sum : sigmoid_f32(held(v)); };
+    auto score = [&](float v) { return softmax ? expf(held(v) - top) / sum : score_sigmoid(held(v)); };
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
         const int e = g0 + i * LPT;
@@ -209,7 +216,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t t, bool live,
     if (id >= 0) {
         const float v = held(load_logit<BF16>(a.logits, row + id));
         if (softmax) w = sum > 0.0f ? expf(v - top) / sum : expf(v - top);
-        else w = sigmoid_f32(v);
+        else w = score_sigmoid(v);
     }
     if (a.renorm) w = w / fmaxf(reduce_sum<LPT>(w), kTiny);
     w = w * a.scale;
@@ -442,7 +449,7 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         s[i] = 0.0f;
-        if (id[i] >= 0) s[i] = softmax ? expf(z[i] - top) / sum : sigmoid_f32(z[i]);
+        if (id[i] >= 0) s[i] = softmax ? expf(z[i] - top) / sum : score_sigmoid(z[i]);
         part += w[i] * dw[i];
         chosen += s[i];
     }
@@ -469,7 +476,7 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
     for (int i = 0; i < 2; ++i)
         if (id[i] >= 0) {
             // (1 - s from the logit: as a difference it has no bits left where s is close to 1, a quarter of the value at z = 16)
-            const float d = softmax ? q[i] * s[i] : q[i] * s[i] * sigmoid_f32(-z[i]);
+            const float d = softmax ? q[i] * s[i] : q[i] * s[i] * score_sigmoid(-z[i]);
             if (dense) mine[id[i]] += d;
             else mine[id[i]] = d;
         }

@@ -40,3 +40,27 @@ def test_sigmoid_gradient_of_confident_choices(dtype):
     ref = 2.5 * f32(dw).astype(np.float64) / (1 + np.exp(-zz)) / (1 + np.exp(zz))
     tol = (2 * 12 + 4) * EPS + (2.0 ** -8 if dtype == torch.bfloat16 else 0.0)
     assert (np.abs(gradient(desc, z, ids, w, dw) - ref) <= tol * np.abs(ref)).all()
+
+
+# relative error of a weight: the argument of the exponential rounded once where it is below 32, expf and the sigmoid good to 6 ulp, a sum of 16
+# terms in sequence and 6 in a tree, two divisions and a product
+W_TOL = (32 + 2 * 6 + 22 + 3) * 2 * EPS
+
+
+def test_sigmoid_scores_of_low_logits():
+    """As they are: e^z down to the smallest number, in steps of it."""
+    z = -torch.arange(75, 110, 0.25)[:, None]
+    desc = desc_of(z, 1, score=SIGMOID, renorm=0)
+    ids, w = route(desc, z)
+    ref = np.exp(f32(z).astype(np.float64))
+    assert (np.abs(f32(w) - ref) <= W_TOL * ref + 2 * 2.0 ** -149).all()
+    dz = gradient(desc, z, ids, w, torch.ones(z.shape[0], 1, device=DEV))
+    assert (np.abs(dz - ref) <= W_TOL * ref + 4 * 2.0 ** -149).all()
+    dz = gradient(desc_of(z, 1, score=SIGMOID, renorm=0), -z, ids, w, torch.ones(z.shape[0], 1, device=DEV))
+    assert (np.abs(dz - ref) <= W_TOL * ref + 4 * 2.0 ** -149).all()
+
+
+def test_the_order_of_the_lowest_scores():
+    z = torch.tensor([[-100.0, -89.0, -95.0, -92.0, -101.0]])
+    for bias in (None, torch.zeros(5, device=DEV)):
+        assert route(desc_of(z, 5, score=SIGMOID), z, bias)[0].tolist() == [[1, 3, 2, 0, 4]]
