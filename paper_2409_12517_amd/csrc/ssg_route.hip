@@ -74,7 +74,11 @@ __device__ __forceinline__ float score_sigmoid(float z) {
     return s;
 }
 
-constexpr float kTiny = 1e-38f;                           // what a sum of scores is held above where it divides
+constexpr float kTiny = 1e-38f;                           // what a sum of scores is held above where it divides (without any it is 0)
+
+// Renormalised weights need the chosen scores up to a common factor, which is taken so that their sum neither underflows nor loses bits:
+// softmax scores beside the largest chosen logit, and so sigmoids where that is below this, which are e^z to 2e-9.
+constexpr float kLowSigmoid = -20.0f;
 
 // The k largest keys of the group's lanes, key i of lane l in slot l + i LPT: lane j returns the slot of the j-th, -1 if there is none.
 template <int LPT, int VPL> __device__ __forceinline__ int pick(uint32_t (&key)[VPL], int k) {
@@ -213,10 +217,16 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int64_t t, bool live,
         id = pick<LPT>(key, a.k);
     }
     w = 0.0f;
+    const float v = id >= 0 ? held(load_logit<BF16>(a.logits, row + id)) : 0.0f;
+    bool beside_best = false;
+    if (a.renorm) {
+        const uint32_t m = reduce_max<LPT>(id >= 0 ? ordered(v) : 0u);
+        if (m) top = from_ordered(m);
+        beside_best = softmax || (m && top < kLowSigmoid);
+    }
     if (id >= 0) {
-        const float v = held(load_logit<BF16>(a.logits, row + id));
-        if (softmax) w = sum > 0.0f ? expf(v - top) / sum : expf(v - top);
-        else w = score_sigmoid(v);
+        if (beside_best) w = expf(v - top);
+        else w = softmax ? expf(v - top) / sum : score_sigmoid(v);
     }
     if (a.renorm) w = w / fmaxf(reduce_sum<LPT>(w), kTiny);
     w = w * a.scale;
@@ -417,7 +427,7 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
         z[i] = id[i] >= 0 ? held(load_logit<BF16>(a.logits, t * a.ld + id[i])) : 0.0f;
     }
     float top = 0.0f, sum = 1.0f;
-    if (softmax) {
+    if (softmax || a.renorm) {
         uint32_t m = 0;
         if (dense) {
             for (int e = g0; e < a.E; e += 16) {
@@ -449,7 +459,7 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         s[i] = 0.0f;
-        if (id[i] >= 0) s[i] = softmax ? expf(z[i] - top) / sum : score_sigmoid(z[i]);
+        if (id[i] >= 0) s[i] = softmax || (a.renorm && top < kLowSigmoid) ? expf(z[i] - top) / sum : score_sigmoid(z[i]);
         part += w[i] * dw[i];
         chosen += s[i];
     }

@@ -64,3 +64,46 @@ def test_the_order_of_the_lowest_scores():
     z = torch.tensor([[-100.0, -89.0, -95.0, -92.0, -101.0]])
     for bias in (None, torch.zeros(5, device=DEV)):
         assert route(desc_of(z, 5, score=SIGMOID), z, bias)[0].tolist() == [[1, 3, 2, 0, 4]]
+
+
+def shares(z):
+    """Sigmoids of each row of z, divided by their sum."""
+    log = -np.logaddexp(0.0, -z)
+    e = np.exp(log - log.max(-1, keepdims=True))
+    return e / e.sum(-1, keepdims=True)
+
+
+def low_logits(T, E):
+    """Rows whose largest logit is between -10 and -3e38, the others up to 30 below it."""
+    gen = np.random.default_rng(3)
+    base = np.array([-10, -15, -21, -60, -79.5, -86, -88.5, -90, -104, -120, -500, -3e38])[np.arange(T) % 12]
+    return torch.from_numpy((base[:, None] - gen.permuted(np.linspace(0, 30, E), axis=None) * gen.random((T, 1)))).float()
+
+
+@pytest.mark.parametrize("E,k", [(5, 1), (16, 4), (40, 20)])
+def test_renormalised_sigmoid_weights_of_low_logits(E, k):
+    z = low_logits(48, E)
+    desc = desc_of(z, k, score=SIGMOID, scale=2.5)
+    ids, w = route(desc, z)
+    ids = ids.cpu().numpy()
+    ref = 2.5 * shares(np.take_along_axis(f32(z).astype(np.float64), ids, 1))
+    assert (np.abs(f32(w) - ref) <= W_TOL * ref).all()
+    # the gradient: r_j (1 - s_j) sum_i r_i (dw_j - dw_i) scale, where 1 - s_j is 1 to 5e-5
+    dw = torch.randn(48, k, generator=torch.Generator().manual_seed(1)).to(DEV)
+    got = np.take_along_axis(gradient(desc, z, torch.from_numpy(ids).to(DEV), w, dw), ids, 1)
+    chosen, d = np.take_along_axis(f32(z).astype(np.float64), ids, 1), f32(dw).astype(np.float64)
+    r = shares(chosen)
+    want = 2.5 * r / (1 + np.exp(chosen)) * (r[:, None, :] * (d[:, :, None] - d[:, None, :])).sum(-1)
+    assert (np.abs(got - want) <= 4 * W_TOL * 2.5 * r * np.abs(d).max(-1, keepdims=True)).all()
+
+
+def test_renormalised_softmax_weights_far_below_the_largest():
+    """A bias sends tokens past their best expert; the chosen ones' scores, e^-60 to e^-130, still have their ratios."""
+    z = torch.tensor([[t, 0.0, -1.0, -2.5, 1.5] for t in (0.0, 60.0, 85.0, 95.0, 130.0)])
+    bias = torch.tensor([-1e3, 4.0, 3.0, 2.0, 1.0], device=DEV)
+    desc = desc_of(z, 3, scale=2.5)
+    ids, w = route(desc, z, bias)
+    assert ids.tolist() == [[1, 2, 3]] * 5
+    e = np.exp(np.array([0.0, -1.0, -2.5]))
+    ref = 2.5 * e / e.sum()
+    assert (np.abs(f32(w) - ref) <= W_TOL * ref).all()
