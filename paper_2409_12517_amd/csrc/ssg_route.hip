@@ -404,6 +404,9 @@ __global__ __launch_bounds__(kBlock) void dispatch_kernel(RouteArgs a, int block
 // With q_j = ds/dw of the chosen: (scale dw_j - sum_i w_i dw_i) / S where renormalised (S the sum of the chosen scores), else scale dw_j;
 //   sigmoid: dz_j = q_j s_j (1 - s_j)        softmax: dz_e = s_e ([e chosen] q_e - sum_j q_j s_j)
 // and with renormalised softmax weights the last sum is zero and s_j / S = w_j / scale: only the chosen experts' logits have one.
+// A sum over shares of which one is nearly 1 is nearly that one's own term, and its difference from it would have no bits left.  So the dw
+// and q above are counted from those of the expert with the largest share (not renormalised: where that is above one half; the
+// experts that were not chosen, whose q is 0, then have minus that): its own term is zero, and what remains is the others'.
 // A block forms the rows of its tokens in LDS, 16 lanes to a token, and streams them out: 16384 x 256 fp32 (17 MB written, 1.5 read)
 // 6.9 us, which is the writes and a launch.  Without renormalisation the row's logits are read too.
 constexpr int kBwdThreads = 256, kBwdTokens = kBwdThreads / 16;
@@ -456,12 +459,30 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
         }
     }
     float s[2], part = 0.0f, chosen = 0.0f;
+    uint32_t most = 0, star = 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         s[i] = 0.0f;
         if (id[i] >= 0) s[i] = softmax || (a.renorm && top < kLowSigmoid) ? expf(z[i] - top) / sum : score_sigmoid(z[i]);
-        part += w[i] * dw[i];
+        const uint32_t u = __float_as_uint(s[i]);
+        most = most > u ? most : u;
         chosen += s[i];
+    }
+    most = reduce_max<16>(most);
+    float from = 0.0f;                                     // what the dw are counted from
+    if (a.renorm || (dense && __uint_as_float(most) > 0.5f)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t u = id[i] >= 0 && __float_as_uint(s[i]) == most ? ordered(dw[i]) : 0u;
+            star = star > u ? star : u;
+        }
+        star = reduce_max<16>(star);
+        if (star) from = from_ordered(star);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (id[i] >= 0) dw[i] -= from;
+        part += w[i] * dw[i];
     }
     if (a.renorm) {
         part = reduce_sum<16>(part);
@@ -476,8 +497,22 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
     }
     if (dense) {
         mean = reduce_sum<16>(mean);
-        const float by = mean / sum;
-        for (int e = g0; e < a.E; e += 16) mine[e] = -mine[e] * by;
+        const float none = -a.scale * from;                // q of the experts that were not chosen
+        if (__any(from != 0.0f)) {
+            // their share, summed without the chosen ones
+            __builtin_amdgcn_wave_barrier();
+            __threadfence_block();
+            float rest = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (id[i] >= 0) mine[id[i]] = 0.0f;
+            __builtin_amdgcn_wave_barrier();
+            __threadfence_block();
+            for (int e = g0; e < a.E; e += 16) rest += mine[e];
+            mean += none * (reduce_sum<16>(rest) / sum);
+        }
+        const float by = (none - mean) / sum;
+        for (int e = g0; e < a.E; e += 16) mine[e] = mine[e] * by;
     } else {
         for (int e = g0; e < a.E; e += 16) mine[e] = 0.0f;
     }
@@ -486,9 +521,8 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
     for (int i = 0; i < 2; ++i)
         if (id[i] >= 0) {
             // (1 - s from the logit: as a difference it has no bits left where s is close to 1, a quarter of the value at z = 16)
-            const float d = softmax ? q[i] * s[i] : q[i] * s[i] * score_sigmoid(-z[i]);
-            if (dense) mine[id[i]] += d;
-            else mine[id[i]] = d;
+            if (dense) mine[id[i]] = s[i] * (q[i] - mean);
+            else mine[id[i]] = softmax ? q[i] * s[i] : q[i] * s[i] * score_sigmoid(-z[i]);
         }
     __syncthreads();
     // the block's rows are one run of memory that starts on 16 bytes (kBwdTokens rows are a multiple of it)

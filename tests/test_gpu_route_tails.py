@@ -107,3 +107,31 @@ def test_renormalised_softmax_weights_far_below_the_largest():
     e = np.exp(np.array([0.0, -1.0, -2.5]))
     ref = 2.5 * e / e.sum()
     assert (np.abs(f32(w) - ref) <= W_TOL * ref).all()
+
+
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("k", [1, 3, 20])
+@pytest.mark.parametrize("E", [23, 160])
+def test_softmax_gradient_of_confident_choices(renorm, k, E):
+    """dz_e = s_e sum_i s_i (q_e - q_i): over the pairs with the expert that has nearly all of the softmax, and every other.  An error is
+    relative to the terms of the sum, each a product of two scores (of shares, where they are renormalised)."""
+    gen = torch.Generator().manual_seed(E + k)
+    z = torch.randn(64, E, generator=gen)
+    z[torch.arange(64), torch.randint(0, E, (64,), generator=gen)] += torch.linspace(0, 20, 64)
+    desc = desc_of(z, k, renorm=renorm, scale=2.5)
+    ids, w = route(desc, z)
+    dw = torch.randn(64, k, generator=gen).to(DEV)
+    got = gradient(desc, z, ids, w, dw)
+    rows, host = np.arange(64)[:, None], ids.cpu().numpy()
+    zz, q = f32(z).astype(np.longdouble), np.zeros((64, E), np.longdouble)
+    q[rows, host] = 2.5 * f32(dw)
+    s = np.exp(zz - zz.max(-1, keepdims=True))
+    if renorm:
+        chosen = np.zeros((64, E), bool)
+        chosen[rows, host] = True
+        s = np.where(chosen, s, 0)
+    s /= s.sum(-1, keepdims=True)
+    apart = q[:, :, None] - q[:, None, :]
+    ref = s * (s[:, None, :] * apart).sum(-1)
+    size = s * (s[:, None, :] * (np.abs(q)[:, :, None] + np.abs(q)[:, None, :]) * ~np.eye(E, dtype=bool)).sum(-1)
+    assert (np.abs(got - ref) <= 4 * W_TOL * size).all()
