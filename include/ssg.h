@@ -374,8 +374,8 @@ ssg_status ssg_adam_view_state(int64_t n, int32_t step, const void *state, ssg_a
  * its two best scores, with the bias where there is one (group_top = 2; what it has, if that is one).  Then the k largest keys are
  * chosen, in descending order; ties go to the lower index.  The weights are scale * score_e, with renorm = 1
  * divided by the sum of the chosen scores; the bias enters the choice only.
- * An expert whose logit is -inf or NaN, or whose biased key is, is closed to the token (a closed one has score 0); +inf counts as the largest finite
- * number.  Where fewer than k experts are open the last ids are -1 and their weights 0: a row of -inf is a padding token.
+ * An expert whose logit is -inf or NaN is closed to the token and has score 0; +inf counts as the largest finite number.  A bias of -inf or NaN keeps
+ * an expert from being chosen and changes no score: a softmax's sum counts it.  Where fewer than k experts can be chosen the last ids are -1 and their weights 0: a row of -inf is a padding token.
  *
  * The order of dispatch: assignment a = t * k + j, sorted by expert and by a within one; each expert's rows start at a multiple of
  * row_align.  counts[e]: rows of expert e; offsets[e]: its first row, offsets[E] the end of the last; place[a]: the row of an

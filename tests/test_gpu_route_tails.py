@@ -135,3 +135,19 @@ def test_softmax_gradient_of_confident_choices(renorm, k, E):
     ref = s * (s[:, None, :] * apart).sum(-1)
     size = s * (s[:, None, :] * (np.abs(q)[:, :, None] + np.abs(q)[:, None, :]) * ~np.eye(E, dtype=bool)).sum(-1)
     assert (np.abs(got - ref) <= 4 * W_TOL * size).all()
+
+
+@pytest.mark.parametrize("shut", [-torch.inf, torch.nan])
+def test_a_bias_that_shuts_an_expert_changes_no_score(shut):
+    z = torch.tensor([[3.0, 2.0, 1.0, 0.0], [-torch.inf, 0.5, 0.25, torch.nan]])
+    bias = torch.tensor([shut, 0.0, 0.0, 0.0], device=DEV)
+    desc = desc_of(z, 3, renorm=0)
+    ids, w = route(desc, z, bias)
+    assert ids.tolist() == [[1, 2, 3], [1, 2, -1]]
+    e = np.exp(np.array([[3.0, 2.0, 1.0, 0.0], [-np.inf, 0.5, 0.25, -np.inf]]))
+    s = e / e.sum(-1, keepdims=True)
+    ref = np.stack([s[0, 1:], [s[1, 1], s[1, 2], 0.0]])
+    assert (np.abs(f32(w) - ref) <= W_TOL * ref).all()
+    # its logit moves the others' scores: dz_0 = -s_0 sum_j s_j dw_j
+    got = gradient(desc, z, ids, w, torch.ones(2, 3, device=DEV))
+    assert abs(got[0, 0] + s[0, 0] * s[0, 1:].sum()) <= 4 * W_TOL and got[1, 0] == 0.0
