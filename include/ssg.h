@@ -450,8 +450,9 @@ size_t ssg_moe_workspace_bytes(const ssg_moe_desc *desc);
 ssg_status ssg_moe_fwd(const ssg_moe_desc *desc, const void *x, const void *logits, const float *bias, const void *W1, size_t W1_bytes,
                        const void *W2, size_t W2_bytes, const void *W3, size_t W3_bytes, void *y, void *workspace, size_t workspace_bytes,
                        void *stream);
-/* Pointers into `workspace` after a call, for tests and reports.  A call of up to four tokens (with d up to 65536 and k f up to about
- * 128 K) keeps only ids, weights and h, its row t k + j for assignment (t, j); the others are NULL then.  Its results are the same bits. */
+/* Pointers into `workspace` after a call, for tests and reports.  A call of up to four tokens, with d up to 65536 and f up to 8192
+ * times the largest power of two that is at most 16 / k (8192 for k > 8), keeps only ids, weights and h, its row t k + j for assignment (t, j); the
+ * others are NULL then.  Its results are the same bits. */
 typedef struct {
     int64_t rows;                        /* rows of x_q, h, h_q and o; those from offsets[E] on are not written */
     const int32_t *ids;
