@@ -17,17 +17,23 @@ namespace ssg {
 namespace {
 
 typedef int v4i_t __attribute__((ext_vector_type(4)));
-constexpr int kAtOnce = 8;                     // steps of 64 whose weights a wave loads before it multiplies
+// Steps of 64 whose weights a wave loads before it multiplies; beyond its share it loads the last one again.  Microseconds, one token, by the
+// steps that are a wave's share:
+//   mix kernel                  3     6     8    11    16    22    28    32       token kernel   2 matrices: 4     8    16   1 matrix: 4     8    16    28
+//    8 at once                8.2   8.9   8.2  12.2  12.8  16.3  20.4  18.4        4 at once             6.9  17.2  14.7            6.8   5.5   8.8  12.3
+//   12                        9.2  10.2   9.0  11.5  15.2  17.1  21.9  19.9        8                     7.5  16.8  13.8            8.3   6.0   8.3  12.6
+//   16                       10.8  11.7  10.5  13.1  13.8  19.5  21.0  20.5       12                     8.5  19.8  16.2            9.6   6.7   9.3  13.4
+constexpr int kAtOnce = 8;
 
 // The products of this wave's steps [k0, k1) of 64 along K: weights from `b` (1 KB a step), codes of lane l & 15's row from LDS at
-// `codes`, where step k0 lies first.  `first` holds the first kAtOnce steps' weights; beyond the end the last step again, times zero.
-template <int NB, int AT_ONCE> struct Stream {
+// `codes`, where step k0 lies first: kAtOnce at a time, beyond the end the last step again, times zero.
+template <int NB> struct Stream {
     const uint8_t *b[NB];
     int k0, k1;
-    v4i_t w[AT_ONCE][NB];
+    v4i_t w[kAtOnce][NB];
     __device__ __forceinline__ void load(int k) {
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
+        for (int u = 0; u < kAtOnce; ++u) {
             const int at = k + u < k1 ? k + u : (k1 > 0 ? k1 - 1 : 0);
 #pragma unroll
             for (int c = 0; c < NB; ++c) w[u][c] = __builtin_nontemporal_load(reinterpret_cast<const v4i_t *>(b[c] + (int64_t)at * 1024));
@@ -35,7 +41,7 @@ template <int NB, int AT_ONCE> struct Stream {
     }
     __device__ __forceinline__ void multiply(int k, const uint8_t *codes, v4i_t (&acc)[NB]) {
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
+        for (int u = 0; u < kAtOnce; ++u) {
             const bool in = k + u < k1;
             const v4i_t x = *reinterpret_cast<const v4i_t *>(codes + (in ? k + u - k0 : 0) * 64) & (in ? -1 : 0);
 #pragma unroll
@@ -56,7 +62,7 @@ template <bool BF16, bool DUAL, int WAVES, int ROWS> __global__ __launch_bounds_
     if (expert < 0) return;
     const int64_t from = a.ids ? pair / a.k : 0;
     const int share = (KB + WAVES - 1) / WAVES;
-    Stream<NB, kAtOnce> s;
+    Stream<NB> s;
     s.k0 = w * share < KB ? w * share : KB;
     s.k1 = s.k0 + share < KB ? s.k0 + share : KB;
 #pragma unroll
@@ -145,7 +151,7 @@ template <bool BF16, bool DUAL, int WAVES, int ROWS> __global__ __launch_bounds_
 }
 
 // y[t, 16 columns]: kMixWaves waves, `split` of them to an expert, each with a share of K; h row t k + j is the expert's input.
-constexpr int kMixWaves = 16, kMixAtOnce = 12;        // (a share of f = 1376 is 11 steps; with 8 at once 12.3 us for 11.3, with 16 12.4)
+constexpr int kMixWaves = 16;
 template <bool O_F32, bool Y_F32> __global__ __launch_bounds__(64 * kMixWaves) void i8_mix_kernel(I8MixArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t codes[];          // kMixWaves shares
     __shared__ v4i_t part[kMixWaves][4];
@@ -166,7 +172,7 @@ template <bool O_F32, bool Y_F32> __global__ __launch_bounds__(64 * kMixWaves) v
         const int expert = w / split < at_once && j < a.k ? __builtin_amdgcn_readfirstlane(a.ids[t * a.k + j]) : -1;
         float scale = 0.0f;
         if (expert >= 0) {
-            Stream<1, kMixAtOnce> s;
+            Stream<1> s;
             s.k0 = w % split * share < KB ? w % split * share : KB;
             s.k1 = s.k0 + share < KB ? s.k0 + share : KB;
             s.b[0] = a.B + ((int64_t)expert * col_blocks + cb) * KB * 1024 + l * 16;
@@ -198,7 +204,7 @@ template <bool O_F32, bool Y_F32> __global__ __launch_bounds__(64 * kMixWaves) v
             const uint8_t *x = mine + (l >> 4) * 16;    // (all 16 rows the same: only one is used)
             if (s.k0 < s.k1) {
                 s.multiply(s.k0, x, acc);
-                for (int k = s.k0 + kMixAtOnce; k < s.k1; k += kMixAtOnce) {
+                for (int k = s.k0 + kAtOnce; k < s.k1; k += kAtOnce) {
                     s.load(k);
                     s.multiply(k, x, acc);
                 }
