@@ -110,9 +110,14 @@ template <bool BF16, int ROWS> void launch_rows_as(const I8RowsArgs &a, hipStrea
     else if (runs <= 2 * kCols * kMost) go(i8_rows_kernel<BF16, 512, kMost, ROWS>, 512);
     else go(i8_rows_kernel<BF16, 1024, kMost, ROWS>, 1024);
 }
-// Few rows in smaller blocks, so that they are more compute units' work (11008 bf16 a row, cold, with the events around the launch: 333 rows
-// 12.1 us in blocks of eight, 11.4 of four, 9.1 of two; 2304 rows of 4096 12.7, 10.2 and 11.1); many in blocks of eight, whose pieces fill cache
-// lines (4096 rows of 11008 34, 37 and 46).
+// Few rows in smaller blocks, so that they are more compute units' work; many in blocks of eight, whose pieces fill cache lines.  Microseconds in
+// blocks of two, four and eight rows, bf16, cold, of 1376, 4096 and 11008:
+//    384 rows   3.7  4.0  4.5     4.5  5.2  7.5     7.4  9.2 10.1       2816 rows   6.1  5.3  5.2    13.2 11.6 12.9    31.2 22.6 22.8
+//    768        4.0  4.0  4.3     5.2  5.4  7.8    11.3 13.4 14.0       3584        6.6  6.2  5.6    15.2 11.7 13.3    37.5 29.3 25.6
+//   1536        4.8  4.6  4.8     6.8  6.1  8.2    15.9 15.7 16.5       8192       13.4 11.4 12.0    29.2 22.1 21.4
+//   2304        5.6  5.1  5.1    11.5 10.0 12.0    27.9 20.9 22.5
+// Between 2304 and 2816 rows four are faster than eight, or within 4 %, at every width from 688 to 11008 in both types; beyond, that depends on the
+// width.
 template <bool BF16> void launch_rows(const I8RowsArgs &a, hipStream_t st) {
     if (a.rows <= 512) launch_rows_as<BF16, 2>(a, st);
     else if (a.rows <= 2560) launch_rows_as<BF16, 4>(a, st);
