@@ -126,7 +126,7 @@ template <bool BF16> void launch_rows(const I8RowsArgs &a, hipStream_t st) {
 
 // Row-major codes and scales into the layout and back, 16 bytes to a thread.
 __global__ void i8_pack_kernel(const int8_t *codes, const float *scales, int64_t rows, int64_t K, uint8_t *out, float *out_scales) {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const int64_t i = block_of_many() * 256 + threadIdx.x;
     const int64_t padded = i8_width(K) / 16, up = i8_up(rows, 16);
     if (i < up) out_scales[i] = i < rows ? scales[i] : 0.0f;
     if (i >= up * padded) return;
@@ -136,7 +136,7 @@ __global__ void i8_pack_kernel(const int8_t *codes, const float *scales, int64_t
     *reinterpret_cast<uint4 *>(out + i * 16) = v;
 }
 __global__ void i8_unpack_kernel(const uint8_t *in, const float *in_scales, int64_t rows, int64_t K, int8_t *codes, float *scales) {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const int64_t i = block_of_many() * 256 + threadIdx.x;
     const int64_t padded = i8_width(K) / 16, up = i8_up(rows, 16);
     if (i < rows) scales[i] = in_scales[i];
     if (i >= up * padded) return;
@@ -156,12 +156,12 @@ void launch_i8_quantize(const I8RowsArgs &a, hipStream_t st) {
 
 void launch_i8_pack(const int8_t *codes, const float *scales, int64_t rows, int64_t K, uint8_t *out, float *out_scales, hipStream_t st) {
     const int64_t n = i8_code_bytes(rows, K) / 16;
-    hipLaunchKernelGGL(i8_pack_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, codes, scales, rows, K, out, out_scales);
+    hipLaunchKernelGGL(i8_pack_kernel, grid_of_many((n + 255) / 256), dim3(256), 0, st, codes, scales, rows, K, out, out_scales);
 }
 
 void launch_i8_unpack(const uint8_t *in, const float *in_scales, int64_t rows, int64_t K, int8_t *codes, float *scales, hipStream_t st) {
     const int64_t n = i8_code_bytes(rows, K) / 16;
-    hipLaunchKernelGGL(i8_unpack_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, in, in_scales, rows, K, codes, scales);
+    hipLaunchKernelGGL(i8_unpack_kernel, grid_of_many((n + 255) / 256), dim3(256), 0, st, in, in_scales, rows, K, codes, scales);
 }
 
 }  // namespace ssg

@@ -551,7 +551,7 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
 // F32: the rows' type, Y_F32: y's.
 template <bool F32, bool Y_F32, int AT_ONCE> __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     const int per_row = (int)(a.d / 8);
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t i = block_of_many() * 256 + threadIdx.x;
     if (i >= a.T * per_row) return;
     const int64_t t = i / per_row;
     const int64_t c = (i - t * per_row) * 8;
@@ -702,7 +702,7 @@ void launch_combine(const CombineArgs &a, hipStream_t st) {
     profile_before(kTagCombine, st, (a.k * (a.o_f32 ? 4.0 : 2.0) + (a.y_f32 ? 4.0 : 2.0)) * a.T * a.d);
     // as many rows at once as there are, up to 128 bytes a thread (k = 8: one at a time 29.4 us, eight 23.9; k = 2, 1041 tokens of 4096: two
     // 7.0, eight 8.7)
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, a); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid_of_many(blocks), dim3(256), 0, st, a); };
     if (a.y_f32) {
         if (a.k <= 2) go(combine_kernel<true, true, 2>);
         else go(combine_kernel<true, true, 4>);
