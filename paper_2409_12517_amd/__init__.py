@@ -22,8 +22,12 @@ if not os.path.exists(LIB_PATH):
 
 # torch brings a HIP runtime of its own.  Loaded after it the library takes that one; loaded before it, it would bring in the installed
 # one, and the process would have two, of which the library's sees no device.
+_raw_stream = None
 try:
-    import torch  # noqa: F401
+    import torch
+    # The current stream's handle without a Stream object around it, which costs 3 us a call.  The name is not one of torch's public ones:
+    # where it is missing, the public way.
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 except ImportError:
     pass                       # (without torch there is one runtime, and pointers are passed as integers)
 
@@ -217,8 +221,9 @@ def _ptr(t):
 def _stream(stream):
     if stream is None:
         import torch
-        # the stream's handle without a Stream object around it, which costs 3 us a call
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
+        return torch.cuda.current_stream().cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
