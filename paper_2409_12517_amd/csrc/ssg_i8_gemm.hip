@@ -1,6 +1,6 @@
 // Products in 8-bit integers with a scale for each token and channel, for one matrix of weights or for those of E experts:
 //
-//   C[m,n] = (sum_k a[m,k] b[n,k]) sa[m] sb[n]            the sum exact, in 32-bit integers (K <= 131072)
+//   C[m,n] = (sum_k a[m,k] b[n,k]) sa[m] sb[n]            the sum exact, in 32-bit integers (K <= 131056)
 //   h[m,n] = u g sigma(g),  u and g two such products      the gate/up form, h rounded to bf16
 //
 // Both operands lie in blocks of 16 rows by 64 codes in the order in which a wave holds them (see I8RowsArgs), so a block
@@ -472,9 +472,12 @@ I8Form choose_form(const I8GemmArgs &a, bool dual) {
     if (a.E == 0) {
         const int64_t tiles128 = (a.M + 127) / 128 * cols128, tiles256 = (a.M + 255) / 256 * cols256;
         const int64_t cols16 = (a.N + 15) / 16;
-        if (a.M <= 16 || (a.M + 15) / 16 * cols16 <= 256) return FEW_16;
-        if (a.M <= 32 || (a.M + 31) / 32 * cols16 <= 256) return FEW_32;
-        if (a.M <= 64 || tiles128 <= 64) return FEW_64;
+        // (two matrices come with experts only; should they ever come without, there are tiles for them and no other form)
+        if (!dual) {
+            if (a.M <= 16 || (a.M + 15) / 16 * cols16 <= 256) return FEW_16;
+            if (a.M <= 32 || (a.M + 31) / 32 * cols16 <= 256) return FEW_32;
+            if (a.M <= 64 || tiles128 <= 64) return FEW_64;
+        }
         return (double)((tiles256 + 255) / 256) * large_step < small_time((double)tiles128) ? TILE_256 : TILE_128;
     }
     const double active = (double)std::min<int64_t>(a.E, a.rows_expected), rows = (double)a.rows_expected / active;
@@ -505,7 +508,7 @@ template <bool DUAL> void launch_form(const I8GemmArgs &a, hipStream_t st) {
     if (form == TILE_128) go(i8_tile_kernel<2, DUAL>, DUAL ? 64 : 128, 256, 2 * units);
     else if (form == TILE_256) go(i8_tile_kernel<4, DUAL>, DUAL ? 128 : 256, 256, units);
     else if (form == FEW_16_EXPERTS) go(i8_few_kernel<1, 1, 4, DUAL>, 16, 256, kAll);
-    else if constexpr (!DUAL) {                          // (two matrices only with experts)
+    else if constexpr (!DUAL) {                          // (see choose_form)
         if (form == FEW_16) go(i8_few_kernel<1, 1, 8, false>, 16, 512, kAll);
         else if (form == FEW_32) go(i8_few_kernel<2, 1, 4, false>, 16, 256, kAll);
         else go(i8_few_kernel<4, 2, 8, false>, 32, 512, kAll);
