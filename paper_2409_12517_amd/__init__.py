@@ -497,7 +497,13 @@ def ssg_i8_linear(x, x_dtype, M, K, ldx, W, N, y, y_dtype, ldy, workspace, strea
                               _nbytes(workspace, workspace_bytes), _stream(stream)))
 
 
-def make_moe_desc(route: ssg_route_desc, d: int, f: int, y_dtype: int = SSG_BF16, f32_terms: int = 0) -> ssg_moe_desc:
+def make_moe_desc(route: ssg_route_desc, d: int, f: int, y_dtype: int | None = None, f32_terms: int | None = None) -> ssg_moe_desc:
+    """y is bf16 and the sum of fp32 terms, rounded once, where nothing else is asked for.  Who names y's type gets terms of that type too, half the
+    bytes of bf16 ones, unless f32_terms says otherwise."""
+    if f32_terms is None:
+        f32_terms = int(y_dtype is None)
+    if y_dtype is None:
+        y_dtype = SSG_BF16
     return ssg_moe_desc(route, d, f, y_dtype, f32_terms, (c_int32 * 2)(0, 0))
 
 

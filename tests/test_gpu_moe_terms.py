@@ -20,6 +20,13 @@ def test_workspace():
     assert size(ssg.SSG_BF16, 1) == size(ssg.SSG_F32, 0) == size(ssg.SSG_F32, 1) > size(ssg.SSG_BF16, 0)
 
 
+def test_what_a_caller_gets_who_names_nothing():
+    route = ssg.make_route_desc(4, 8, 2)
+    kinds = [(d.y_dtype, d.f32_terms) for d in (ssg.make_moe_desc(route, 64, 48), ssg.make_moe_desc(route, 64, 48, ssg.SSG_BF16),
+                                                ssg.make_moe_desc(route, 64, 48, ssg.SSG_F32), ssg.make_moe_desc(route, 64, 48, f32_terms=0))]
+    assert kinds == [(ssg.SSG_BF16, 1), (ssg.SSG_BF16, 0), (ssg.SSG_F32, 0), (ssg.SSG_BF16, 0)]
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 4, 5, 40, 700])
 @pytest.mark.parametrize("E,k,d,f", [(3, 1, 272, 80), (8, 2, 528, 400), (12, 5, 96, 208), (24, 8, 256, 336), (40, 20, 80, 64)])
