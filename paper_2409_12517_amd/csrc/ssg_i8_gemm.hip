@@ -106,9 +106,9 @@ __device__ __forceinline__ void dma_from_unless(int no, const uint8_t *base_unif
 // A workgroup has several tiles one after the other and the ring runs on from one to the next: while a tile's last steps are
 // multiplied and its results stored, the first stages of the next are on their way.  A tile with no more rows than half (an expert's
 // last one) loads and multiplies half of them: 4 by 8 blocks to a wave.
-// Bound by the matrix cores under the chip's power: 4096 x 4096 x 11008 takes 131 us, 2.8 POP/s, with MFMAs in 76 % of the cycles
-// at 1.75 GHz (32 x 32 x 32 MFMAs 163, a ring of five stages the same).  With the SwiGLU product a large tile also spends 9 us on
-// its results, half of them (counted) the sigmoid, which its one wave to a SIMD cannot hide: 32768 rows of 64 experts, d = 2048, f = 1376, 222 us, 1.7 POP/s.
+// Bound by the matrix cores under the chip's power: 4096 x 4096 x 11008 takes 125 to 143 us, 140 on average, 2.6 POP/s, with MFMAs in 76 % of the
+// cycles at 1.75 GHz (32 x 32 x 32 MFMAs 163 where it took 148, a ring of five stages the same).  With the SwiGLU product a large tile also spends 9 us on
+// its results, half of them (counted) the sigmoid, which its one wave to a SIMD cannot hide: 32768 rows of 64 experts, d = 2048, f = 1376, 226 us, 1.6 POP/s.
 constexpr int kI8Stages = 4;
 template <int WB> constexpr int i8_stage_bytes() { return 8 * WB * 1024; }
 template <int WB, bool DUAL> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void i8_tile_kernel(I8Params p) {

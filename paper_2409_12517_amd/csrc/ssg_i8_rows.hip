@@ -13,12 +13,6 @@ namespace ssg {
 
 namespace {
 
-// Bound by memory: 4096 rows of 11008 bf16 (135 MB) 30 us, 4.5 TB/s; 4096 tokens of 2048 gathered into 32768 rows (17 MB read eight
-// times, out of the caches, 67 MB written) 28 us.  A block owns ROWS rows, up to half of a row of
-// the layout's blocks: thread t has row t % ROWS and every (threads / ROWS)-th run of 16 codes, so that with eight a wave reads 8 rows x 128
-// elements and writes pieces of 128 bytes; at most 128 registers, since one more halves the blocks on a compute unit (2304 rows of 11008
-// 25 us, 30 then).  The first HELD runs of a thread stay in registers between the
-// maximum and the codes; what a row has beyond them is read again, out of the L2.
 // The list of row tiles, by one wave.
 __device__ __forceinline__ void list_tiles(const int *offsets, int E, int *list, int edge) {
     const int lane = threadIdx.x & 63;
@@ -41,6 +35,12 @@ __device__ __forceinline__ void list_tiles(const int *offsets, int E, int *list,
     if (lane == 0) *reinterpret_cast<int4 *>(list) = make_int4(before, 0, 0, 0);
 }
 
+// Bound by memory: 4096 rows of 11008 bf16 (135 MB) 30 us, 4.5 TB/s; 4096 tokens of 2048 gathered into 32768 rows (17 MB read eight
+// times, out of the caches, 67 MB written) 28 us.  A block owns ROWS rows, up to half of a row of
+// the layout's blocks: thread t has row t % ROWS and every (threads / ROWS)-th run of 16 codes, so that with eight a wave reads 8 rows x 128
+// elements and writes pieces of 128 bytes; at most 128 registers, since one more halves the blocks on a compute unit (a fifth more time for 2304
+// rows of 11008).  The first HELD runs of a thread stay in registers between the
+// maximum and the codes; what a row has beyond them is read again, out of the L2.
 template <bool BF16, int THREADS, int HELD, int ROWS> __global__ __launch_bounds__(THREADS, 4) void i8_rows_kernel(I8RowsArgs a) {
     constexpr int kCols = THREADS / ROWS, kWaves = THREADS / 64;
     __shared__ uint32_t maxima[kWaves][ROWS];

@@ -6,9 +6,10 @@
 //   i8_token_kernel   up to four rows by 16 columns of one matrix, or one row by 16 columns of the two matrices of the expert that
 //                     an assignment (token, choice) names, with the SwiGLU product; waves share K out
 //   i8_mix_kernel     16 columns of a token's result: its experts side by side, a few waves each, and their weighted sum
-// One token: 11008 x 4096 9.4 us, 4.8 TB/s (13.6 in two launches); 8 experts of d = 2048, f = 1376 9 to 11 and 10.5 us for 45 and
+// One token: 11008 x 4096 9.4 us, 4.8 TB/s (13.6 in two launches); 8 experts of d = 2048, f = 1376 9 to 11 and 11 us for 45 and
 // 23 MB (43 us a call in five launches, 25 in three).  What bounds them now is the start and the end of a single
-// round of workgroups: x and the first weights from memory, two barriers, the sums in LDS.
+// round of workgroups: x and the first weights from memory, two barriers, the sums in LDS; in the mix kernel also that one token has d / 16
+// workgroups, 128 on 256 compute units there.
 #include "ssg_gemm_tile.h"
 #include "ssg_i8.h"
 

@@ -264,8 +264,8 @@ size_t adam_scalar_words();
 void launch_adam_init(uint32_t *scalars, uint8_t *codes, size_t code_bytes, hipStream_t st);
 void launch_adam_step(const AdamArgs &a, hipStream_t st);
 
-// Blocks of 256 threads, any number: a launch takes fewer than 2^32 threads along x, which 64 GB at 16 bytes a thread pass, so that they are
-// 2^22 to a row of the grid.  (The last row may reach beyond the blocks asked for.)
+// Blocks of 256 threads, any number: a launch takes fewer than 2^32 threads along x, which 64 GB at 16 bytes a thread pass (what is asked for beyond is
+// left out, without an error), so that they are 2^22 to a row of the grid.  (The last row may reach beyond the blocks asked for.)
 inline dim3 grid_of_many(int64_t blocks) {
     constexpr int64_t kRow = (int64_t)1 << 22;
     return blocks <= kRow ? dim3((unsigned)blocks) : dim3((unsigned)kRow, (unsigned)((blocks + kRow - 1) / kRow));

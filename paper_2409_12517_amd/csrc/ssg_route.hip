@@ -9,9 +9,9 @@
 // A group of LPT lanes owns a token, expert e in lane e % LPT, so that a wave of 16-lane groups chooses for four tokens at once.
 // Keys are compared as integers that order like the floats; 0 is "closed" or "already taken".  Each of the k rounds is a scan of the
 // lane's own keys and two reductions over the group (largest key, lowest expert that has it) in DPP steps.
-// Long batches are bound by the vector ALU: 16384 tokens, 256 experts, sigmoid and bias, 8 of 4 groups of 8: 16 us (21 with the keys of
+// Long batches are bound by the vector ALU: 16384 tokens, 256 experts, sigmoid and bias, 8 of 4 groups of 8: 17.8 us (5 more with the keys of
 // all groups in every round and the groups read in step, from the same banks), half the time with k = 1; 17 MB would take 3.3.  Short ones
-// by latency: 331 tokens 6.6 us.  The order of the rows is a second launch (5 to 9 us), whose blocks each need the counts of all.
+// by latency: 331 tokens 7.1 us.  The order of the rows is a second launch (5 to 9 us), whose blocks each need the counts of all.
 #include "ssg_device.h"
 #include "ssg_internal.h"
 
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(kBlock) void dispatch_kernel(RouteArgs a, int block
 // and q above are counted from those of the expert with the largest share (not renormalised: where that is above one half; the
 // experts that were not chosen, whose q is 0, then have minus that): its own term is zero, and what remains is the others'.
 // A block forms the rows of its tokens in LDS, 16 lanes to a token, and streams them out: 16384 x 256 fp32 (17 MB written, 1.5 read)
-// 6.9 us, which is the writes and a launch.  Without renormalisation the row's logits are read too.
+// 7.9 us, which is the writes and a launch.  Without renormalisation the row's logits are read too (4099 x 64 bf16 5.1 us).
 constexpr int kBwdThreads = 256, kBwdTokens = kBwdThreads / 16;
 template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_kernel(RouteBwdArgs a) {
     extern __shared__ float rows[];
@@ -547,7 +547,7 @@ template <bool BF16> __global__ __launch_bounds__(kBwdThreads) void route_bwd_ke
 
 // ---- the weighted sum of the experts' rows -------------------------------------------------------------------
 // y[t] = sum_j w[t,j] o[place[t,j]], in the order of j, in fp32.  A thread owns 8 columns of a token.  At the rate of a copy: 4096
-// tokens of 8 rows of 2048 bf16 (151 MB) 23.8 us, 6.3 TB/s, part of them still in the memory-side cache.
+// tokens of 8 rows of 2048 bf16 (151 MB) 23.8 us, 6.3 TB/s, part of them still in the memory-side cache; rows in fp32 (285 MB) 51.6, 5.5 TB/s.
 // F32: the rows' type, Y_F32: y's.
 template <bool F32, bool Y_F32, int AT_ONCE> __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     const int per_row = (int)(a.d / 8);
