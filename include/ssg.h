@@ -464,6 +464,88 @@ typedef struct {
 } ssg_moe_workspace_view;
 ssg_status ssg_moe_view_workspace(const ssg_moe_desc *desc, const void *workspace, ssg_moe_workspace_view *out);
 
+/* ---- microscaled 4-bit floating point -------------------------------------------
+ * Matrices whose elements are E2M1 codes (0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives) and in which 32 neighbours along K, the axis that a
+ * product sums over, share a scale, a power of two X.  With amax the largest magnitude of a block and 2^e <= amax < 2^(e+1):
+ *     SSG_MX_FLOOR  X = 2^(e-2): amax / X lies between 4 and 8, magnitudes above 6 X saturate
+ *     SSG_MX_CEIL   X the smallest power of two with amax <= 6 X: nothing saturates
+ *     code = nearest E2M1 value to x / X, of two as near the one whose code is even, with x's sign
+ * X is kept as the byte log2 X + 127, held between 0 and 252 (6 X stays finite; a block of zeros has 0).  A block with a NaN or an infinity
+ * has the byte 255 and codes 0, and every product with it is NaN.
+ * They live in a buffer of ssg_mx4_bytes(rows, K) bytes, 256-byte aligned, in the layout that the products read: blocks of 16 rows by 128
+ * codes, 1 KB each, with Kp = K filled up to 256 by zeros: code (r, k) is a half, the low one for even k, of byte
+ * ((r / 16) * (Kp / 128) + k / 128) * 1024 + (k % 128 / 32) * 256 + r % 16 * 16 + k % 32 / 2; behind them, rows filled up to 16, the
+ * scales: of (r, k) at ((r / 16) * (Kp / 256) + k / 256) * 128 + (k % 128 / 32 * 16 + r % 16) * 2 + k % 256 / 128.
+ * rows up to 2^26, none among them (nothing is launched then), K from 1 to 2^24.
+ * ssg_mx4_quantize: transposed = 0: from rows of src, [rows, K], K a multiple of 16; transposed = 1: from the columns of src, [K, rows], rows a
+ * multiple of 16, K any.  src rows `ld` elements apart, on 16 bytes.
+ * ssg_mx4_dequantize: the values that the codes stand for, exact in both types, into dst [rows, K], rows `ld` elements apart on 16 bytes; what
+ * lies between rows is left alone.
+ * ssg_mx4_pack: from codes [rows, K / 2], the even column's in the low half of a byte, on 8 bytes, and scales [rows, (K + 31) / 32] that a program
+ * has already; ssg_mx4_unpack the way back; K a multiple of 16. */
+typedef enum { SSG_MX_FLOOR = 0, SSG_MX_CEIL = 1 } ssg_mx_rule;
+size_t ssg_mx4_bytes(int64_t rows, int64_t K);
+ssg_status ssg_mx4_quantize(const void *src, ssg_dtype src_dtype, int64_t rows, int64_t K, int64_t ld, int transposed, ssg_mx_rule rule, void *q,
+                            size_t q_bytes, void *stream);
+ssg_status ssg_mx4_dequantize(const void *q, size_t q_bytes, int64_t rows, int64_t K, void *dst, ssg_dtype dst_dtype, int64_t ld, void *stream);
+ssg_status ssg_mx4_pack(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t K, void *q, size_t q_bytes, void *stream);
+ssg_status ssg_mx4_unpack(const void *q, size_t q_bytes, int64_t rows, int64_t K, uint8_t *codes, uint8_t *scales, void *stream);
+/* C[m,n] = sum_k a[m,k] b[n,k] of the values that the codes stand for, fp32 accumulation.  A: M rows, any number; B: N rows, a multiple of 16;
+ * C rows ldc elements apart, on 16 bytes.  The order of the sum, and with it the last bits, is the kernel's that ssg_mx4_gemm_plan names;
+ * the same call gives the same bits. */
+ssg_status ssg_mx4_gemm(const void *A, size_t A_bytes, int64_t M, const void *B, size_t B_bytes, int64_t N, int64_t K, void *C,
+                        ssg_dtype c_dtype, int64_t ldc, void *stream);
+/* Which kernel such a product runs in, as ssg_i8_gemm_plan. */
+ssg_status ssg_mx4_gemm_plan(int64_t M, int64_t N, int64_t K, ssg_gemm_plan *out);
+/* y = x W^T with x [M,K] quantized in the call; W: N rows of K, both multiples of 16.  A few rows are quantized where they are multiplied. */
+size_t ssg_mx4_linear_workspace_bytes(int64_t M, int64_t K);
+ssg_status ssg_mx4_linear(const void *x, ssg_dtype x_dtype, int64_t M, int64_t K, int64_t ldx, ssg_mx_rule rule, const void *W, size_t W_bytes,
+                          int64_t N, void *y, ssg_dtype y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+/* Its backward pass, straight through every quantization: each product's operands are quantized in blocks along the axis that it sums over,
+ *     dx = Q(dy) Q(W^T)^T  (blocks along N)        dW = Q(dy^T) Q(x^T)^T  (blocks along the M rows)
+ * dy [M,N], x [M,K], dx [M,K], dW [N,K]; M any number, also 0 (dW is zeros then).  Wt: W^T quantized, K rows of N (ssg_mx4_quantize of W with
+ * transposed = 1).  dx or dW may be NULL: that product, and what it alone needs (Wt; x), is left out. */
+size_t ssg_mx4_linear_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K);
+ssg_status ssg_mx4_linear_bwd(const void *dy, ssg_dtype dy_dtype, int64_t lddy, const void *x, ssg_dtype x_dtype, int64_t ldx, int64_t M, int64_t N,
+                              int64_t K, ssg_mx_rule rule, const void *Wt, size_t Wt_bytes, void *dx, ssg_dtype dx_dtype, int64_t lddx, void *dW,
+                              ssg_dtype dw_dtype, int64_t lddw, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- root-mean-square norm with the residual's addition ----------------------------
+ * What hands the products above, the block and its 8-bit relatives their rows.  For every row, in fp32:
+ *     s = x + residual, rounded to the residual's type and kept in residual_out (no residual: s = x)
+ *     rstd = 1 / sqrt(mean(s^2) + eps),   y = (s rstd) g,   g = w_offset + w     (w NULL: g = 1)
+ * y leaves in one of five forms:
+ *     SSG_NORM_BF16, SSG_NORM_F32  rows ldy elements apart
+ *     SSG_NORM_E4M3  codes satcast(fl32(y * y_scale[0])), rows ldy bytes apart: an operand of ssg_gemm_fp8 under delayed scaling.  y_amax: out, [T], the
+ *                    rows' ranges max |y| (ssg_amax of them is the tensor's, NaN ignored), or NULL
+ *     SSG_NORM_I8    the buffer that ssg_i8_quantize makes of y in fp32
+ *     SSG_NORM_MX4   the buffer that ssg_mx4_quantize makes of y in fp32, by `rule`
+ * Squares may leave the range of fp32: rstd is right for every finite row.  A row with a NaN or an infinity gives what the formula gives. */
+typedef enum { SSG_NORM_BF16 = 0, SSG_NORM_F32 = 1, SSG_NORM_E4M3 = 2, SSG_NORM_I8 = 3, SSG_NORM_MX4 = 4 } ssg_norm_format;
+typedef struct {
+    int64_t T, d;            /* rows, any number (up to 2^31, to a quantized buffer 2^26), of d values, a multiple of 16 up to 32768 */
+    int64_t ldx, ldr, ldy;   /* elements from one row to the next: of x (and dx), of the residual (and residual_out, ds, dresidual), of y; rows start on 16 bytes */
+    int32_t x_dtype, r_dtype, w_dtype;       /* ssg_dtype */
+    int32_t residual;        /* 1: a residual is added */
+    int32_t y_format;        /* ssg_norm_format */
+    int32_t rule;            /* ssg_mx_rule, of SSG_NORM_MX4 */
+    float eps;               /* 2^-100 to 1 */
+    float w_offset;          /* 1 for weights that are stored around zero */
+    int32_t reserved[2];     /* must be 0 */
+} ssg_rmsnorm_desc;
+/* x, residual, residual_out [T,d]; w [d]; rstd out, [T] fp32, for the backward pass, or NULL.  residual_out may be the residual itself.
+ * y_bytes: the buffer's size (SSG_NORM_I8, SSG_NORM_MX4; else not read). */
+ssg_status ssg_rmsnorm_fwd(const ssg_rmsnorm_desc *desc, const void *x, const void *residual, const void *w, void *residual_out, void *y, size_t y_bytes,
+                           const float *y_scale, float *y_amax, float *rstd, void *stream);
+/* The gradient, straight through y's rounding, with a = dy g and n = s rstd:
+ *     dresidual = ds + rstd (a - n mean(a n)),   dx the same in x's type,   dw = sum over rows of dy n  (fp32, in one order for every call)
+ * dy [T,d]; s: the normed rows as the forward pass left them, residual_out, or x where there is no residual; rstd of the forward pass; ds: the
+ * gradient that reaches residual_out from the layers behind, of the residual's type, or NULL.  dx, dresidual, dw: out, any of them NULL;
+ * dresidual may be ds itself.  T = 0: dw is zeros.  The workspace is for dw alone. */
+size_t ssg_rmsnorm_bwd_workspace_bytes(const ssg_rmsnorm_desc *desc);
+ssg_status ssg_rmsnorm_bwd(const ssg_rmsnorm_desc *desc, const void *dy, ssg_dtype dy_dtype, int64_t lddy, const void *s, const float *rstd, const void *w,
+                           const void *ds, void *dx, void *dresidual, float *dw, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- kernel timing for benchmarks (optional) --------------------------------
  * The one piece of state the library keeps, off by default.  While enabled, every kernel launch of the
  * library is bracketed by two HIP events recorded on the launch's own stream (events are host objects; no
@@ -489,7 +571,8 @@ ssg_status ssg_moe_view_workspace(const ssg_moe_desc *desc, const void *workspac
  * (w3_layer_bf16 = 1), 47 = the passes of 42 and 43 in one launch.
  * Adam: 32 = range pass, 33 = update pass.
  * Experts: 48 = choice (and with few tokens the dispatch), 49 = dispatch, 50 = gradient of the weights, 51 = weighted sum of the experts'
- * rows, 52 = quantization of rows in 8-bit integers; 53 = their products and 54 = the gate/up form (bytes = 0). */
+ * rows, 52 = quantization of rows in 8-bit integers; 53 = their products and 54 = the gate/up form (bytes = 0).
+ * 4 bits and norm: 55 = quantization in microscaled 4-bit floating point and the way back, 56 = products (bytes = 0), 57 = norm, 58 = its gradient. */
 ssg_status ssg_profile_enable(int max_records);
 ssg_status ssg_profile_select(int tag);
 int ssg_profile_read(float *ms, int *tags, double *bytes, int cap);

@@ -40,6 +40,8 @@ SSG_BF16, SSG_F32 = 0, 1
 SSG_SCALE_CURRENT, SSG_SCALE_GIVEN, SSG_SCALE_DELAYED = 0, 1, 2
 SSG_ROUND_EXACT_DIV, SSG_ROUND_POW2 = 0, 1
 SSG_ROUTE_SOFTMAX, SSG_ROUTE_SIGMOID = 0, 1
+SSG_MX_FLOOR, SSG_MX_CEIL = 0, 1
+SSG_NORM_BF16, SSG_NORM_F32, SSG_NORM_E4M3, SSG_NORM_I8, SSG_NORM_MX4 = range(5)
 
 EXPORTS = [
     "ssg_last_error", "ssg_version", "ssg_amax", "ssg_quantize", "ssg_quantize_wait", "ssg_gemm_fp8", "ssg_gemm_fp8_layout", "ssg_gemm_fp8_plan", "ssg_swiglu",
@@ -52,6 +54,9 @@ EXPORTS = [
     "ssg_route_workspace_bytes", "ssg_route_rows", "ssg_route", "ssg_route_bwd",
     "ssg_i8_bytes", "ssg_i8_quantize", "ssg_i8_pack", "ssg_i8_unpack", "ssg_i8_gemm", "ssg_i8_gemm_plan", "ssg_i8_linear_workspace_bytes", "ssg_i8_linear",
     "ssg_moe_workspace_bytes", "ssg_moe_fwd", "ssg_moe_view_workspace",
+    "ssg_mx4_bytes", "ssg_mx4_quantize", "ssg_mx4_dequantize", "ssg_mx4_pack", "ssg_mx4_unpack", "ssg_mx4_gemm", "ssg_mx4_gemm_plan",
+    "ssg_mx4_linear_workspace_bytes", "ssg_mx4_linear", "ssg_mx4_linear_bwd_workspace_bytes", "ssg_mx4_linear_bwd",
+    "ssg_rmsnorm_fwd", "ssg_rmsnorm_bwd_workspace_bytes", "ssg_rmsnorm_bwd",
     "ssg_profile_enable", "ssg_profile_select", "ssg_profile_read",
 ]
 
@@ -103,6 +108,12 @@ class ssg_moe_desc(Structure):
 class ssg_moe_workspace_view(Structure):
     _fields_ = [("rows", c_int64)] + [(n, c_void_p) for n in (
         "ids", "weights", "counts", "offsets", "place", "source", "x_q", "h_q", "h", "o")]
+
+
+class ssg_rmsnorm_desc(Structure):
+    _fields_ = [(n, c_int64) for n in ("T", "d", "ldx", "ldr", "ldy")] + [
+        (n, c_int32) for n in ("x_dtype", "r_dtype", "w_dtype", "residual", "y_format", "rule")] + [
+        ("eps", c_float), ("w_offset", c_float), ("reserved", c_int32 * 2)]
 
 
 class ssg_mlp_saved_view(Structure):
@@ -184,6 +195,26 @@ _lib.ssg_moe_workspace_bytes.argtypes = [POINTER(ssg_moe_desc)]
 _lib.ssg_moe_workspace_bytes.restype = c_size_t
 _lib.ssg_moe_fwd.argtypes = [POINTER(ssg_moe_desc)] + [c_void_p] * 3 + [c_void_p, c_size_t] * 3 + [c_void_p, c_void_p, c_size_t, c_void_p]
 _lib.ssg_moe_view_workspace.argtypes = [POINTER(ssg_moe_desc), c_void_p, POINTER(ssg_moe_workspace_view)]
+_lib.ssg_mx4_bytes.argtypes = [c_int64, c_int64]
+_lib.ssg_mx4_bytes.restype = c_size_t
+_lib.ssg_mx4_quantize.argtypes = [c_void_p, c_int, c_int64, c_int64, c_int64, c_int, c_int, c_void_p, c_size_t, c_void_p]
+_lib.ssg_mx4_dequantize.argtypes = [c_void_p, c_size_t, c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p]
+_lib.ssg_mx4_pack.argtypes = [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_size_t, c_void_p]
+_lib.ssg_mx4_unpack.argtypes = [c_void_p, c_size_t, c_int64, c_int64, c_void_p, c_void_p, c_void_p]
+_lib.ssg_mx4_gemm.argtypes = [c_void_p, c_size_t, c_int64, c_void_p, c_size_t, c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p]
+_lib.ssg_mx4_gemm_plan.argtypes = [c_int64, c_int64, c_int64, POINTER(ssg_gemm_plan)]
+_lib.ssg_mx4_linear_workspace_bytes.argtypes = [c_int64, c_int64]
+_lib.ssg_mx4_linear_workspace_bytes.restype = c_size_t
+_lib.ssg_mx4_linear.argtypes = [c_void_p, c_int, c_int64, c_int64, c_int64, c_int, c_void_p, c_size_t, c_int64, c_void_p, c_int, c_int64,
+                                c_void_p, c_size_t, c_void_p]
+_lib.ssg_mx4_linear_bwd_workspace_bytes.argtypes = [c_int64, c_int64, c_int64]
+_lib.ssg_mx4_linear_bwd_workspace_bytes.restype = c_size_t
+_lib.ssg_mx4_linear_bwd.argtypes = [c_void_p, c_int, c_int64, c_void_p, c_int, c_int64, c_int64, c_int64, c_int64, c_int, c_void_p, c_size_t,
+                                    c_void_p, c_int, c_int64, c_void_p, c_int, c_int64, c_void_p, c_size_t, c_void_p]
+_lib.ssg_rmsnorm_fwd.argtypes = [POINTER(ssg_rmsnorm_desc)] + [c_void_p] * 5 + [c_size_t] + [c_void_p] * 4
+_lib.ssg_rmsnorm_bwd_workspace_bytes.argtypes = [POINTER(ssg_rmsnorm_desc)]
+_lib.ssg_rmsnorm_bwd_workspace_bytes.restype = c_size_t
+_lib.ssg_rmsnorm_bwd.argtypes = [POINTER(ssg_rmsnorm_desc), c_void_p, c_int, c_int64] + [c_void_p] * 8 + [c_size_t, c_void_p]
 for _n in EXPORTS[2:]:
     if not _n.endswith("_bytes"):          # the size queries return size_t, everything else a status
         getattr(_lib, _n).restype = c_int
@@ -522,6 +553,75 @@ def ssg_moe_view_workspace(desc, workspace) -> ssg_moe_workspace_view:
     v = ssg_moe_workspace_view()
     _check(_lib.ssg_moe_view_workspace(ctypes.byref(desc), _ptr(workspace), ctypes.byref(v)))
     return v
+
+
+def ssg_mx4_bytes(rows: int, K: int) -> int:
+    return int(_lib.ssg_mx4_bytes(rows, K))
+
+
+def ssg_mx4_quantize(src, src_dtype, rows, K, ld, transposed, rule, q, stream=None, q_bytes=None) -> None:
+    _check(_lib.ssg_mx4_quantize(_ptr(src), src_dtype, rows, K, ld, transposed, rule, _ptr(q), _nbytes(q, q_bytes), _stream(stream)))
+
+
+def ssg_mx4_dequantize(q, rows, K, dst, dst_dtype, ld, stream=None, q_bytes=None) -> None:
+    _check(_lib.ssg_mx4_dequantize(_ptr(q), _nbytes(q, q_bytes), rows, K, _ptr(dst), dst_dtype, ld, _stream(stream)))
+
+
+def ssg_mx4_pack(codes, scales, rows, K, q, stream=None, q_bytes=None) -> None:
+    _check(_lib.ssg_mx4_pack(_ptr(codes), _ptr(scales), rows, K, _ptr(q), _nbytes(q, q_bytes), _stream(stream)))
+
+
+def ssg_mx4_unpack(q, rows, K, codes, scales, stream=None, q_bytes=None) -> None:
+    _check(_lib.ssg_mx4_unpack(_ptr(q), _nbytes(q, q_bytes), rows, K, _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+def ssg_mx4_gemm(A, M, B, N, K, C, c_dtype, ldc, stream=None, A_bytes=None, B_bytes=None) -> None:
+    _check(_lib.ssg_mx4_gemm(_ptr(A), _nbytes(A, A_bytes), M, _ptr(B), _nbytes(B, B_bytes), N, K, _ptr(C), c_dtype, ldc, _stream(stream)))
+
+
+def ssg_mx4_gemm_plan(M, N, K) -> ssg_gemm_plan:
+    p = ssg_gemm_plan()
+    _check(_lib.ssg_mx4_gemm_plan(M, N, K, ctypes.byref(p)))
+    return p
+
+
+def ssg_mx4_linear_workspace_bytes(M: int, K: int) -> int:
+    return int(_lib.ssg_mx4_linear_workspace_bytes(M, K))
+
+
+def ssg_mx4_linear(x, x_dtype, M, K, ldx, rule, W, N, y, y_dtype, ldy, workspace, stream=None, W_bytes=None, workspace_bytes=None) -> None:
+    _check(_lib.ssg_mx4_linear(_ptr(x), x_dtype, M, K, ldx, rule, _ptr(W), _nbytes(W, W_bytes), N, _ptr(y), y_dtype, ldy, _ptr(workspace),
+                               _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def ssg_mx4_linear_bwd_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(_lib.ssg_mx4_linear_bwd_workspace_bytes(M, N, K))
+
+
+def ssg_mx4_linear_bwd(dy, dy_dtype, lddy, x, x_dtype, ldx, M, N, K, rule, Wt, dx, dx_dtype, lddx, dW, dw_dtype, lddw, workspace, stream=None,
+                       Wt_bytes=None, workspace_bytes=None) -> None:
+    _check(_lib.ssg_mx4_linear_bwd(_ptr(dy), dy_dtype, lddy, _ptr(x), x_dtype, ldx, M, N, K, rule, _ptr(Wt), _nbytes(Wt, Wt_bytes), _ptr(dx), dx_dtype,
+                                   lddx, _ptr(dW), dw_dtype, lddw, _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+def make_rmsnorm_desc(T, d, eps, x_dtype=SSG_BF16, residual=0, r_dtype=SSG_BF16, w_dtype=SSG_BF16, w_offset=0.0, y_format=SSG_NORM_BF16, ldx=None,
+                      ldr=None, ldy=None, rule=SSG_MX_FLOOR) -> ssg_rmsnorm_desc:
+    ldx, ldr, ldy = (d if ld is None else ld for ld in (ldx, ldr, ldy))
+    return ssg_rmsnorm_desc(T, d, ldx, ldr, ldy, x_dtype, r_dtype, w_dtype, residual, y_format, rule, eps, w_offset, (c_int32 * 2)(0, 0))
+
+
+def ssg_rmsnorm_fwd(desc, x, residual, w, residual_out, y, y_scale, y_amax, rstd, stream=None, y_bytes=None) -> None:
+    _check(_lib.ssg_rmsnorm_fwd(ctypes.byref(desc), _ptr(x), _ptr(residual), _ptr(w), _ptr(residual_out), _ptr(y), _nbytes(y, y_bytes), _ptr(y_scale),
+                                _ptr(y_amax), _ptr(rstd), _stream(stream)))
+
+
+def ssg_rmsnorm_bwd_workspace_bytes(desc) -> int:
+    return int(_lib.ssg_rmsnorm_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def ssg_rmsnorm_bwd(desc, dy, dy_dtype, lddy, s, rstd, w, ds, dx, dresidual, dw, workspace, stream=None, workspace_bytes=None) -> None:
+    _check(_lib.ssg_rmsnorm_bwd(ctypes.byref(desc), _ptr(dy), dy_dtype, lddy, _ptr(s), _ptr(rstd), _ptr(w), _ptr(ds), _ptr(dx), _ptr(dresidual), _ptr(dw),
+                                _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
 
 
 def view_tensor(saved, base_ptr: int, field_ptr: int, shape, dtype):

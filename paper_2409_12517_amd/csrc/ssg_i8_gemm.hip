@@ -11,6 +11,7 @@
 
 #include "ssg_gemm_tile.h"
 #include "ssg_i8.h"
+#include "ssg_lds_load.h"
 
 namespace ssg {
 
@@ -69,34 +70,6 @@ __device__ __forceinline__ void scaled4(const v4i_t &acc, float sa, const float4
     v[1] = __fmul_rn(__fmul_rn((float)acc[1], sa), sb.y);
     v[2] = __fmul_rn(__fmul_rn((float)acc[2], sa), sb.z);
     v[3] = __fmul_rn(__fmul_rn((float)acc[3], sa), sb.w);
-}
-
-// f(0) to f(N - 1), the numbers as constants
-template <int N, int I = 0, class F> __device__ __forceinline__ void each(F &&f) {
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>{});
-        each<N, I + 1>(f);
-    }
-}
-
-// A load of 16 bytes a lane to LDS in two statements, with an MFMA or two between them, which hide one or two other instructions each and
-// no more: where in LDS (M0, which nothing else here uses), then the load, from a wave-uniform base and 32-bit offsets.  `no`: not if it
-// is 1 (wave-uniform; the branch is inside the statement, so that the code around it stays one block).
-template <int OFF> __device__ __forceinline__ void dma_to(uint32_t lds_addr) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_add_u32 m0, %0, %1" :: "s"(lds_addr), "n"(OFF) : "m0", "scc");
-#endif
-}
-__device__ __forceinline__ void dma_from(const uint8_t *base_uniform, uint32_t lane_off) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("global_load_lds_dwordx4 %0, %1" :: "v"(lane_off), "s"(base_uniform) : "memory");
-#endif
-}
-__device__ __forceinline__ void dma_from_unless(int no, const uint8_t *base_uniform, uint32_t lane_off) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_cmp_lg_u32 %2, 0\n\ts_cbranch_scc1 1f\n\tglobal_load_lds_dwordx4 %0, %1\n1:"
-                 :: "v"(lane_off), "s"(base_uniform), "s"(no) : "memory", "scc");
-#endif
 }
 
 // ---- tiles through LDS -----------------------------------------------------------------------------------

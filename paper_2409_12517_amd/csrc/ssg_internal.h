@@ -386,4 +386,80 @@ bool i8_token_ok(int64_t T, int64_t N, int64_t K);
 bool i8_mix_ok(int64_t T, int64_t d, int64_t f, int k);
 constexpr int kTagRoute = 48, kTagDispatch = 49, kTagRouteBwd = 50, kTagCombine = 51, kTagI8Rows = 52, kTagI8Gemm = 53, kTagI8Swiglu = 54;
 
+// ---- microscaled 4-bit floating point (ssg_mx4_rows.hip, ssg_mx4_gemm.hip) --------------
+// Codes lie in blocks of 16 rows by 128 codes of K, 1 KB each, a row of blocks after the other, K filled up with zeros to 256, an even number of
+// blocks: code (r, k) is a half (the low one for even k) of byte ((r / 16) * (Kp / 128) + k / 128) * 1024 + (k % 128 / 32) * 256 + (r % 16) * 16 +
+// k % 32 / 2, which is the order in which the 64 lanes of a wave hold the operand of v_mfma_scale_f32_16x16x128_f8f6f4, 32 codes with one
+// scale each.  Behind them the scales, a byte each, those of two blocks side by side: of (r, k) at ((r / 16) * (Kp / 256) + k / 256) * 128 +
+// ((k % 128 / 32) * 16 + r % 16) * 2 + k % 256 / 128.
+constexpr int64_t mx4_width(int64_t K) { return i8_up(K, 256); }
+constexpr int64_t mx4_code_bytes(int64_t rows, int64_t K) { return i8_up(rows, 16) * (mx4_width(K) / 2); }      // a multiple of 2 KB
+constexpr int64_t mx4_scale_bytes(int64_t rows, int64_t K) { return i8_up(rows, 16) * (mx4_width(K) / 32); }
+struct Mx4RowsArgs {
+    const void *src = nullptr;       // rows of K, `ld` elements apart; transposed: K rows of `rows`
+    uint8_t *codes = nullptr, *scales = nullptr;
+    int64_t rows = 0, K = 0, ld = 0;
+    int bf16 = 0, transposed = 0, ceil = 0;
+};
+void launch_mx4_quantize(const Mx4RowsArgs &a, hipStream_t st);
+struct Mx4ValuesArgs {
+    const uint8_t *codes = nullptr, *scales = nullptr;
+    void *dst = nullptr;
+    int64_t rows = 0, K = 0, ld = 0;
+    int bf16 = 0;
+};
+void launch_mx4_dequantize(const Mx4ValuesArgs &a, hipStream_t st);
+// row-major codes, two to a byte, and scales into the layout and back
+void launch_mx4_pack(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t K, uint8_t *out, uint8_t *out_scales, hipStream_t st);
+void launch_mx4_unpack(const uint8_t *in, const uint8_t *in_scales, int64_t rows, int64_t K, uint8_t *codes, uint8_t *scales, hipStream_t st);
+struct Mx4GemmArgs {
+    const uint8_t *A = nullptr, *B = nullptr, *sa = nullptr, *sb = nullptr;
+    void *C = nullptr;
+    int64_t M = 0, N = 0, K = 0, ldc = 0;
+    int c_f32 = 0;
+};
+I8Plan mx4_gemm_plan(const Mx4GemmArgs &a);
+void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st);
+// up to kMx4TokenRows rows of x, quantized in the product's own kernel
+constexpr int kMx4TokenRows = 4;
+struct Mx4TokenArgs {
+    const void *x = nullptr;         // rows of K, `ld` elements apart
+    const uint8_t *B = nullptr, *sb = nullptr;
+    void *C = nullptr;
+    int64_t N = 0, K = 0, ld = 0, ldc = 0;
+    int rows = 1, bf16 = 0, c_f32 = 0, ceil = 0;
+};
+bool mx4_token_ok(int64_t M, int64_t N, int64_t K);
+void launch_mx4_token(const Mx4TokenArgs &a, hipStream_t st);
+constexpr int kTagMx4Rows = 55, kTagMx4Gemm = 56, kTagNorm = 57, kTagNormBwd = 58;
+
+// ---- root-mean-square norm (ssg_norm.hip) ---------------------------------------------
+enum NormForm { NORM_BF16 = 0, NORM_F32 = 1, NORM_E4M3 = 2, NORM_I8 = 3, NORM_MX4 = 4 };       // as in ssg_norm_format
+constexpr int64_t kMaxNormWidth = 32768;
+struct NormArgs {
+    const void *x = nullptr, *r = nullptr, *w = nullptr;     // rows of d; r: the residual or null; w: [d] or null
+    void *r_out = nullptr;           // r + x in r's type
+    void *y = nullptr;               // rows, or codes in the layout of the products
+    void *y_scales = nullptr;        // NORM_I8, NORM_MX4: the layout's scales
+    const float *y_scale = nullptr;  // NORM_E4M3: the given scale
+    float *amax = nullptr;           // NORM_E4M3: [T] or null
+    float *rstd = nullptr;           // [T] or null
+    int64_t T = 0, d = 0, ldx = 0, ldr = 0, ldy = 0;
+    int x_bf16 = 0, r_bf16 = 0, w_bf16 = 0, form = 0, ceil = 0;
+    float eps = 0, w_offset = 0;
+};
+void launch_norm(const NormArgs &a, hipStream_t st);
+struct NormBwdArgs {
+    const void *dy = nullptr, *s = nullptr, *ds = nullptr, *w = nullptr;     // s: the normed rows; ds, of s's type: the gradient that comes to them beside, or null
+    const float *rstd = nullptr;
+    void *dx = nullptr, *dr = nullptr;   // either or both; dr of s's type
+    float *dw = nullptr;             // [d] or null
+    float *partial = nullptr;        // norm_bwd_blocks(T, d) rows of d
+    int64_t T = 0, d = 0, lddy = 0, lds = 0, lddx = 0;       // lds: of s, ds and dr
+    int dy_bf16 = 0, s_bf16 = 0, dx_bf16 = 0, w_bf16 = 0;
+    float w_offset = 0;
+};
+int64_t norm_bwd_blocks(int64_t T, int64_t d);
+void launch_norm_bwd(const NormBwdArgs &a, hipStream_t st);
+
 }  // namespace ssg
