@@ -35,6 +35,13 @@ template <int STEP> __device__ __forceinline__ v4f_t mfma_mx4(const v4i_t &w, ui
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, kE2M1, kE2M1, STEP, (int)sw, STEP, (int)sx);
 }
 
+// The same of 32 x 32: a lane holds row l & 31 of C and, in its sixteen registers i, columns 8 (i / 4) + 4 (l >> 5) + i % 4.
+template <int STEP> __device__ __forceinline__ v16f mfma_mx4_wide(const v4i_t &w, uint32_t sw, const v4i_t &x, uint32_t sx, const v16f &c) {
+    constexpr int kE2M1 = 4;
+    const v8i a = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, b = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, kE2M1, kE2M1, STEP, (int)sw, STEP, (int)sx);
+}
+
 // Tile number v of rows * tiles_n: the column tiles of one row tile after the other in groups of four row tiles, and eight contiguous
 // ranges of that order for the eight XCDs.
 struct Mx4Tile { int rb, cb; };                          // first row block and column block
@@ -55,61 +62,83 @@ __device__ __forceinline__ void store4(const Mx4Params &p, int64_t row, int64_t 
 }
 
 // ---- tiles through LDS -----------------------------------------------------------------------------------
-// 4 waves as 2 x 2, RB x RB blocks of 16 x 16 each (RB = 8: 256 x 256, one workgroup to a compute unit; RB = 4: 128 x 128, two).
-// K advances in steps of 128 through a ring of four stages.  The fragments of a step are read while the step before it is
-// multiplied, so when all waves have passed the barrier at the start of step k the stage of step k is free, and k + 4 is loaded into it.
-// Two steps are a pair, whose scales go through a ring of their own, of three pairs: loaded before the pair's first stage, read into registers in
-// the step before the pair.
+// 4 waves as 2 x 2, TA x TB blocks of 32 x 32 each.
+// Products of 32 x 32 x 64, which reach the chip's rate where 16 x 16 x 128 wait on their issue (registers alone, one wave to a SIMD, random codes: 6.2
+// and 4.2 PFLOP/s): a fragment is the blocks of two neighbouring 16 rows, half of each along K.
+// K advances in steps of 128 through a ring of kStages stages, each in two halves of 64.  The fragments of a half are read while the half before it is
+// multiplied, so when all waves have passed the barrier in the middle of step k, everything of its stage is in registers, and k + kStages is loaded
+// into it.  Two steps are a pair, whose scales go through a ring of their own, of two pairs: loaded before the pair's first stage, read into
+// registers, those of either half while the other half is multiplied.
 // A workgroup has several tiles one after the other and the rings run on from one to the next: while a tile's last steps are
 // multiplied and its results stored, the first stages of the next are on their way.  A tile with no more rows than half
-// loads and multiplies half of them: 4 by 8 blocks to a wave.
-constexpr int kStages = 4, kScaleSlots = 3;
-template <int WB> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void mx4_tile_kernel(Mx4Params p) {
-    constexpr int RB = 2 * WB, kBlocks = 4 * WB;         // blocks of 16 rows, or columns, of a wave and of the tile
-    constexpr int kStage = 2 * kBlocks * 1024, kRing = kStages * kStage;
-    constexpr int kPatch = 16 * (64 * WB + 16);          // of a wave: 16 rows of 64 WB bytes
-    constexpr int kScales = 2 * kBlocks * 128;           // of a pair: the rows', then the columns'
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[kRing + 4 * kPatch + kScaleSlots * kScales];
+// loads and multiplies half of them.
+constexpr int kScaleSlots = 2;
+template <int TA, int TB, int STAGES> struct TileShape {
+    static constexpr int kA = 4 * TA, kB = 4 * TB;       // blocks of 16 rows, and of 16 columns, of the tile
+    static constexpr int kRows = 16 * kA, kCols = 16 * kB, kStage = (kA + kB) * 1024, kRing = STAGES * kStage;
+    static constexpr int kScales = (kA + kB) * 128;      // of a pair: the rows', then the columns'
+    static constexpr int kLds = kRing + kScaleSlots * kScales, kAtOnce = 163840 / kLds;
+};
+// wait_dma, unless `no` is above zero (wave-uniform)
+template <int N> __device__ __forceinline__ void wait_dma_unless(int no) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_cmp_gt_i32 %1, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(%0)\n1:" :: "n"(N), "s"(no) : "memory", "scc");
+#endif
+}
+// a's lanes 32 to 63 for b's lanes 0 to 31; of each 32, a's lanes 16 to 31 for b's 0 to 15
+__device__ __forceinline__ void swap32(uint32_t &a, uint32_t &b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0]; b = r[1];
+}
+__device__ __forceinline__ void swap16(uint32_t &a, uint32_t &b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0]; b = r[1];
+}
+
+template <int TA, int TB, int STAGES> __global__ __launch_bounds__(256, (TileShape<TA, TB, STAGES>::kAtOnce)) void mx4_tile_kernel(Mx4Params p) {
+    using Shape = TileShape<TA, TB, STAGES>;
+    constexpr int kA = Shape::kA, kB = Shape::kB, kStage = Shape::kStage, kRing = Shape::kRing, kScales = Shape::kScales;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[Shape::kLds];
     const int row_blocks = (int)((p.M + 15) / 16), col_blocks = (int)(p.N / 16);
-    const int rows = (row_blocks + kBlocks - 1) / kBlocks, all = rows * p.tiles_n;
+    const int rows = (row_blocks + kA - 1) / kA, all = rows * p.tiles_n;
     int v = blockIdx.x;
     if (v >= all) return;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w >> 1, wn = w & 1;
     const int lane_id = tid & 63;
     const int KB = p.KB;
     const uint32_t smem_base = (uint32_t)(uintptr_t)(lds_void_ptr)smem;
-    const uint32_t b_dst = smem_base + (kBlocks + w * WB) * 1024u;
-    // The scales that this wave loads, eight blocks' of a pair: rows' (waves 0 and 1) or columns' (2 and 3).  (A small tile has eight blocks of
-    // each, which two waves load both, the same bytes to the same place.)
-    const bool s_cols = w >= 2;
-    const int s_first = WB == 4 ? (w & 1) * 8 : 0;
-    const uint32_t s_dst = smem_base + kRing + 4 * kPatch + ((s_cols ? kBlocks : 0) + s_first) * 128u;
+    const uint32_t b_dst = smem_base + (kA + w * TB) * 1024u;
+    // The scales that this wave loads, those of eight blocks of a pair, rows or columns (where there are fewer than four times eight, the last waves load
+    // the same bytes to the same place).
+    constexpr int kPieces = (kA + kB) / 8;
+    const int piece = w < kPieces ? w : kPieces - 1;
+    const bool s_cols = piece >= kA / 8;
+    const int s_first = s_cols ? (piece - kA / 8) * 8 : piece * 8;
+    const uint32_t s_dst = smem_base + kRing + piece * 1024u;
     // The blocks of a tile that this wave loads: where its first one begins and how far the others are, wave-uniform; beyond the
     // matrix its last one again (not stored).
     struct Source {
         const uint8_t *a, *b, *s;
-        uint32_t a_off[WB], b_off[WB], a_dst, s_last;
+        uint32_t a_off[TA], b_off[TB], a_dst, s_last;
         int half;
     };
     auto source = [&](const Mx4Tile &tile) {
         Source s;
         const int last_r = row_blocks - 1 - tile.rb, last_c = col_blocks - 1 - tile.cb;      // the last ones there are, from the tile's first on
-        s.half = (int)((uint32_t)(last_r - RB) >> 31);       // 1: no more than RB row blocks
-        const int mine = (w * WB) >> s.half;             // the first row block of this wave's
+        s.half = (int)((uint32_t)(last_r - kA / 2) >> 31);   // 1: no more than half of the row blocks
+        const int mine = (w * TA) >> s.half;             // the first row block of this wave's
         s.a_dst = smem_base + mine * 1024u;
         s.a = p.A + (int64_t)tile.rb * KB * 1024;
         s.b = p.B + (int64_t)tile.cb * KB * 1024;
         s.s = s_cols ? p.sb + (int64_t)tile.cb * KB * 64 : p.sa + (int64_t)tile.rb * KB * 64;
         s.s_last = (uint32_t)(s_cols ? last_c : last_r);
 #pragma unroll
-        for (int j = 0; j < WB; ++j) {
-            const int r = mine + j, c = w * WB + j;
-            s.a_off[j] = (uint32_t)(r < last_r ? r : last_r) * (uint32_t)KB * 1024u;
-            s.b_off[j] = (uint32_t)(c < last_c ? c : last_c) * (uint32_t)KB * 1024u;
-        }
+        for (int j = 0; j < TA; ++j) s.a_off[j] = (uint32_t)(mine + j < last_r ? mine + j : last_r) * (uint32_t)KB * 1024u;
+#pragma unroll
+        for (int j = 0; j < TB; ++j) s.b_off[j] = (uint32_t)(w * TB + j < last_c ? w * TB + j : last_c) * (uint32_t)KB * 1024u;
         return s;
     };
-    Mx4Tile tile = find_tile(p, kBlocks, kBlocks, rows, v), next_tile = tile;
+    Mx4Tile tile = find_tile(p, kA, kB, rows, v), next_tile = tile;
     Source src = source(tile), next_src = src;
     auto scalar = [](const Source &s) {
         auto u32 = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
@@ -122,10 +151,9 @@ template <int WB> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void mx4_ti
         r.b = ptr(s.b);
         r.s = ptr(s.s);
 #pragma unroll
-        for (int j = 0; j < WB; ++j) {
-            r.a_off[j] = u32(s.a_off[j]);
-            r.b_off[j] = u32(s.b_off[j]);
-        }
+        for (int j = 0; j < TA; ++j) r.a_off[j] = u32(s.a_off[j]);
+#pragma unroll
+        for (int j = 0; j < TB; ++j) r.b_off[j] = u32(s.b_off[j]);
         r.a_dst = u32(s.a_dst);
         r.s_last = u32(s.s_last);
         r.half = (int)u32((uint32_t)s.half);
@@ -138,13 +166,12 @@ template <int WB> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void mx4_ti
         asm volatile("" : "+v"(l));
         return l;
     };
-    uint32_t a_lane[WB], b_lane[WB], s_lane;             // lane offsets of the blocks of `src`
+    uint32_t a_lane[TA], b_lane[TB], s_lane;             // lane offsets of the blocks of `src`
     auto take_lanes = [&]() {
 #pragma unroll
-        for (int j = 0; j < WB; ++j) {
-            a_lane[j] = lane + src.a_off[j];
-            b_lane[j] = lane + src.b_off[j];
-        }
+        for (int j = 0; j < TA; ++j) a_lane[j] = lane + src.a_off[j];
+#pragma unroll
+        for (int j = 0; j < TB; ++j) b_lane[j] = lane + src.b_off[j];
         const uint32_t block = (uint32_t)(s_first + lane_id / 8);
         s_lane = (block < src.s_last ? block : src.s_last) * (uint32_t)KB * 64u + (lane_id & 7) * 16;
     };
@@ -152,14 +179,14 @@ template <int WB> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void mx4_ti
     // load j of a stage into `slot`: where to, and the load
     auto issue_to = [&](auto which, uint32_t slot) {
         constexpr int j = decltype(which)::value;
-        if (j < WB) dma_to<j * 1024>(src.a_dst + slot);
-        else dma_to<(j - WB) * 1024>(b_dst + slot);
+        if (j < TA) dma_to<j * 1024>(src.a_dst + slot);
+        else dma_to<(j - TA) * 1024>(b_dst + slot);
     };
     auto issue_from = [&](auto which) {
         constexpr int j = decltype(which)::value;
-        if constexpr (j < WB / 2) dma_from(src.a, a_lane[j]);
-        else if constexpr (j < WB) dma_from_unless(src.half, src.a, a_lane[j]);
-        else dma_from(src.b, b_lane[j - WB]);
+        if constexpr (j < TA / 2) dma_from(src.a, a_lane[j]);
+        else if constexpr (j < TA) dma_from_unless(src.half, src.a, a_lane[j]);
+        else dma_from(src.b, b_lane[j - TA]);
     };
     // the scales of the pair whose first stage is loaded next
     auto issue_scales = [&](uint32_t scale_slot) {
@@ -168,12 +195,7 @@ template <int WB> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void mx4_ti
         dma_from(src.s, s_lane);
         src.s += 128;
     };
-    auto later = [](uint32_t scale_slot, int by) {
-        const uint32_t at = scale_slot + by * kScales;
-        return at >= kScaleSlots * kScales ? at - kScaleSlots * kScales : at;
-    };
-    constexpr int kLoads = 2 * WB, kFewest = kLoads - WB / 2;            // of a stage; where the tile is half of one
-    static_assert(kLoads == RB, "a load to every column of blocks");
+    constexpr int kLoads = TA + TB, kFewest = kLoads - TA / 2;           // of a stage; where the tile is half of one
     // After the last stage of this tile come those of the next one (of the last tile's: the same again, which nothing reads).
     // Their number is even, so that it is asked for after every second one.
     int loaded = 0;
@@ -184,12 +206,11 @@ template <int WB> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void mx4_ti
             loaded = 0;
         }
     };
-    uint8_t *patch = smem + kRing + w * kPatch;
     // the next tile, known before the loads come to it
     auto look_ahead = [&]() {
         const int n = v + (int)gridDim.x;
         if (n < all) {
-            next_tile = find_tile(p, kBlocks, kBlocks, rows, n);
+            next_tile = find_tile(p, kA, kB, rows, n);
             next_src = source(next_tile);
         } else {
             next_src = source(tile);
@@ -197,7 +218,7 @@ template <int WB> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void mx4_ti
     };
     look_ahead();
 #pragma unroll
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < STAGES; ++s) {
         if (s % 2 == 0) issue_scales(s / 2 * kScales);
         each<kLoads>([&](auto j) {
             issue_to(j, s * kStage);
@@ -209,114 +230,167 @@ template <int WB> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void mx4_ti
         if (s % 2 == 1) two_loaded();
     }
     uint32_t slot = 0, scale_slot = 0;                   // of this step's stage; of this pair's scales
-    wait_dma<(kStages - 1) * kFewest + 1>();             // stage 0 and the scales before it (those of the second pair came later)
+    wait_dma<(STAGES - 1) * kFewest + 1>();              // stage 0 and the scales before it (those of the second pair came later)
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    // One tile, RA row blocks to a wave.
-    auto run_tile = [&](auto row_blocks_of_wave) {
-        constexpr int RA = decltype(row_blocks_of_wave)::value;
-        v4f_t acc[RA][RB];
-        v4i_t fa[2][RA], fb[2][RB];
-        uint32_t xa[RA], xb[RB], next_xa[RA], next_xb[RB];
-        const uint8_t *a_frag = smem + wm * RA * 1024 + lane, *b_frag = smem + (kBlocks + wn * RB) * 1024 + lane;
-        const uint8_t *a_scale = smem + kRing + 4 * kPatch + wm * RA * 128 + lane_id * 2, *b_scale = smem + kRing + 4 * kPatch + (kBlocks + wn * RB) * 128 + lane_id * 2;
-        // fragment i in the order of use: the first column's and the rows', then the other columns'
-        auto read_one = [&](int set, int i, uint32_t slot) {
-            if (i >= 1 && i <= RA) fa[set][i - 1] = *reinterpret_cast<const v4i_t *>(a_frag + slot + (i - 1) * 1024);
-            else fb[set][i == 0 ? 0 : i - RA] = *reinterpret_cast<const v4i_t *>(b_frag + slot + (i == 0 ? 0 : i - RA) * 1024);
+    // Steps of a tile whose wait there is none for: before the last tile's results were stored, all that was loaded had landed.  (A wait for a
+    // load waits for the older stores, too, so those get the time of these steps.)
+    int waited = 0;
+    // One tile, QA blocks of 32 rows to a wave.
+    auto run_tile = [&](auto blocks_of_wave) {
+        constexpr int QA = decltype(blocks_of_wave)::value, QB = TB;
+        v16f acc[QA][QB];
+        v4i_t fa[2][QA], fb[2][QB];                      // of the two halves
+        uint32_t xa[2][QA], xb[2][QB];
+        // lanes 0 to 15 and 32 to 47 have the first block's rows, 16 to 31 and 48 to 63 the second's; the upper half of the lanes the next run of 32
+        const int l16 = lane_id & 15, lhi = lane_id >> 4 & 1, run = lane_id >> 5;
+        const uint32_t frag_lane = lhi * 1024 + run * 256 + l16 * 16, scale_lane = lhi * 128 + (run * 16 + l16) * 2;
+        const uint8_t *a_frag = smem + wm * QA * 2048 + frag_lane, *b_frag = smem + (kA + wn * 2 * TB) * 1024 + frag_lane;
+        const uint8_t *a_scale = smem + kRing + wm * QA * 256 + scale_lane, *b_scale = smem + kRing + (kA + wn * 2 * TB) * 128 + scale_lane;
+        // fragment i of a half in the order of use: the first column's and the rows', then the other columns'
+        auto read_one = [&](int half, int i, uint32_t slot) {
+            if (i >= 1 && i <= QA) fa[half][i - 1] = *reinterpret_cast<const v4i_t *>(a_frag + slot + half * 512 + (i - 1) * 2048);
+            else fb[half][i == 0 ? 0 : i - QA] = *reinterpret_cast<const v4i_t *>(b_frag + slot + half * 512 + (i == 0 ? 0 : i - QA) * 2048);
         };
-        auto read_scale = [&](int i, uint32_t slot) {
-            if (i < RA) next_xa[i] = *reinterpret_cast<const uint16_t *>(a_scale + slot + i * 128);
-            else next_xb[i - RA] = *reinterpret_cast<const uint16_t *>(b_scale + slot + (i - RA) * 128);
+        auto read_scale = [&](int half, int i, uint32_t slot) {
+            if (i < QA) xa[half][i] = *reinterpret_cast<const uint16_t *>(a_scale + slot + half * 64 + i * 256);
+            else xb[half][i - QA] = *reinterpret_cast<const uint16_t *>(b_scale + slot + half * 64 + (i - QA) * 256);
         };
-        auto take_scales = [&]() {
-#pragma unroll
-            for (int i = 0; i < RA; ++i) xa[i] = next_xa[i];
-#pragma unroll
-            for (int i = 0; i < RB; ++i) xb[i] = next_xb[i];
-        };
-        auto step = [&](auto parity) {
-            constexpr int set = decltype(parity)::value;
-            const uint32_t next = slot == (kStages - 1) * kStage ? 0 : slot + kStage;
-            wait_dma<(kStages - 2) * kFewest + 1>();         // the next step's stage has landed, and what came before it (of two stages one brings scales)
-            __builtin_amdgcn_s_waitcnt(0xC07F);              // this step's fragments are here
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_sched_barrier(0);
-            if (set == 0) issue_scales(later(scale_slot, 2));
-            const uint32_t next_scales = later(scale_slot, 1);
-            constexpr int kEvery = RA * RB / (RA + RB);      // MFMAs to a fragment read
-            each<RA * RB>([&](auto at) {
-                constexpr int t = decltype(at)::value, c = t / RA, r = c & 1 ? RA - 1 - t % RA : t % RA;
-                acc[r][c] = mfma_mx4<set>(fb[set][c], xb[c], fa[set][r], xa[r], acc[r][c]);
-                if (t % kEvery == 0 && t / kEvery < RA + RB) {
-                    read_one(set ^ 1, t / kEvery, next);
-                    if (set == 1) read_scale(t / kEvery, next_scales);
-                }
-                if (t % RA == (RA > 4 ? 1 : 0)) issue_to(std::integral_constant<int, t / RA>{}, slot);
-                if (t % RA == (RA > 4 ? 2 : 1)) issue_from(std::integral_constant<int, t / RA>{});
+        // One half of a step; `other`: what is read and loaded between the MFMAs.
+        auto multiply = [&](auto parity, auto half, auto &&other) {
+            constexpr int P = decltype(parity)::value, H = decltype(half)::value;
+            each<QA * QB>([&](auto at) {
+                constexpr int t = decltype(at)::value, c = t / QA, r = c & 1 ? QA - 1 - t % QA : t % QA;
+                acc[r][c] = mfma_mx4_wide<P>(fb[H][c], xb[H][c], fa[H][r], xa[H][r], acc[r][c]);
+                other(at);
                 __builtin_amdgcn_sched_barrier(0);
             });
+        };
+        constexpr int kMfmas = QA * QB, kReads = QA + QB, kReadsEach = (kReads + kMfmas - 1) / kMfmas, kLoadsEach = (kLoads + kMfmas - 1) / kMfmas;
+        auto step = [&](auto parity) {
+            constexpr int P = decltype(parity)::value;
+            const uint32_t next = slot == (STAGES - 1) * kStage ? 0 : slot + kStage, next_scales = scale_slot ^ kScales;
+            multiply(parity, std::integral_constant<int, 0>{}, [&](auto at) {
+                constexpr int t = decltype(at)::value;
+#pragma unroll
+                for (int i = t * kReadsEach; i < (t + 1) * kReadsEach && i < kReads; ++i) {
+                    read_one(1, i, slot);
+                    if (P == 0) read_scale(1, i, scale_slot);
+                }
+            });
+            // the next step's stage has landed, and the scales before it: of the stages after it those of even number bring scales
+            wait_dma_unless<(STAGES - 2) * kFewest + (STAGES - 2 + (P == 0)) / 2>(waited);
+            --waited;
+            __builtin_amdgcn_s_waitcnt(0xC07F);              // all of this step's fragments are here
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            if (P == STAGES % 2) issue_scales(scale_slot);
+            multiply(parity, std::integral_constant<int, 1>{}, [&](auto at) {
+                constexpr int t = decltype(at)::value;
+#pragma unroll
+                for (int i = t * kReadsEach; i < (t + 1) * kReadsEach && i < kReads; ++i) {
+                    read_one(0, i, next);
+                    if (P == 1) read_scale(0, i, next_scales);
+                }
+                if constexpr (kMfmas >= 2 * kLoads) {
+                    if constexpr (t % 2 == 0 && t / 2 < kLoads) issue_to(std::integral_constant<int, t / 2>{}, slot);
+                    if constexpr (t % 2 == 1 && t / 2 < kLoads) issue_from(std::integral_constant<int, t / 2>{});
+                } else {
+                    each<kLoadsEach>([&](auto i) {
+                        constexpr int j = t * kLoadsEach + decltype(i)::value;
+                        if constexpr (j < kLoads) {
+                            issue_to(std::integral_constant<int, j>{}, slot);
+                            asm volatile("s_nop 0");
+                            issue_from(std::integral_constant<int, j>{});
+                        }
+                    });
+                }
+            });
+            // (else the compiler moves all the MFMAs, whose results nothing else in the block reads, behind the block's reads and loads)
+#pragma unroll
+            for (int r = 0; r < QA; ++r)
+#pragma unroll
+                for (int c = 0; c < QB; ++c) {
+                    if (TA * TB > 8) asm volatile("" : "+a"(acc[r][c]));
+                    else asm volatile("" : "+v"(acc[r][c]));
+                }
             src.a += 1024;
             src.b += 1024;
             slot = next;
-            if (set == 1) {
-                take_scales();
-                scale_slot = next_scales;
-            }
+            if (P == 1) scale_slot = next_scales;
+            if (P != STAGES % 2) two_loaded();
         };
-        // 16 rows at a time go through the patch, so that rows leave in pieces of 16 bytes side by side
+        // A lane has row l % 32 of a block and of each eight columns four, those from 4 (l / 32) on.  Exchanged between lanes until one store takes 64 bytes of
+        // each of 16 rows.
         auto store = [&](auto f32) {
             const int l = lane_now();
             constexpr bool F32 = decltype(f32)::value;
-            constexpr int kSize = F32 ? 4 : 2, kRowBytes = RB * 16 * kSize < 64 * WB ? RB * 16 * kSize : 64 * WB;
-            constexpr int kPitch = kRowBytes + 16, kPart = kRowBytes / (16 * kSize);             // column blocks at a time
-            constexpr int kLanes = kRowBytes / 16, kAtOnce = 64 / kLanes;        // lanes to a row, rows to a store
-            static_assert(16 * kPitch <= kPatch && RB % kPart == 0, "a part of the columns fits the patch");
+            const int piece_of_lane = (l >> 4 & 1) * 2 + (l >> 5);
 #pragma unroll
-            for (int r = 0; r < RA; ++r) {
-                const int rb = tile.rb + wm * RA + r;
-                if (rb >= row_blocks) break;
+            for (int r = 0; r < QA; ++r) {
+                const int64_t row0 = (int64_t)(tile.rb + (wm * QA + r) * 2) * 16;
+                if (row0 >= p.M) break;
 #pragma unroll
-                for (int c0 = 0; c0 < RB; c0 += kPart) {
-                    const int64_t col0 = (int64_t)(tile.cb + wn * RB + c0) * 16 + (l % kLanes) * (16 / kSize);
+                for (int c = 0; c < QB; ++c) {
+                    const int64_t col0 = (int64_t)(tile.cb + (wn * TB + c) * 2) * 16;
+                    auto put = [&](int64_t row, int64_t col, const uint32_t (&q)[4]) {
+                        if (row < p.M && col < p.N)
+                            *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.C) + (row * p.ldc + col) * (F32 ? 4 : 2)) = make_uint4(q[0], q[1], q[2], q[3]);
+                    };
+                    if constexpr (F32) {
 #pragma unroll
-                    for (int c = c0; c < c0 + kPart; ++c) {
-                        const v4f_t x = acc[r][c];
-                        uint8_t *at = patch + (l & 15) * kPitch + ((c - c0) * 16 + (l >> 4) * 4) * kSize;
-                        if (F32) *reinterpret_cast<float4 *>(at) = make_float4(x[0], x[1], x[2], x[3]);
-                        else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-                    }
+                        for (int i = 0; i < 16; i += 8) {        // columns 2 i .. 2 i + 15
+                            uint32_t x[4], y[4];
 #pragma unroll
-                    for (int i = 0; i < 16 / kAtOnce; ++i) {
-                        const int at = i * kAtOnce + l / kLanes;
-                        const uint4 x = *reinterpret_cast<const uint4 *>(patch + at * kPitch + l % kLanes * 16);
-                        const int64_t row = (int64_t)rb * 16 + at;
-                        if (row < p.M && col0 < p.N) *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.C) + (row * p.ldc + col0) * kSize) = x;
+                            for (int j = 0; j < 4; ++j) {
+                                x[j] = __float_as_uint(acc[r][c][i + j]);
+                                y[j] = __float_as_uint(acc[r][c][i + 4 + j]);
+                                swap16(x[j], y[j]);
+                            }
+                            put(row0 + (l & 15), col0 + 2 * i + piece_of_lane * 4, x);
+                            put(row0 + 16 + (l & 15), col0 + 2 * i + piece_of_lane * 4, y);
+                        }
+                    } else {
+                        uint32_t x[4], y[4];                     // of columns 0 to 15 and 16 to 31
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            x[j] = pack_bf16x2(acc[r][c][2 * j], acc[r][c][2 * j + 1]);
+                            x[2 + j] = pack_bf16x2(acc[r][c][4 + 2 * j], acc[r][c][4 + 2 * j + 1]);
+                            y[j] = pack_bf16x2(acc[r][c][8 + 2 * j], acc[r][c][8 + 2 * j + 1]);
+                            y[2 + j] = pack_bf16x2(acc[r][c][12 + 2 * j], acc[r][c][12 + 2 * j + 1]);
+                            swap32(x[j], x[2 + j]);
+                            swap32(y[j], y[2 + j]);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) swap16(x[j], y[j]);
+                        put(row0 + (l & 15), col0 + piece_of_lane * 8, x);
+                        put(row0 + 16 + (l & 15), col0 + piece_of_lane * 8, y);
                     }
                 }
             }
         };
 #pragma unroll
-        for (int r = 0; r < RA; ++r)
+        for (int r = 0; r < QA; ++r)
 #pragma unroll
-            for (int c = 0; c < RB; ++c) {
-                acc[r][c] = v4f_t{0, 0, 0, 0};
+            for (int c = 0; c < QB; ++c) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
                 // (else the compiler knows the zeros, has them in both halves of the register file and moves accumulators about in every step)
-                if (WB == 4) asm volatile("" : "+a"(acc[r][c]));
+                if (TA * TB > 8) asm volatile("" : "+a"(acc[r][c]));
             }
         // (read again, though the last step of the tile before has, so that no fragments are kept across the epilogue)
 #pragma unroll
-        for (int i = 0; i < RA + RB; ++i) {
+        for (int i = 0; i < kReads; ++i) {
             read_one(0, i, slot);
-            read_scale(i, scale_slot);
+            read_scale(0, i, scale_slot);
         }
-        take_scales();
 #pragma nounroll
         for (int k = 0; k < KB; k += 2) {
             step(std::integral_constant<int, 0>{});
             step(std::integral_constant<int, 1>{});
-            two_loaded();
         }
+        wait_dma<0>();
+        waited = STAGES - 1;
         if (p.c_f32) store(std::true_type{});
         else store(std::false_type{});
     };
@@ -327,9 +401,10 @@ template <int WB> __global__ __launch_bounds__(256, WB == 4 ? 1 : 2) void mx4_ti
         slot = (uint32_t)__builtin_amdgcn_readfirstlane((int)slot);
         scale_slot = (uint32_t)__builtin_amdgcn_readfirstlane((int)scale_slot);
         loaded = __builtin_amdgcn_readfirstlane(loaded);
+        waited = __builtin_amdgcn_readfirstlane(waited);
         v = __builtin_amdgcn_readfirstlane(v);
-        if (__builtin_amdgcn_readfirstlane(row_blocks - tile.rb) <= RB) run_tile(std::integral_constant<int, RB / 2>{});
-        else run_tile(std::integral_constant<int, RB>{});
+        if (__builtin_amdgcn_readfirstlane(row_blocks - tile.rb) <= kA / 2) run_tile(std::integral_constant<int, TA / 2>{});
+        else run_tile(std::integral_constant<int, TA>{});
         v += (int)gridDim.x;
         if (v >= all) break;
         tile = next_tile;
@@ -488,10 +563,10 @@ void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st) {
     // the tiles' workgroups stay, one or two to a compute unit; a tile of no more steps than the ring has stages is a workgroup's only one
     // (its loads would run two tiles ahead)
     constexpr int64_t kAll = (int64_t)1 << 31;
-    const int64_t units = p.KB > kStages ? 256 : kAll;
+    auto units = [&](int stages, int at_once) { return p.KB > stages ? 256 * (int64_t)at_once : kAll; };
     profile_before(kTagMx4Gemm, st);
-    if (form == TILE_256) go(mx4_tile_kernel<4>, 256, 256, 256, units);
-    else if (form == TILE_128) go(mx4_tile_kernel<2>, 128, 128, 256, 2 * units);
+    if (form == TILE_256) go(mx4_tile_kernel<4, 4, 4>, 256, 256, 256, units(4, 1));
+    else if (form == TILE_128) go(mx4_tile_kernel<2, 2, 4>, 128, 128, 256, units(4, 2));
     else if (form == FEW_16) go(mx4_few_kernel<1, 1, 8>, 16, 16, 512, kAll);
     else if (form == FEW_32) go(mx4_few_kernel<2, 1, 4>, 32, 16, 256, kAll);
     else go(mx4_few_kernel<4, 2, 8>, 64, 32, 512, kAll);
