@@ -402,6 +402,8 @@ struct Mx4RowsArgs {
     int bf16 = 0, transposed = 0, ceil = 0;
 };
 void launch_mx4_quantize(const Mx4RowsArgs &a, hipStream_t st);
+// In one launch: the transposes of dy and of x, and the rows of dy where `rows` is not null.
+void launch_mx4_quantize_bwd(const Mx4RowsArgs *rows, const Mx4RowsArgs &dy, const Mx4RowsArgs &x, hipStream_t st);
 struct Mx4ValuesArgs {
     const uint8_t *codes = nullptr, *scales = nullptr;
     void *dst = nullptr;

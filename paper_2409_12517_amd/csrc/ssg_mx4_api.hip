@@ -249,17 +249,14 @@ ssg_status ssg_mx4_linear_bwd(const void *dy, ssg_dtype dy_dtype, int64_t lddy, 
     SSG_CHECK(check_entry(who));
     uint8_t *b = static_cast<uint8_t *>(workspace);
     hipStream_t st = (hipStream_t)stream;
-    if (dx) {
-        ssg::launch_mx4_quantize(rows_args(dy, dy_dtype, M, N, lddy, 0, rule, b + L.dy), st);
-        ssg::launch_mx4_gemm(gemm_args(b + L.dy, M, Wt, K, N, dx, dx_dtype, lddx), st);
-    }
-    if (dW) {
-        if (M > 0) {                                         // (of no rows the product is zero)
-            ssg::launch_mx4_quantize(rows_args(dy, dy_dtype, N, M, lddy, 1, rule, b + L.dy_t), st);
-            ssg::launch_mx4_quantize(rows_args(x, x_dtype, K, M, ldx, 1, rule, b + L.x_t), st);
-        }
-        ssg::launch_mx4_gemm(gemm_args(b + L.dy_t, N, b + L.x_t, K, M, dW, dw_dtype, lddw), st);
-    }
+    const ssg::Mx4RowsArgs rows = rows_args(dy, dy_dtype, M, N, lddy, 0, rule, b + L.dy);
+    if (dW && M > 0)                                         // (of no rows the product is zero)
+        ssg::launch_mx4_quantize_bwd(dx ? &rows : nullptr, rows_args(dy, dy_dtype, N, M, lddy, 1, rule, b + L.dy_t),
+                                     rows_args(x, x_dtype, K, M, ldx, 1, rule, b + L.x_t), st);
+    else if (dx)
+        ssg::launch_mx4_quantize(rows, st);
+    if (dx) ssg::launch_mx4_gemm(gemm_args(b + L.dy, M, Wt, K, N, dx, dx_dtype, lddx), st);
+    if (dW) ssg::launch_mx4_gemm(gemm_args(b + L.dy_t, N, b + L.x_t, K, M, dW, dw_dtype, lddw), st);
     return check_launch(who);
 }
 

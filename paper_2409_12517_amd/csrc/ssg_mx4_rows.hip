@@ -27,67 +27,157 @@ template <bool BF16> __global__ __launch_bounds__(256) void mx4_rows_kernel(Mx4R
     *reinterpret_cast<uint16_t *>(a.scales + (rb * pairs + p) * 128 + l * 2) = (uint16_t)bytes;
 }
 
-// The transpose: a thread has eight columns (four in fp32) of the source and in each half of 256 tokens a run of 32, so that it forms
-// their scales and codes by itself and the codes of its columns, neighbouring rows of the layout, lie side by side.
-template <bool BF16> __global__ __launch_bounds__(256) void mx4_columns_kernel(Mx4RowsArgs a) {
-    constexpr int COLS = BF16 ? 8 : 4;
-    const int64_t pairs = mx4_width(a.K) / 256, across = a.rows / COLS, i = block_of_many() * 256 + threadIdx.x;
-    if (i >= across * pairs * 4) return;
-    const int64_t c0 = i % across * COLS, p = i / across / 4, rb = c0 / 16;
-    const int g = (int)(i / across % 4), r0 = (int)(c0 % 16);
-    const uint8_t *src = static_cast<const uint8_t *>(a.src) + c0 * (BF16 ? 2 : 4);
-    uint32_t bytes[COLS] = {};
+// The transpose, and with it the rows where both are wanted: a block has 64 of the source's rows (tokens) by 512 bytes of each.  Its threads read pieces of
+// 16 bytes, form the rows' codes from them, four neighbouring threads a block of 32, and leave them in LDS, out of which a thread takes 32
+// tokens of a column, or of two in bf16, and forms theirs.  The tokens and columns that fill the layouts up are zeros.
+constexpr int kTileTokens = 64;
+struct Mx4Both {
+    const void *src;                 // [M, N], `ld` elements apart
+    uint8_t *row_codes, *row_scales; // of [M, N], or null
+    uint8_t *col_codes, *col_scales; // of its transpose [N, M]
+    int64_t M, N, ld;
+    int ceil;
+    int tiles_n;                     // tiles across, of up(N, 256) columns where rows are wanted, else of N
+};
+template <bool BF16> struct BothTile { static constexpr int kCols = BF16 ? 256 : 128; };
+inline int64_t both_tiles_n(int64_t N, bool rows, bool bf16) { const int cols = bf16 ? 256 : 128; return ((rows ? mx4_width(N) : N) + cols - 1) / cols; }
+inline int64_t both_tiles(int64_t M, int64_t N, bool rows, bool bf16) { return mx4_width(M) / kTileTokens * both_tiles_n(N, rows, bf16); }
+
+// a four by four transpose of words among four neighbouring lanes: lane i's word j becomes lane j's word i
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+    const int lane = threadIdx.x & 3;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t k0 = p * 256 + h * 128 + g * 32;
-        uint4 v[32];
-#pragma unroll
-        for (int t = 0; t < 32; ++t) {
-            v[t] = make_uint4(0, 0, 0, 0);
-            if (k0 + t < a.K) v[t] = *reinterpret_cast<const uint4 *>(src + (k0 + t) * a.ld * (BF16 ? 2 : 4));
-        }
-        uint32_t w[32][4];
-#pragma unroll
-        for (int t = 0; t < 32; ++t) { w[t][0] = v[t].x; w[t][1] = v[t].y; w[t][2] = v[t].z; w[t][3] = v[t].w; }
-        uint8_t *out = a.codes + ((rb * pairs + p) * 2 + h) * 1024 + (g * 16 + r0) * 16;
+    for (int d = 1; d < 4; d *= 2) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-            uint32_t top = 0;
-#pragma unroll
-            for (int t = 0; t < 32; ++t) {
-                if (BF16) top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, w[t][j] & 0x7fff7fffu)));
-                else top = top > (w[t][j] & 0x7fffffffu) ? top : w[t][j] & 0x7fffffffu;
-            }
-#pragma unroll
-            for (int half = 0; half < (BF16 ? 2 : 1); ++half) {      // the two columns of a word
-                const int c = BF16 ? 2 * j + half : j;
-                const uint32_t byte = mx4_scale_byte(BF16 ? (half ? top & 0xffff0000u : top << 16) : top, a.ceil);
-                const float scale = mx4_scale(byte);
-                bytes[c] |= byte << 8 * h;
-                uint32_t q[4];
-#pragma unroll
-                for (int o = 0; o < 4; ++o) {
-                    if constexpr (BF16) {
-                        uint32_t pair[4];
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) pair[t] = __builtin_amdgcn_perm(w[8 * o + 2 * t + 1][j], w[8 * o + 2 * t][j], half ? 0x07060302u : 0x05040100u);
-                        q[o] = mx4_codes8(pair, scale);
-                    } else {
-                        float f[8];
-#pragma unroll
-                        for (int t = 0; t < 8; ++t) f[t] = __uint_as_float(w[8 * o + t][j]);
-                        q[o] = mx4_codes8(f, scale);
-                    }
-                }
-                *reinterpret_cast<uint4 *>(out + c * 16) = byte == 255u ? make_uint4(0, 0, 0, 0) : make_uint4(q[0], q[1], q[2], q[3]);
-            }
+            if (j & d) continue;
+            const bool up = lane & d;                        // gives word j and takes word j + d; the others the other way round
+            const uint32_t out = up ? w[j] : w[j + d];
+            const uint32_t in = (uint32_t)__shfl_xor((int)out, d, 64);
+            if (up) w[j] = in;
+            else w[j + d] = in;
         }
     }
-    uint8_t *out = a.scales + (rb * pairs + p) * 128 + (g * 16 + r0) * 2;
-    if constexpr (BF16)
-        *reinterpret_cast<uint4 *>(out) = make_uint4(bytes[0] | bytes[1] << 16, bytes[2] | bytes[3] << 16, bytes[4] | bytes[5] << 16, bytes[6] | bytes[7] << 16);
-    else *reinterpret_cast<uint2 *>(out) = make_uint2(bytes[0] | bytes[1] << 16, bytes[2] | bytes[3] << 16);
+}
+
+template <bool BF16> __device__ __forceinline__ void both_tile(const Mx4Both &a, int64_t tile, uint32_t (*lds)[129]) {
+    constexpr int kCols = BothTile<BF16>::kCols, kLanes = kCols / 8, kGroups = 256 / kLanes, kEach = kTileTokens / kGroups;      // threads to a row, rows at a time, tokens of a thread
+    constexpr int kWords = BF16 ? 4 : 8;                     // of a thread's eight values
+    const int tid = threadIdx.x, across = tid % kLanes, group = tid / kLanes;
+    const int64_t t0 = tile / a.tiles_n * kTileTokens, c0 = tile % a.tiles_n * kCols, col = c0 + across * 8;
+    uint32_t w[kEach][kWords];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int64_t t = t0 + group * kEach + e;
+        const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(a.src) + (t * a.ld + col) * (BF16 ? 2 : 4));
+#pragma unroll
+        for (int i = 0; i < kWords / 4; ++i) {
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (t < a.M && col < a.N) q = p[i];
+            w[e][4 * i] = q.x; w[e][4 * i + 1] = q.y; w[e][4 * i + 2] = q.z; w[e][4 * i + 3] = q.w;
+        }
+    }
+    // (a word of two bf16, columns 2 i and 2 i + 1, or of one fp32)
+#pragma unroll
+    for (int e = 0; e < kEach; ++e)
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) lds[group * kEach + e][across * kWords + i] = w[e][i];
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    auto larger = [](uint32_t x, uint32_t y) {
+        if (BF16) return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
+        return x > y ? x : y;
+    };
+    constexpr uint32_t kAbs = BF16 ? 0x7fff7fffu : 0x7fffffffu;
+    if (a.row_codes && t0 < i8_up(a.M, 16)) {
+        const int64_t pairs = mx4_width(a.N) / 256;
+        uint32_t code[kEach], byte[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) top = larger(top, w[e][i] & kAbs);
+            if (BF16) top = (top & 0xffff0000u) > top << 16 ? top & 0xffff0000u : top << 16;
+#pragma unroll
+            for (int d = 1; d < 4; d *= 2) {
+                const uint32_t o = (uint32_t)__shfl_xor((int)top, d, 64);
+                top = top > o ? top : o;
+            }
+            byte[e] = mx4_scale_byte(top, a.ceil);
+            if constexpr (BF16) code[e] = mx4_codes8(w[e], mx4_scale(byte[e]));
+            else {
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[e][i]);
+                code[e] = mx4_codes8(f, mx4_scale(byte[e]));
+            }
+            if (byte[e] == 255u) code[e] = 0;
+        }
+        const int q = tid & 3;
+        const int64_t block_col = col - 8 * q;               // of the block of 32
+        auto place = [&](int64_t t) { return t / 16 * pairs + block_col / 256; };
+        auto lane_of = [&](int64_t t) { return (int)(block_col % 128 / 32 * 16 + t % 16); };
+#pragma unroll
+        for (int e = 0; e < kEach; e += 4) {
+            uint32_t x[4] = {code[e], code[e + 1], code[e + 2], code[e + 3]};
+            transpose4(x);
+            const int64_t t = t0 + group * kEach + e + q;
+            if (t >= i8_up(a.M, 16) || block_col >= pairs * 256) continue;
+            *reinterpret_cast<uint4 *>(a.row_codes + (place(t) * 2 + block_col % 256 / 128) * 1024 + lane_of(t) * 16) = make_uint4(x[0], x[1], x[2], x[3]);
+            const uint32_t b = q == 0 ? byte[e] : q == 1 ? byte[e + 1] : q == 2 ? byte[e + 2] : byte[e + 3];
+            a.row_scales[place(t) * 128 + lane_of(t) * 2 + block_col % 256 / 128] = (uint8_t)b;
+        }
+    }
+    __syncthreads();
+    constexpr int kUnits = BF16 ? 2 : 1, kAcross = 128;      // columns of a thread; words across the tile
+    const int word = tid % kAcross, half = tid / kAcross;    // half: which 32 of the tokens
+    const int64_t n0 = c0 + word * kUnits, k0 = t0 + half * 32;
+    if (n0 >= a.N) return;
+    uint32_t v[32], top = 0;
+#pragma unroll
+    for (int t = 0; t < 32; ++t) {
+        v[t] = lds[half * 32 + t][word];
+        top = larger(top, v[t] & kAbs);
+    }
+    const int64_t pairs = mx4_width(a.M) / 256, block = n0 / 16 * pairs + k0 / 256;
+    const int parity = (int)(k0 % 256 / 128), lane = (int)(k0 % 128 / 32 * 16 + n0 % 16);
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const uint32_t byte = mx4_scale_byte(BF16 ? (u ? top & 0xffff0000u : top << 16) : top, a.ceil);
+        const float scale = mx4_scale(byte);
+        uint32_t q[4];
+#pragma unroll
+        for (int o = 0; o < 4; ++o) {
+            if constexpr (BF16) {
+                uint32_t pair[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) pair[t] = __builtin_amdgcn_perm(v[8 * o + 2 * t + 1], v[8 * o + 2 * t], u ? 0x07060302u : 0x05040100u);
+                q[o] = mx4_codes8(pair, scale);
+            } else {
+                float f[8];
+#pragma unroll
+                for (int t = 0; t < 8; ++t) f[t] = __uint_as_float(v[8 * o + t]);
+                q[o] = mx4_codes8(f, scale);
+            }
+        }
+        *reinterpret_cast<uint4 *>(a.col_codes + (block * 2 + parity) * 1024 + (lane + u) * 16) = byte == 255u ? make_uint4(0, 0, 0, 0) : make_uint4(q[0], q[1], q[2], q[3]);
+        a.col_scales[block * 128 + (lane + u) * 2 + parity] = (uint8_t)byte;
+    }
+}
+
+// one matrix after the other: tiles of the first below `first`
+template <bool BF16, bool BF16_2> __global__ __launch_bounds__(256) void mx4_columns_kernel(Mx4Both a, Mx4Both b, int64_t first, int64_t all) {
+    __shared__ uint32_t lds[kTileTokens][129];
+    const int64_t tile = block_of_many();
+    if (tile < first) both_tile<BF16>(a, tile, lds);
+    else if (tile < all) both_tile<BF16_2>(b, tile - first, lds);
+}
+
+Mx4Both both_args(const Mx4RowsArgs &t, const Mx4RowsArgs *rows) {
+    Mx4Both b;
+    b.src = t.src; b.col_codes = t.codes; b.col_scales = t.scales; b.M = t.K; b.N = t.rows; b.ld = t.ld; b.ceil = t.ceil;
+    b.row_codes = rows ? rows->codes : nullptr; b.row_scales = rows ? rows->scales : nullptr;
+    b.tiles_n = (int)both_tiles_n(b.N, rows != nullptr, t.bf16);
+    return b;
 }
 
 // The values that the codes stand for.  (Exact in fp32, and in bf16: 0 to 6 times a power of two from 2^-127 up.)
@@ -188,13 +278,26 @@ void launch_mx4_quantize(const Mx4RowsArgs &a, hipStream_t st) {
     if (a.rows == 0) return;
     profile_before(kTagMx4Rows, st, (double)a.rows * a.K * (a.bf16 ? 2 : 4) + (double)(mx4_code_bytes(a.rows, a.K) + mx4_scale_bytes(a.rows, a.K)));
     if (a.transposed) {
-        const dim3 grid = grid_of_many((a.rows / (a.bf16 ? 8 : 4) * (mx4_width(a.K) / 64) + 255) / 256);
-        if (a.bf16) hipLaunchKernelGGL(mx4_columns_kernel<true>, grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL(mx4_columns_kernel<false>, grid, dim3(256), 0, st, a);
+        const Mx4Both b = both_args(a, nullptr);
+        const int64_t tiles = both_tiles(b.M, b.N, false, a.bf16);
+        if (a.bf16) hipLaunchKernelGGL((mx4_columns_kernel<true, true>), grid_of_many(tiles), dim3(256), 0, st, b, b, tiles, tiles);
+        else hipLaunchKernelGGL((mx4_columns_kernel<false, false>), grid_of_many(tiles), dim3(256), 0, st, b, b, tiles, tiles);
     } else {
         if (a.bf16) hipLaunchKernelGGL(mx4_rows_kernel<true>, grid_of_pairs(a.rows, a.K), dim3(256), 0, st, a);
         else hipLaunchKernelGGL(mx4_rows_kernel<false>, grid_of_pairs(a.rows, a.K), dim3(256), 0, st, a);
     }
+    profile_after(st);
+}
+
+void launch_mx4_quantize_bwd(const Mx4RowsArgs *rows, const Mx4RowsArgs &dy, const Mx4RowsArgs &x, hipStream_t st) {
+    const Mx4Both a = both_args(dy, rows), b = both_args(x, nullptr);
+    const int64_t first = both_tiles(a.M, a.N, rows != nullptr, dy.bf16), all = first + both_tiles(b.M, b.N, false, x.bf16);
+    profile_before(kTagMx4Rows, st, (double)dy.K * ((double)dy.rows * ((dy.bf16 ? 2 : 4) + (rows ? 2 : 1) * 17 / 32.) + (double)x.rows * ((x.bf16 ? 2 : 4) + 17 / 32.)));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid_of_many(all), dim3(256), 0, st, a, b, first, all); };
+    if (dy.bf16 && x.bf16) go(mx4_columns_kernel<true, true>);
+    else if (dy.bf16) go(mx4_columns_kernel<true, false>);
+    else if (x.bf16) go(mx4_columns_kernel<false, true>);
+    else go(mx4_columns_kernel<false, false>);
     profile_after(st);
 }
 
