@@ -1,5 +1,6 @@
 // Matrices in microscaled 4-bit floating point (see ssg_mx4.h), in the layout of the products: from rows, from columns, the way back.
 #include "ssg_internal.h"
+#include "ssg_lds_load.h"
 #include "ssg_mx4.h"
 
 namespace ssg {
@@ -60,7 +61,7 @@ __device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
     }
 }
 
-template <bool BF16> __device__ __forceinline__ void both_tile(const Mx4Both &a, int64_t tile, uint32_t (*lds)[129]) {
+template <bool BF16> __device__ __forceinline__ void both_tile(const Mx4Both &a, int64_t tile, uint32_t (*lds)[128]) {
     constexpr int kCols = BothTile<BF16>::kCols, kLanes = kCols / 8, kGroups = 256 / kLanes, kEach = kTileTokens / kGroups;      // threads to a row, rows at a time, tokens of a thread
     constexpr int kWords = BF16 ? 4 : 8;                     // of a thread's eight values
     const int tid = threadIdx.x, across = tid % kLanes, group = tid / kLanes;
@@ -81,7 +82,7 @@ template <bool BF16> __device__ __forceinline__ void both_tile(const Mx4Both &a,
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) lds[group * kEach + e][across * kWords + i] = w[e][i];
+        for (int i = 0; i < kWords; i += 4) *reinterpret_cast<uint4 *>(&lds[group * kEach + e][across * kWords + i]) = make_uint4(w[e][i], w[e][i + 1], w[e][i + 2], w[e][i + 3]);
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     auto larger = [](uint32_t x, uint32_t y) {
         if (BF16) return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
@@ -166,7 +167,7 @@ template <bool BF16> __device__ __forceinline__ void both_tile(const Mx4Both &a,
 
 // one matrix after the other: tiles of the first below `first`
 template <bool BF16, bool BF16_2> __global__ __launch_bounds__(256) void mx4_columns_kernel(Mx4Both a, Mx4Both b, int64_t first, int64_t all) {
-    __shared__ uint32_t lds[kTileTokens][129];
+    __shared__ __attribute__((aligned(16))) uint32_t lds[kTileTokens][128];
     const int64_t tile = block_of_many();
     if (tile < first) both_tile<BF16>(a, tile, lds);
     else if (tile < all) both_tile<BF16_2>(b, tile - first, lds);
@@ -180,56 +181,59 @@ Mx4Both both_args(const Mx4RowsArgs &t, const Mx4RowsArgs *rows) {
     return b;
 }
 
-// The values that the codes stand for.  (Exact in fp32, and in bf16: 0 to 6 times a power of two from 2^-127 up.)
+// The values that the codes stand for.  (Exact in fp32, and in bf16: 0 to 6 times a power of two from 2^-127 up.)  A wave has 16 rows by 256 columns
+// and stores 16 bytes to a lane side by side along a row, 256 (512) bytes of four (two) rows at a time; the codes, 4 (2) bytes to a lane, come out of
+// the cache lines of a 1 KB block.
 template <bool BF16> __global__ __launch_bounds__(256) void mx4_values_kernel(Mx4ValuesArgs a) {
+    constexpr int kEach = BF16 ? 8 : 4, kLanes = 128 / kEach, kRowsAtOnce = 64 / kLanes, kSteps = 16 / kRowsAtOnce;      // values of a lane, lanes to 128 columns
     const int64_t pairs = mx4_width(a.K) / 256, wave = block_of_many() * 4 + threadIdx.x / 64, rb = wave / pairs, p = wave % pairs;
-    const int l = threadIdx.x & 63, g = l >> 4;
-    const int64_t row = rb * 16 + (l & 15);
-    if (row >= a.rows) return;
-    const uint32_t bytes = *reinterpret_cast<const uint16_t *>(a.scales + (rb * pairs + p) * 128 + l * 2);
+    if (rb * 16 >= a.rows) return;
+    const int l = threadIdx.x & 63, c = l % kLanes * kEach, g = c / 32;      // column of the 128, its run of 32
+    const uint8_t *codes = a.codes + (rb * pairs + p) * 2048 + g * 256 + c % 32 / 2, *scales = a.scales + (rb * pairs + p) * 128 + g * 32;
+    uint32_t word[2][kSteps], bytes[kSteps];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t k0 = p * 256 + h * 128 + g * 32;
-        const uint4 q = *reinterpret_cast<const uint4 *>(a.codes + ((rb * pairs + p) * 2 + h) * 1024 + l * 16);
-        const uint32_t byte = bytes >> 8 * h & 255u, words[4] = {q.x, q.y, q.z, q.w};
-        const float scale = byte == 255u ? __uint_as_float(0x7fc00000u) : mx4_scale(byte);
+    for (int i = 0; i < kSteps; ++i) {
+        const int r = i * kRowsAtOnce + l / kLanes;
+        bytes[i] = *reinterpret_cast<const uint16_t *>(scales + r * 2);
 #pragma unroll
-        for (int o = 0; o < 4; ++o) {                        // eight values
-            const int64_t k = k0 + 8 * o;
-            if (k >= a.K) break;
-            float v[8];
-            auto two = [&](auto at) {
-                constexpr int i = decltype(at)::value;
-                const ssg_f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(words[o], 1.0f, i);
-                v[2 * i] = __fmul_rn(x[0], scale);
-                v[2 * i + 1] = __fmul_rn(x[1], scale);
-            };
-            two(std::integral_constant<int, 0>{});
-            two(std::integral_constant<int, 1>{});
-            two(std::integral_constant<int, 2>{});
-            two(std::integral_constant<int, 3>{});
-            if (BF16) {
+        for (int h = 0; h < 2; ++h)
+            word[h][i] = BF16 ? *reinterpret_cast<const uint32_t *>(codes + h * 1024 + r * 16) : *reinterpret_cast<const uint16_t *>(codes + h * 1024 + r * 16);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const int64_t row = rb * 16 + i * kRowsAtOnce + l / kLanes, k = p * 256 + h * 128 + c;
+            const uint32_t byte = bytes[i] >> 8 * h & 255u;
+            const float scale = byte == 255u ? __uint_as_float(0x7fc00000u) : mx4_scale(byte);
+            float v[kEach];
+            each<kEach / 2>([&](auto at) {
+                constexpr int j = decltype(at)::value;
+                const ssg_f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[h][i], 1.0f, j);
+                v[2 * j] = __fmul_rn(x[0], scale);
+                v[2 * j + 1] = __fmul_rn(x[1], scale);
+            });
+            if (row >= a.rows || k >= a.K) continue;
+            if constexpr (BF16) {
                 uint16_t *out = static_cast<uint16_t *>(a.dst) + row * a.ld + k;
-                if (k + 8 <= a.K) {
+                if (k + kEach <= a.K) {
                     *reinterpret_cast<uint4 *>(out) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (k + i < a.K) out[i] = (uint16_t)f32_to_bf16_bits(v[i]);
+                    for (int j = 0; j < kEach; ++j)
+                        if (k + j < a.K) out[j] = (uint16_t)f32_to_bf16_bits(v[j]);
                 }
             } else {
                 float *out = static_cast<float *>(a.dst) + row * a.ld + k;
-                if (k + 8 <= a.K) {
+                if (k + kEach <= a.K) {
                     *reinterpret_cast<float4 *>(out) = make_float4(v[0], v[1], v[2], v[3]);
-                    *reinterpret_cast<float4 *>(out + 4) = make_float4(v[4], v[5], v[6], v[7]);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (k + i < a.K) out[i] = v[i];
+                    for (int j = 0; j < kEach; ++j)
+                        if (k + j < a.K) out[j] = v[j];
                 }
             }
         }
-    }
 }
 
 // Row-major codes [rows, K / 2] and scales [rows, (K + 31) / 32] into the layout and back; K a multiple of 16.
