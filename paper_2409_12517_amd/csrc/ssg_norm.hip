@@ -227,6 +227,8 @@ dim3 grid_of_blocks(int64_t blocks) {                        // of up to 1024 th
     return blocks <= kRow ? dim3((unsigned)blocks) : dim3((unsigned)kRow, (unsigned)((blocks + kRow - 1) / kRow));
 }
 
+template <int N> constexpr std::integral_constant<int, N> kHeld{};
+
 template <bool XBF16, int RES> void launch_norm_as(const NormArgs &a, hipStream_t st) {
     auto go = [&](auto kernel, auto share) {
         using S = decltype(share);
@@ -237,22 +239,38 @@ template <bool XBF16, int RES> void launch_norm_as(const NormArgs &a, hipStream_
         const int64_t runs = (a.form == NORM_I8 ? i8_width(a.d) : mx4_width(a.d)) / 8;
         auto form = [&](auto out) {
             constexpr int OUT = decltype(out)::value;
-            if (runs <= 64) go(norm_kernel<XBF16, RES, OUT, Share<256, 4, 4>, 1>, Share<256, 4, 4>{});
-            else if (runs <= 256) go(norm_kernel<XBF16, RES, OUT, Share<256, 4, 4>, 4>, Share<256, 4, 4>{});
-            else if (runs <= 1024) go(norm_kernel<XBF16, RES, OUT, Share<1024, 4, 4>, 4>, Share<1024, 4, 4>{});
-            else go(norm_kernel<XBF16, RES, OUT, Share<1024, 1, 64>, 4>, Share<1024, 1, 64>{});
+            auto as = [&](auto share, auto held) { go(norm_kernel<XBF16, RES, OUT, decltype(share), decltype(held)::value>, share); };
+            if (OUT == OUT_I8 && runs <= 16) as(Share<256, 16, 4>{}, kHeld<1>);
+            else if (runs <= 32) as(Share<256, 8, 4>{}, kHeld<1>);
+            else if (runs <= 64) as(Share<256, 4, 4>{}, kHeld<1>);
+            else if (runs <= 128) as(Share<256, 4, 4>{}, kHeld<2>);
+            else if (runs <= 256) as(Share<512, 4, 4>{}, kHeld<2>);
+            else if (runs <= 512 && a.T <= 512) as(Share<512, 2, 4>{}, kHeld<2>);
+            else if (runs <= 512) as(Share<1024, 4, 4>{}, kHeld<2>);
+            else if (runs <= 768) as(Share<1024, 4, 4>{}, kHeld<3>);
+            else if (runs <= 1024) as(Share<1024, 4, 4>{}, kHeld<4>);
+            else if (runs <= 1536) as(Share<1024, 2, 4>{}, kHeld<3>);
+            else if (runs <= 2048) as(Share<1024, 2, 4>{}, kHeld<4>);
+            else as(Share<1024, 1, 64>{}, kHeld<4>);
         };
         if (a.form == NORM_I8) form(std::integral_constant<int, OUT_I8>{});
         else form(std::integral_constant<int, OUT_MX4>{});
         return;
     }
     const int64_t runs = a.d / 8;
-    if (runs <= 8) go(norm_kernel<XBF16, RES, OUT_ROWS, Share<256, 32, 8>, 1>, Share<256, 32, 8>{});
-    else if (runs <= 16) go(norm_kernel<XBF16, RES, OUT_ROWS, Share<256, 16, 16>, 1>, Share<256, 16, 16>{});
-    else if (runs <= 64) go(norm_kernel<XBF16, RES, OUT_ROWS, Share<256, 4, 64>, 1>, Share<256, 4, 64>{});
-    else if (runs <= 256) go(norm_kernel<XBF16, RES, OUT_ROWS, Share<256, 1, 64>, 1>, Share<256, 1, 64>{});
-    else if (runs <= 1024) go(norm_kernel<XBF16, RES, OUT_ROWS, Share<256, 1, 64>, 4>, Share<256, 1, 64>{});
-    else go(norm_kernel<XBF16, RES, OUT_ROWS, Share<1024, 1, 64>, 4>, Share<1024, 1, 64>{});
+    auto as = [&](auto share, auto held) { go(norm_kernel<XBF16, RES, OUT_ROWS, decltype(share), decltype(held)::value>, share); };
+    if (runs <= 8) as(Share<256, 32, 8>{}, kHeld<1>);
+    else if (runs <= 16) as(Share<256, 16, 16>{}, kHeld<1>);
+    else if (runs <= 32) as(Share<256, 8, 32>{}, kHeld<1>);
+    else if (runs <= 64) as(Share<256, 4, 64>{}, kHeld<1>);
+    else if (runs <= 128) as(Share<256, 4, 64>{}, kHeld<2>);
+    else if (runs <= 256) as(Share<256, 1, 64>{}, kHeld<1>);
+    else if (runs <= 512) as(Share<256, 1, 64>{}, kHeld<2>);
+    else if (runs <= 768) as(Share<256, 1, 64>{}, kHeld<3>);
+    else if (runs <= 1024) as(Share<256, 1, 64>{}, kHeld<4>);
+    else if (runs <= 1536) as(Share<512, 1, 64>{}, kHeld<3>);
+    else if (runs <= 2048) as(Share<512, 1, 64>{}, kHeld<4>);
+    else as(Share<1024, 1, 64>{}, kHeld<4>);
 }
 
 // ---- the gradient ------------------------------------------------------------------------------------------
@@ -311,7 +329,7 @@ template <bool DYBF16, bool SBF16, class SHARE, int HELD> __global__ __launch_bo
         }
     }
     if (!a.dw) return;
-    float *out = a.partial + (int64_t)blockIdx.x * a.d;
+    float *out = gridDim.x == 1 ? a.dw : a.partial + (int64_t)blockIdx.x * a.d;
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
         if constexpr (ROWS == 1) {
@@ -329,40 +347,45 @@ template <bool DYBF16, bool SBF16, class SHARE, int HELD> __global__ __launch_bo
     }
 }
 
-// The blocks' rows added up, 64 columns to a block, whose waves share the rows out.
-constexpr int kDwWaves = 16;
-__global__ __launch_bounds__(64 * kDwWaves) void norm_dw_kernel(const float *partial, int64_t blocks, int64_t d, float *dw) {
-    __shared__ float part[kDwWaves][64];
-    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * 64 + l;
+// The blocks' rows added up, 32 columns to a block, whose half waves share the rows out.
+constexpr int kDwCols = 32, kDwShares = 32;
+__global__ __launch_bounds__(kDwCols * kDwShares) void norm_dw_kernel(const float *partial, int64_t blocks, int64_t d, float *dw) {
+    __shared__ float part[kDwShares][kDwCols];
+    const int c = threadIdx.x % kDwCols, share = threadIdx.x / kDwCols;
+    const int64_t col = (int64_t)blockIdx.x * kDwCols + c;
     float v = 0.0f;
     if (col < d) {
-#pragma unroll 8
-        for (int64_t b = w; b < blocks; b += kDwWaves) v = __fadd_rn(v, partial[b * d + col]);
+#pragma unroll 16
+        for (int64_t b = share; b < blocks; b += kDwShares) v = __fadd_rn(v, partial[b * d + col]);
     }
-    part[w][l] = v;
+    part[share][c] = v;
     __syncthreads();
-    if (w != 0 || col >= d) return;
+    if (share != 0 || col >= d) return;
 #pragma unroll
-    for (int i = 1; i < kDwWaves; ++i) v = __fadd_rn(v, part[i][l]);
+    for (int i = 1; i < kDwShares; ++i) v = __fadd_rn(v, part[i][c]);
     dw[col] = v;
 }
 
-int64_t bwd_rows(int64_t d) { return d <= 64 ? 32 : d <= 128 ? 16 : d <= 512 ? 4 : 1; }
+int64_t bwd_rows(int64_t d) { return d <= 64 ? 32 : d <= 128 ? 16 : d <= 256 ? 8 : d <= 512 ? 4 : d <= 1024 ? 2 : 1; }
 
 template <bool DYBF16, bool SBF16> void launch_norm_bwd_as(const NormBwdArgs &a, hipStream_t st) {
-    auto go = [&](auto kernel, auto share) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)norm_bwd_blocks(a.T, a.d)), dim3(decltype(share)::kThreads), 0, st, a);
-    };
     const int64_t runs = a.d / 8;
-    if (runs <= 8) go(norm_bwd_kernel<DYBF16, SBF16, Share<256, 32, 8>, 1>, Share<256, 32, 8>{});
-    else if (runs <= 16) go(norm_bwd_kernel<DYBF16, SBF16, Share<256, 16, 16>, 1>, Share<256, 16, 16>{});
-    else if (runs <= 64) go(norm_bwd_kernel<DYBF16, SBF16, Share<256, 4, 64>, 1>, Share<256, 4, 64>{});
-    else if (runs <= 256) go(norm_bwd_kernel<DYBF16, SBF16, Share<256, 1, 64>, 1>, Share<256, 1, 64>{});
-    else if (runs <= 512) go(norm_bwd_kernel<DYBF16, SBF16, Share<256, 1, 64>, 2>, Share<256, 1, 64>{});
-    else if (runs <= 1024) go(norm_bwd_kernel<DYBF16, SBF16, Share<512, 1, 64>, 2>, Share<512, 1, 64>{});
-    else if (runs <= 2048) go(norm_bwd_kernel<DYBF16, SBF16, Share<1024, 1, 64>, 2>, Share<1024, 1, 64>{});
-    else go(norm_bwd_kernel<DYBF16, SBF16, Share<1024, 1, 64>, 4>, Share<1024, 1, 64>{});
+    auto as = [&](auto share, auto held) {
+        using S = decltype(share);
+        hipLaunchKernelGGL((norm_bwd_kernel<DYBF16, SBF16, S, decltype(held)::value>), dim3((unsigned)norm_bwd_blocks(a.T, a.d)), dim3(S::kThreads), 0, st, a);
+    };
+    if (runs <= 8) as(Share<256, 32, 8>{}, kHeld<1>);
+    else if (runs <= 16) as(Share<256, 16, 16>{}, kHeld<1>);
+    else if (runs <= 32) as(Share<256, 8, 32>{}, kHeld<1>);
+    else if (runs <= 64) as(Share<256, 4, 64>{}, kHeld<1>);
+    else if (runs <= 128) as(Share<256, 2, 32>{}, kHeld<1>);
+    else if (runs <= 256) as(Share<256, 1, 64>{}, kHeld<1>);
+    else if (runs <= 512) as(Share<256, 1, 64>{}, kHeld<2>);
+    else if (runs <= 768) as(Share<256, 1, 64>{}, kHeld<3>);
+    else if (runs <= 1024) as(Share<512, 1, 64>{}, kHeld<2>);
+    else if (runs <= 1536) as(Share<512, 1, 64>{}, kHeld<3>);
+    else if (runs <= 2048) as(Share<512, 1, 64>{}, kHeld<4>);
+    else as(Share<1024, 1, 64>{}, kHeld<4>);
 }
 
 }  // namespace
@@ -383,7 +406,7 @@ void launch_norm(const NormArgs &a, hipStream_t st) {
 
 int64_t norm_bwd_blocks(int64_t T, int64_t d) {
     const int64_t rows = bwd_rows(d);
-    return std::max<int64_t>(1, std::min<int64_t>((T + rows - 1) / rows, 512));
+    return std::max<int64_t>(1, std::min<int64_t>((T + rows - 1) / rows, d <= 6144 ? 512 : 256));
 }
 
 void launch_norm_bwd(const NormBwdArgs &a, hipStream_t st) {
@@ -392,7 +415,7 @@ void launch_norm_bwd(const NormBwdArgs &a, hipStream_t st) {
     else if (a.dy_bf16) launch_norm_bwd_as<true, false>(a, st);
     else if (a.s_bf16) launch_norm_bwd_as<false, true>(a, st);
     else launch_norm_bwd_as<false, false>(a, st);
-    if (a.dw) hipLaunchKernelGGL(norm_dw_kernel, dim3((unsigned)((a.d + 63) / 64)), dim3(64 * kDwWaves), 0, st, a.partial, norm_bwd_blocks(a.T, a.d), a.d, a.dw);
+    if (a.dw && norm_bwd_blocks(a.T, a.d) > 1) hipLaunchKernelGGL(norm_dw_kernel, dim3((unsigned)((a.d + kDwCols - 1) / kDwCols)), dim3(kDwCols * kDwShares), 0, st, a.partial, norm_bwd_blocks(a.T, a.d), a.d, a.dw);
     profile_after(st);
 }
 
