@@ -424,6 +424,7 @@ I8Plan mx4_gemm_plan(const Mx4GemmArgs &a);
 void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st);
 // up to kMx4TokenRows rows of x, quantized in the product's own kernel
 constexpr int kMx4TokenRows = 4;
+constexpr int64_t kMx4TokenLds = 48 << 10;
 struct Mx4TokenArgs {
     const void *x = nullptr;         // rows of K, `ld` elements apart
     const uint8_t *B = nullptr, *sb = nullptr;

@@ -72,10 +72,11 @@ __device__ __forceinline__ void store4(const Mx4Params &p, int64_t row, int64_t 
 // A workgroup has several tiles one after the other and the rings run on from one to the next: while a tile's last steps are
 // multiplied and its results stored, the first stages of the next are on their way.  A tile with no more rows than half
 // loads and multiplies half of them.
-constexpr int kScaleSlots = 2;
-template <int TA, int TB, int STAGES> struct TileShape {
+constexpr int kStages = 4, kScaleSlots = 2;
+static_assert(kStages % 2 == 0, "a pair's scales come with the first of two stages, and a tile's last stage with the second of a pair of steps");
+template <int TA, int TB> struct TileShape {
     static constexpr int kA = 4 * TA, kB = 4 * TB;       // blocks of 16 rows, and of 16 columns, of the tile
-    static constexpr int kRows = 16 * kA, kCols = 16 * kB, kStage = (kA + kB) * 1024, kRing = STAGES * kStage;
+    static constexpr int kRows = 16 * kA, kCols = 16 * kB, kStage = (kA + kB) * 1024, kRing = kStages * kStage;
     static constexpr int kScales = (kA + kB) * 128;      // of a pair: the rows', then the columns'
     static constexpr int kLds = kRing + kScaleSlots * kScales, kAtOnce = 163840 / kLds;
 };
@@ -95,8 +96,8 @@ __device__ __forceinline__ void swap16(uint32_t &a, uint32_t &b) {
     a = r[0]; b = r[1];
 }
 
-template <int TA, int TB, int STAGES> __global__ __launch_bounds__(256, (TileShape<TA, TB, STAGES>::kAtOnce)) void mx4_tile_kernel(Mx4Params p) {
-    using Shape = TileShape<TA, TB, STAGES>;
+template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::kAtOnce)) void mx4_tile_kernel(Mx4Params p) {
+    using Shape = TileShape<TA, TB>;
     constexpr int kA = Shape::kA, kB = Shape::kB, kStage = Shape::kStage, kRing = Shape::kRing, kScales = Shape::kScales;
     __shared__ __attribute__((aligned(1024))) uint8_t smem[Shape::kLds];
     const int row_blocks = (int)((p.M + 15) / 16), col_blocks = (int)(p.N / 16);
@@ -218,7 +219,7 @@ template <int TA, int TB, int STAGES> __global__ __launch_bounds__(256, (TileSha
     };
     look_ahead();
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < kStages; ++s) {
         if (s % 2 == 0) issue_scales(s / 2 * kScales);
         each<kLoads>([&](auto j) {
             issue_to(j, s * kStage);
@@ -230,7 +231,7 @@ template <int TA, int TB, int STAGES> __global__ __launch_bounds__(256, (TileSha
         if (s % 2 == 1) two_loaded();
     }
     uint32_t slot = 0, scale_slot = 0;                   // of this step's stage; of this pair's scales
-    wait_dma<(STAGES - 1) * kFewest + 1>();              // stage 0 and the scales before it (those of the second pair came later)
+    wait_dma<(kStages - 1) * kFewest + 1>();              // stage 0 and the scales before it (those of the second pair came later)
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     // Steps of a tile whose wait there is none for: before the last tile's results were stored, all that was loaded had landed.  (A wait for a
@@ -269,7 +270,7 @@ template <int TA, int TB, int STAGES> __global__ __launch_bounds__(256, (TileSha
         constexpr int kMfmas = QA * QB, kReads = QA + QB, kReadsEach = (kReads + kMfmas - 1) / kMfmas, kLoadsEach = (kLoads + kMfmas - 1) / kMfmas;
         auto step = [&](auto parity) {
             constexpr int P = decltype(parity)::value;
-            const uint32_t next = slot == (STAGES - 1) * kStage ? 0 : slot + kStage, next_scales = scale_slot ^ kScales;
+            const uint32_t next = slot == (kStages - 1) * kStage ? 0 : slot + kStage, next_scales = scale_slot ^ kScales;
             multiply(parity, std::integral_constant<int, 0>{}, [&](auto at) {
                 constexpr int t = decltype(at)::value;
 #pragma unroll
@@ -278,13 +279,13 @@ template <int TA, int TB, int STAGES> __global__ __launch_bounds__(256, (TileSha
                     if (P == 0) read_scale(1, i, scale_slot);
                 }
             });
-            // the next step's stage has landed, and the scales before it: of the stages after it those of even number bring scales
-            wait_dma_unless<(STAGES - 2) * kFewest + (STAGES - 2 + (P == 0)) / 2>(waited);
+            // the next step's stage has landed, and the scales before it: of two stages after it one brings scales
+            wait_dma_unless<(kStages - 2) * kFewest + (kStages - 2) / 2>(waited);
             --waited;
             __builtin_amdgcn_s_waitcnt(0xC07F);              // all of this step's fragments are here
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
-            if (P == STAGES % 2) issue_scales(scale_slot);
+            if (P == 0) issue_scales(scale_slot);
             multiply(parity, std::integral_constant<int, 1>{}, [&](auto at) {
                 constexpr int t = decltype(at)::value;
 #pragma unroll
@@ -318,7 +319,7 @@ template <int TA, int TB, int STAGES> __global__ __launch_bounds__(256, (TileSha
             src.b += 1024;
             slot = next;
             if (P == 1) scale_slot = next_scales;
-            if (P != STAGES % 2) two_loaded();
+            if (P == 1) two_loaded();
         };
         // A lane has row l % 32 of a block and of each eight columns four, those from 4 (l / 32) on.  Exchanged between lanes until one store takes 64 bytes of
         // each of 16 rows.
@@ -390,7 +391,7 @@ template <int TA, int TB, int STAGES> __global__ __launch_bounds__(256, (TileSha
             step(std::integral_constant<int, 1>{});
         }
         wait_dma<0>();
-        waited = STAGES - 1;
+        waited = kStages - 1;
         if (p.c_f32) store(std::true_type{});
         else store(std::false_type{});
     };
@@ -473,6 +474,10 @@ template <int RB, int CB, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
     constexpr int U = RB + CB > 4 ? 2 : 4;
     int at = w * share;
     for (; at + U <= p1; at += U) steps(std::integral_constant<int, U>{}, at);
+    if (U > 2 && at + 2 <= p1) {
+        steps(std::integral_constant<int, 2>{}, at);
+        at += 2;
+    }
     for (; at < p1; ++at) steps(std::integral_constant<int, 1>{}, at);
 #pragma unroll
     for (int r = 0; r < RB; ++r)
@@ -490,65 +495,104 @@ template <int RB, int CB, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
 }
 
 // ---- up to four rows, quantized on the way ------------------------------------------------------------------
-// A block of x has its scale to itself, so a lane forms the codes that it multiplies from 32 values of its row in its own registers, and nothing is
-// exchanged before the products.  16 columns to a workgroup, whose waves share K out.
+// 16 columns to a workgroup, whose waves share K out.  Its threads quantize the rows, a block each, into LDS while the first weights are on their way.
+// (In the registers of the lanes that multiply them, where four of 64 have a row's values, the vector ALU took 3 us: 1 x 4096 -> 11008
+// 10.6 us.)  Bound by the weights' bytes and the start and end of one round of workgroups.
 template <bool BF16, int WAVES> __global__ __launch_bounds__(64 * WAVES) void mx4_token_kernel(Mx4TokenArgs a) {
+    constexpr int U = 4;                                     // pairs of blocks at a time
+    extern __shared__ __attribute__((aligned(16))) uint8_t codes[];          // rows of Kp / 2, then their scales, rows of Kp / 32
     __shared__ v4f_t part[WAVES][64];
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = l >> 4;
     const int pairs = (int)(mx4_width(a.K) / 256), share = (pairs + WAVES - 1) / WAVES;
-    const int p1 = (w + 1) * share < pairs ? (w + 1) * share : pairs;
+    const int p0 = w * share < pairs ? w * share : pairs, p1 = p0 + share < pairs ? p0 + share : pairs;
     const uint8_t *b = a.B + (int64_t)blockIdx.x * pairs * 2048 + l * 16, *sb = a.sb + (int64_t)blockIdx.x * pairs * 128 + l * 2;
-    const bool live = (l & 15) < a.rows;
-    const uint8_t *x = static_cast<const uint8_t *>(a.x) + (live ? l & 15 : 0) * a.ld * (BF16 ? 2 : 4);
+    v4i_t f[U][2];
+    uint32_t sw[U];
+    auto load = [&](int at) {                                // beyond the share its last pair again, or the first there is
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = at + u < p1 ? at + u : p1 > p0 ? p1 - 1 : 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) f[u][h] = __builtin_nontemporal_load(reinterpret_cast<const v4i_t *>(b + (int64_t)k * 2048 + h * 1024));
+            sw[u] = *reinterpret_cast<const uint16_t *>(sb + (int64_t)k * 128);
+        }
+    };
+    load(p0);
+    const int blocks = pairs * 8;                            // of a row
+    uint8_t *scales = codes + a.rows * blocks * 16;
+    for (int i = tid; i < a.rows * blocks; i += 64 * WAVES) {
+        const int r = i / blocks, k = i % blocks;
+        Mx4Block<BF16> v;
+        v.load(static_cast<const uint8_t *>(a.x) + r * a.ld * (BF16 ? 2 : 4), k * 32, a.K, true);
+        const uint32_t byte = mx4_scale_byte(v.top_bits(), a.ceil);
+        *reinterpret_cast<uint4 *>(codes + i * 16) = v.codes(byte);
+        scales[i] = (uint8_t)byte;
+    }
+    __syncthreads();
+    // rows of C beyond a.rows are computed from the first row and not stored
+    const int mine = ((l & 15) < a.rows ? l & 15 : 0) * blocks + g;
     v4f_t acc = {0, 0, 0, 0};
-    for (int at = w * share; at < p1; ++at) {
-        v4i_t f[2];
-        Mx4Block<BF16> v[2];
+    for (int at = p0; at < p1; at += U) {
+        if (at > p0) load(at);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) f[h] = __builtin_nontemporal_load(reinterpret_cast<const v4i_t *>(b + (int64_t)at * 2048 + h * 1024));
-        const uint32_t sw = *reinterpret_cast<const uint16_t *>(sb + (int64_t)at * 128);
+        for (int u = 0; u < U; ++u) {
+            if (at + u >= p1) break;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) v[h].load(x, (int64_t)at * 256 + h * 128 + g * 32, a.K, live);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t byte = mx4_scale_byte(v[h].top_bits(), a.ceil);
-            const uint4 q = v[h].codes(byte);
-            const v4i_t codes = {(int)q.x, (int)q.y, (int)q.z, (int)q.w};
-            acc = h == 0 ? mfma_mx4<0>(f[h], sw, codes, byte, acc) : mfma_mx4<0>(f[h], sw >> 8, codes, byte, acc);
+            for (int h = 0; h < 2; ++h) {
+                const int k = mine + (at + u) * 8 + h * 4;
+                const v4i_t x = *reinterpret_cast<const v4i_t *>(codes + k * 16);
+                acc = mfma_mx4<0>(f[u][h], sw[u] >> 8 * h, x, scales[k], acc);
+            }
         }
     }
     part[w][l] = acc;
     __syncthreads();
-    if (w != 0 || !live) return;
+    if (w != 0 || (l & 15) >= a.rows) return;
     v4f_t v = part[0][l];
 #pragma unroll
     for (int i = 1; i < WAVES; ++i) v += part[i][l];
-    const int64_t at = (l & 15) * a.ldc + (int64_t)blockIdx.x * 16 + g * 4;
-    if (a.c_f32) *reinterpret_cast<float4 *>(static_cast<float *>(a.C) + at) = make_float4(v[0], v[1], v[2], v[3]);
-    else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.C) + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    const int64_t to = (l & 15) * a.ldc + (int64_t)blockIdx.x * 16 + g * 4;
+    if (a.c_f32) *reinterpret_cast<float4 *>(static_cast<float *>(a.C) + to) = make_float4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.C) + to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
 }
 
-enum Mx4Form { FEW_16, FEW_32, FEW_64, TILE_128, TILE_256 };
+// Which kernel, from the extents alone.
+// The smallest blocks whose workgroups the chip holds at once, one to a compute unit, since their waves share K out: microseconds in blocks of
+//                                  16 x 16   32 x 16   32 x 32   64 x 32   64 x 64   tiles of 128
+//     64 x 2736 -> 1040                4.3       3.9       4.5       5.7       8.2       7.0
+//    128 x 2736 -> 1040                4.7       5.1       4.6       5.6       8.0       8.3
+//    256 x 2736 -> 1040                7.7       6.0       6.1       5.9       8.0       8.3
+//     64 x 4096 -> 4096                7.5       6.2       5.6       7.2       9.6       9.0
+//    128 x 4096 -> 4096               12.7       8.8       7.4       7.1       9.4      11.0
+//    256 x 4096 -> 4096               22.6      15.4      12.2      10.0       9.5      11.0
+//    128 x 11008 -> 4096              27.9      19.1      15.8      13.2      18.4      29.4
+//    256 x 11008 -> 4096              53.6      35.5      28.4      21.1      18.0      29.3
+// Where there are more in any of them: up to 16 and 32 rows blocks of 16 and 32 rows by 16 columns (32 x 4096 -> 11008 10.1 8.7 9.0 9.9 9.8), up to 64 rows
+// 32 x 32 (64 x 4096 -> 11008 15.5 12.4 10.5 11.6 10.7 and 11.4 in tiles), then tiles (128 x 4096 -> 11008 27.8 19.0 15.6 14.3 18.0, 13.9 in tiles).
+// Between the tiles: estimated times, where a step of 128 along K takes a compute unit .52 us with two small tiles on it, .28 with
+// one, .88 with a large one, and a tile 4 and 5 us beside its steps.
+enum Mx4Form { FEW_16_16, FEW_32_16, FEW_32_32, FEW_64_32, FEW_64_64, TILE_128, TILE_256 };
+struct Mx4Extent { int rows, cols; };
+constexpr Mx4Extent kExtents[] = {{16, 16}, {32, 16}, {32, 32}, {64, 32}, {64, 64}, {128, 128}, {256, 256}};
+int64_t count_of(const Mx4GemmArgs &a, Mx4Form f) { return (a.M + kExtents[f].rows - 1) / kExtents[f].rows * ((a.N + kExtents[f].cols - 1) / kExtents[f].cols); }
 Mx4Form choose_form(const Mx4GemmArgs &a) {
-    const double KB = (double)(mx4_width(a.K) / 128), small_step = .52 * KB + 4, small_alone = .28 * KB + 4, large_step = .70 * KB + 9;
+    if (a.K == 0) return FEW_32_32;                      // zeros: the tiles' rings want something to load
+    for (Mx4Form f : {FEW_16_16, FEW_32_16, FEW_32_32, FEW_64_32, FEW_64_64})
+        if (kExtents[f].rows < a.M + 16 && count_of(a, f) <= 256) return f;
+    if (a.M <= 64) return a.M <= 16 ? FEW_16_16 : a.M <= 32 ? FEW_32_16 : FEW_32_32;
+    const double KB = (double)(mx4_width(a.K) / 128), small_step = .52 * KB + 4, small_alone = .28 * KB + 4, large_step = .88 * KB + 5;
     auto small_time = [&](double tiles) {                // rounds of two to a compute unit, the last one perhaps of one
         const double rounds = std::floor(tiles / 512), rest = tiles - 512 * rounds;
         return rounds * small_step + (rest <= 0 ? 0 : rest <= 256 ? small_alone : small_step);
     };
-    const int64_t cols16 = a.N / 16, tiles128 = (a.M + 127) / 128 * ((a.N + 127) / 128), tiles256 = (a.M + 255) / 256 * ((a.N + 255) / 256);
-    if (a.K == 0) return FEW_64;                         // zeros: the tiles' rings want something to load
-    if (a.M <= 16 || (a.M + 15) / 16 * cols16 <= 256) return FEW_16;
-    if (a.M <= 32 || (a.M + 31) / 32 * cols16 <= 256) return FEW_32;
-    if (a.M <= 64 || tiles128 <= 64) return FEW_64;
-    return (double)((tiles256 + 255) / 256) * large_step < small_time((double)tiles128) ? TILE_256 : TILE_128;
+    return (double)((count_of(a, TILE_256) + 255) / 256) * large_step < small_time((double)count_of(a, TILE_128)) ? TILE_256 : TILE_128;
 }
 
 }  // namespace
 
 I8Plan mx4_gemm_plan(const Mx4GemmArgs &a) {
     const Mx4Form form = choose_form(a);
-    if (form == TILE_256 || form == TILE_128) return {form == TILE_256 ? 256 : 128, 0, 0};
-    return {0, form == FEW_64 ? 64 : form == FEW_32 ? 32 : 16, form == FEW_64 ? 32 : 16};
+    return {form >= TILE_128 ? kExtents[form].rows : 0, kExtents[form].rows, kExtents[form].cols};
 }
 
 void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st) {
@@ -556,30 +600,35 @@ void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st) {
     const Mx4Form form = choose_form(a);
     Mx4Params p;
     p.A = a.A; p.B = a.B; p.sa = a.sa; p.sb = a.sb; p.C = a.C; p.M = a.M; p.N = a.N; p.ldc = a.ldc; p.KB = (int)(mx4_width(a.K) / 128); p.c_f32 = a.c_f32;
-    auto go = [&](auto kernel, int rows, int cols, int threads, int64_t most) {
-        p.tiles_n = (int)((a.N + cols - 1) / cols);
-        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min((a.M + rows - 1) / rows * p.tiles_n, most)), dim3(threads), 0, st, p);
+    auto go = [&](auto kernel, int threads, int64_t most) {
+        p.tiles_n = (int)((a.N + kExtents[form].cols - 1) / kExtents[form].cols);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(count_of(a, form), most)), dim3(threads), 0, st, p);
     };
     // the tiles' workgroups stay, one or two to a compute unit; a tile of no more steps than the ring has stages is a workgroup's only one
     // (its loads would run two tiles ahead)
     constexpr int64_t kAll = (int64_t)1 << 31;
-    auto units = [&](int stages, int at_once) { return p.KB > stages ? 256 * (int64_t)at_once : kAll; };
+    auto units = [&](int at_once) { return p.KB > kStages ? 256 * (int64_t)at_once : kAll; };
     profile_before(kTagMx4Gemm, st);
-    if (form == TILE_256) go(mx4_tile_kernel<4, 4, 4>, 256, 256, 256, units(4, 1));
-    else if (form == TILE_128) go(mx4_tile_kernel<2, 2, 4>, 128, 128, 256, units(4, 2));
-    else if (form == FEW_16) go(mx4_few_kernel<1, 1, 8>, 16, 16, 512, kAll);
-    else if (form == FEW_32) go(mx4_few_kernel<2, 1, 4>, 32, 16, 256, kAll);
-    else go(mx4_few_kernel<4, 2, 8>, 64, 32, 512, kAll);
+    switch (form) {
+        case FEW_16_16: go(mx4_few_kernel<1, 1, 8>, 512, kAll); break;
+        case FEW_32_16: go(mx4_few_kernel<2, 1, 8>, 512, kAll); break;
+        case FEW_32_32: go(mx4_few_kernel<2, 2, 8>, 512, kAll); break;
+        case FEW_64_32: go(mx4_few_kernel<4, 2, 8>, 512, kAll); break;
+        case FEW_64_64: go(mx4_few_kernel<4, 4, 8>, 512, kAll); break;
+        case TILE_128: go(mx4_tile_kernel<2, 2>, 256, units(2)); break;
+        case TILE_256: go(mx4_tile_kernel<4, 4>, 256, units(1)); break;
+    }
     profile_after(st);
 }
 
-bool mx4_token_ok(int64_t M, int64_t, int64_t) { return M <= kMx4TokenRows; }
+static int64_t token_lds(int64_t M, int64_t K) { return M * (mx4_width(K) / 32 * 17); }
+bool mx4_token_ok(int64_t M, int64_t, int64_t K) { return M <= kMx4TokenRows && token_lds(M, K) <= kMx4TokenLds; }
 
 void launch_mx4_token(const Mx4TokenArgs &a, hipStream_t st) {
     profile_before(kTagMx4Gemm, st);
-    const dim3 blocks((unsigned)(a.N / 16));
-    if (a.bf16) hipLaunchKernelGGL((mx4_token_kernel<true, 8>), blocks, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((mx4_token_kernel<false, 8>), blocks, dim3(512), 0, st, a);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(a.N / 16)), dim3(512), (unsigned)token_lds(a.rows, a.K), st, a); };
+    if (a.bf16) go(mx4_token_kernel<true, 8>);
+    else go(mx4_token_kernel<false, 8>);
     profile_after(st);
 }
 
