@@ -422,6 +422,7 @@ struct Mx4GemmArgs {
 };
 I8Plan mx4_gemm_plan(const Mx4GemmArgs &a);
 void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st);
+void launch_mx4_gemm_pair(const Mx4GemmArgs &a, const Mx4GemmArgs &b, hipStream_t st);      // two products that do not depend on each other
 // up to kMx4TokenRows rows of x, quantized in the product's own kernel
 constexpr int kMx4TokenRows = 4;
 constexpr int64_t kMx4TokenLds = 48 << 10;

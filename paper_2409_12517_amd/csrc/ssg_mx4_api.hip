@@ -255,8 +255,9 @@ ssg_status ssg_mx4_linear_bwd(const void *dy, ssg_dtype dy_dtype, int64_t lddy, 
                                      rows_args(x, x_dtype, K, M, ldx, 1, rule, b + L.x_t), st);
     else if (dx)
         ssg::launch_mx4_quantize(rows, st);
-    if (dx) ssg::launch_mx4_gemm(gemm_args(b + L.dy, M, Wt, K, N, dx, dx_dtype, lddx), st);
-    if (dW) ssg::launch_mx4_gemm(gemm_args(b + L.dy_t, N, b + L.x_t, K, M, dW, dw_dtype, lddw), st);
+    const ssg::Mx4GemmArgs gx = gemm_args(b + L.dy, M, Wt, K, N, dx, dx_dtype, lddx), gw = gemm_args(b + L.dy_t, N, b + L.x_t, K, M, dW, dw_dtype, lddw);
+    if (dx && dW) ssg::launch_mx4_gemm_pair(gx, gw, st);
+    else ssg::launch_mx4_gemm(dx ? gx : gw, st);
     return check_launch(who);
 }
 

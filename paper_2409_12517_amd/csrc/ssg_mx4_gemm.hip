@@ -96,13 +96,12 @@ __device__ __forceinline__ void swap16(uint32_t &a, uint32_t &b) {
     a = r[0]; b = r[1];
 }
 
-template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::kAtOnce)) void mx4_tile_kernel(Mx4Params p) {
+// Tiles v, v + stride, ..
+template <int TA, int TB> __device__ __forceinline__ void run_tiles(const Mx4Params &p, uint8_t *smem, int v, const int stride) {
     using Shape = TileShape<TA, TB>;
     constexpr int kA = Shape::kA, kB = Shape::kB, kStage = Shape::kStage, kRing = Shape::kRing, kScales = Shape::kScales;
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[Shape::kLds];
     const int row_blocks = (int)((p.M + 15) / 16), col_blocks = (int)(p.N / 16);
     const int rows = (row_blocks + kA - 1) / kA, all = rows * p.tiles_n;
-    int v = blockIdx.x;
     if (v >= all) return;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w >> 1, wn = w & 1;
     const int lane_id = tid & 63;
@@ -209,7 +208,7 @@ template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::
     };
     // the next tile, known before the loads come to it
     auto look_ahead = [&]() {
-        const int n = v + (int)gridDim.x;
+        const int n = v + stride;
         if (n < all) {
             next_tile = find_tile(p, kA, kB, rows, n);
             next_src = source(next_tile);
@@ -406,12 +405,23 @@ template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::
         v = __builtin_amdgcn_readfirstlane(v);
         if (__builtin_amdgcn_readfirstlane(row_blocks - tile.rb) <= kA / 2) run_tile(std::integral_constant<int, TA / 2>{});
         else run_tile(std::integral_constant<int, TA>{});
-        v += (int)gridDim.x;
+        v += stride;
         if (v >= all) break;
         tile = next_tile;
         look_ahead();
     }
     wait_dma<0>();                                       // (the workgroup's LDS is another's after it)
+}
+template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::kAtOnce)) void mx4_tile_kernel(Mx4Params p) {
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[TileShape<TA, TB>::kLds];
+    run_tiles<TA, TB>(p, smem, blockIdx.x, gridDim.x);
+}
+// Two products' tiles side by side, those of the first below `first`, one to a workgroup.
+template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::kAtOnce)) void mx4_tile_pair_kernel(Mx4Params a, Mx4Params b, int first) {
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[TileShape<TA, TB>::kLds];
+    const bool in_first = (int)blockIdx.x < first;
+    const Mx4Params p = in_first ? a : b;
+    run_tiles<TA, TB>(p, smem, (int)blockIdx.x - (in_first ? 0 : first), gridDim.x);
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------
@@ -569,23 +579,34 @@ template <bool BF16, int WAVES> __global__ __launch_bounds__(64 * WAVES) void mx
 //    256 x 11008 -> 4096              53.6      35.5      28.4      21.1      18.0      29.3
 // Where there are more in any of them: up to 16 and 32 rows blocks of 16 and 32 rows by 16 columns (32 x 4096 -> 11008 10.1 8.7 9.0 9.9 9.8), up to 64 rows
 // 32 x 32 (64 x 4096 -> 11008 15.5 12.4 10.5 11.6 10.7 and 11.4 in tiles), then tiles (128 x 4096 -> 11008 27.8 19.0 15.6 14.3 18.0, 13.9 in tiles).
-// Between the tiles: estimated times, where a step of 128 along K takes a compute unit .52 us with two small tiles on it, .28 with
-// one, .88 with a large one, and a tile 4 and 5 us beside its steps.
+// 64 x 64 where K is long enough that their few steps are not all start and end (512 x 2064 -> 1376 8.6 us and 7.9 in tiles of 128).
+// Between the tiles: estimated times.  A round of small tiles, two to a compute unit, takes .51 us a step of 128 along K and 5 beside them; with one to a
+// compute unit .33 and 1.5, less where few are left over after whole rounds.  A round of large ones takes .86 us a step with all compute units at work
+// and .55 with half of them, where the clock is higher, and 5 to 8.5 beside them.  Measured, small and large: 1024 x 4096 -> 11008 35.1 33.4 us,
+// 1536 48.4 59.8, 2048 66.6 63.8, 3000 86.6 92.1, 4096 119 98; 4096 x 4096 -> 4096 45.8 39.2; 2048 x 11008 -> 4096 56.3 61.6, 3000 78.9 74.1;
+// 8192 x 2064 -> 1376 20.3 22.8.
 enum Mx4Form { FEW_16_16, FEW_32_16, FEW_32_32, FEW_64_32, FEW_64_64, TILE_128, TILE_256 };
 struct Mx4Extent { int rows, cols; };
 constexpr Mx4Extent kExtents[] = {{16, 16}, {32, 16}, {32, 32}, {64, 32}, {64, 64}, {128, 128}, {256, 256}};
 int64_t count_of(const Mx4GemmArgs &a, Mx4Form f) { return (a.M + kExtents[f].rows - 1) / kExtents[f].rows * ((a.N + kExtents[f].cols - 1) / kExtents[f].cols); }
 Mx4Form choose_form(const Mx4GemmArgs &a) {
     if (a.K == 0) return FEW_32_32;                      // zeros: the tiles' rings want something to load
+    const double KB = (double)(mx4_width(a.K) / 128);
     for (Mx4Form f : {FEW_16_16, FEW_32_16, FEW_32_32, FEW_64_32, FEW_64_64})
-        if (kExtents[f].rows < a.M + 16 && count_of(a, f) <= 256) return f;
+        if (kExtents[f].rows < a.M + 16 && count_of(a, f) <= 256 && (f != FEW_64_64 || KB >= 20)) return f;
     if (a.M <= 64) return a.M <= 16 ? FEW_16_16 : a.M <= 32 ? FEW_32_16 : FEW_32_32;
-    const double KB = (double)(mx4_width(a.K) / 128), small_step = .52 * KB + 4, small_alone = .28 * KB + 4, large_step = .88 * KB + 5;
-    auto small_time = [&](double tiles) {                // rounds of two to a compute unit, the last one perhaps of one
+    const double small_step = .51 * KB + 5, small_alone = .33 * KB + 1.5;
+    auto small_time = [&](double tiles) {
         const double rounds = std::floor(tiles / 512), rest = tiles - 512 * rounds;
-        return rounds * small_step + (rest <= 0 ? 0 : rest <= 256 ? small_alone : small_step);
+        const double left = rest > 256 ? small_alone + (rest - 256) / 256 * (small_step - small_alone) : small_alone * (rounds > 0 ? std::max(.3, rest / 256) : 1);
+        return rounds * small_step + (rest > 0 ? left : 0);
     };
-    return (double)((count_of(a, TILE_256) + 255) / 256) * large_step < small_time((double)count_of(a, TILE_128)) ? TILE_256 : TILE_128;
+    auto large_time = [&](double tiles) {
+        const double rounds = std::floor(tiles / 256), rest = tiles - 256 * rounds;
+        return rounds * (.86 * KB + 5) + (rest > 0 ? KB * (.55 + .31 * std::max(0., rest / 128 - 1)) + 8.5 : 0);
+    };
+    if (KB <= kStages) return TILE_128;                  // no rings that run on (3000 x 512 -> 11008 28.7 us, 35.0 in large tiles)
+    return large_time((double)count_of(a, TILE_256)) < small_time((double)count_of(a, TILE_128)) ? TILE_256 : TILE_128;
 }
 
 }  // namespace
@@ -595,19 +616,36 @@ I8Plan mx4_gemm_plan(const Mx4GemmArgs &a) {
     return {form >= TILE_128 ? kExtents[form].rows : 0, kExtents[form].rows, kExtents[form].cols};
 }
 
+static Mx4Params params_of(const Mx4GemmArgs &a, Mx4Form form) {
+    Mx4Params p;
+    p.A = a.A; p.B = a.B; p.sa = a.sa; p.sb = a.sb; p.C = a.C; p.M = a.M; p.N = a.N; p.ldc = a.ldc; p.KB = (int)(mx4_width(a.K) / 128); p.c_f32 = a.c_f32;
+    p.tiles_n = (int)((a.N + kExtents[form].cols - 1) / kExtents[form].cols);
+    return p;
+}
+
+// Where both have small tiles and the chip holds them all at once, one launch (777 x 2064 -> 1376 and its weights' gradient 8.1 + 5.8 us in two).
+void launch_mx4_gemm_pair(const Mx4GemmArgs &a, const Mx4GemmArgs &b, hipStream_t st) {
+    if (a.M > 0 && b.M > 0 && choose_form(a) == TILE_128 && choose_form(b) == TILE_128 && count_of(a, TILE_128) + count_of(b, TILE_128) <= 512) {
+        const int first = (int)count_of(a, TILE_128), all = first + (int)count_of(b, TILE_128);
+        profile_before(kTagMx4Gemm, st);
+        hipLaunchKernelGGL((mx4_tile_pair_kernel<2, 2>), dim3(all), dim3(256), 0, st, params_of(a, TILE_128), params_of(b, TILE_128), first);
+        profile_after(st);
+        return;
+    }
+    launch_mx4_gemm(a, st);
+    launch_mx4_gemm(b, st);
+}
+
 void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st) {
     if (a.M == 0) return;
     const Mx4Form form = choose_form(a);
-    Mx4Params p;
-    p.A = a.A; p.B = a.B; p.sa = a.sa; p.sb = a.sb; p.C = a.C; p.M = a.M; p.N = a.N; p.ldc = a.ldc; p.KB = (int)(mx4_width(a.K) / 128); p.c_f32 = a.c_f32;
+    const Mx4Params p = params_of(a, form);
     auto go = [&](auto kernel, int threads, int64_t most) {
-        p.tiles_n = (int)((a.N + kExtents[form].cols - 1) / kExtents[form].cols);
         hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(count_of(a, form), most)), dim3(threads), 0, st, p);
     };
     // the tiles' workgroups stay, one or two to a compute unit; a tile of no more steps than the ring has stages is a workgroup's only one
     // (its loads would run two tiles ahead)
     constexpr int64_t kAll = (int64_t)1 << 31;
-    auto units = [&](int at_once) { return p.KB > kStages ? 256 * (int64_t)at_once : kAll; };
     profile_before(kTagMx4Gemm, st);
     switch (form) {
         case FEW_16_16: go(mx4_few_kernel<1, 1, 8>, 512, kAll); break;
@@ -615,8 +653,8 @@ void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st) {
         case FEW_32_32: go(mx4_few_kernel<2, 2, 8>, 512, kAll); break;
         case FEW_64_32: go(mx4_few_kernel<4, 2, 8>, 512, kAll); break;
         case FEW_64_64: go(mx4_few_kernel<4, 4, 8>, 512, kAll); break;
-        case TILE_128: go(mx4_tile_kernel<2, 2>, 256, units(2)); break;
-        case TILE_256: go(mx4_tile_kernel<4, 4>, 256, units(1)); break;
+        case TILE_128: go(mx4_tile_kernel<2, 2>, 256, p.KB > kStages ? 512 : kAll); break;
+        case TILE_256: go(mx4_tile_kernel<4, 4>, 256, 256); break;
     }
     profile_after(st);
 }
