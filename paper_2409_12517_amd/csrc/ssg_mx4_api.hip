@@ -233,7 +233,7 @@ ssg_status ssg_mx4_linear_bwd(const void *dy, ssg_dtype dy_dtype, int64_t lddy, 
     const char *who = "ssg_mx4_linear_bwd";
     SSG_CHECK(check_bwd_shape(who, M, N, K));
     SSG_CHECK(check_rule(who, rule));
-    if (!dx && !dW && M > 0) return fail(SSG_ERR_ARG, "%s: dx and dW are both NULL", who);
+    if (!dx && !dW) return fail(SSG_ERR_ARG, "%s: dx and dW are both NULL", who);
     SSG_CHECK(check_rows_of(who, "dy", dy, dy_dtype, M, N, lddy));
     if (dx) {
         SSG_CHECK(check_rows_of(who, "dx", dx, dx_dtype, M, K, lddx));
@@ -323,7 +323,7 @@ ssg_status ssg_rmsnorm_bwd(const ssg_rmsnorm_desc *desc, const void *dy, ssg_dty
     SSG_CHECK(check_ptr(who, "ds", ds, 16, false));
     if (dx) SSG_CHECK(check_rows_of(who, "dx", dx, (ssg_dtype)desc->x_dtype, T, d, desc->ldx));
     SSG_CHECK(check_ptr(who, "dresidual", dresidual, 16, false));
-    SSG_CHECK(check_ptr(who, "dw", dw, 4, false));
+    SSG_CHECK(check_ptr(who, "dw", dw, 16, false));
     if (dw) {
         SSG_CHECK(check_ptr(who, "workspace", workspace, 16, true));
         const size_t need = ssg_rmsnorm_bwd_workspace_bytes(desc);

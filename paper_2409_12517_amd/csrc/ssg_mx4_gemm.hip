@@ -590,7 +590,6 @@ struct Mx4Extent { int rows, cols; };
 constexpr Mx4Extent kExtents[] = {{16, 16}, {32, 16}, {32, 32}, {64, 32}, {64, 64}, {128, 128}, {256, 256}};
 int64_t count_of(const Mx4GemmArgs &a, Mx4Form f) { return (a.M + kExtents[f].rows - 1) / kExtents[f].rows * ((a.N + kExtents[f].cols - 1) / kExtents[f].cols); }
 Mx4Form choose_form(const Mx4GemmArgs &a) {
-    if (a.K == 0) return FEW_32_32;                      // zeros: the tiles' rings want something to load
     const double KB = (double)(mx4_width(a.K) / 128);
     for (Mx4Form f : {FEW_16_16, FEW_32_16, FEW_32_32, FEW_64_32, FEW_64_64})
         if (kExtents[f].rows < a.M + 16 && count_of(a, f) <= 256 && (f != FEW_64_64 || KB >= 20)) return f;
@@ -616,6 +615,12 @@ I8Plan mx4_gemm_plan(const Mx4GemmArgs &a) {
     return {form >= TILE_128 ? kExtents[form].rows : 0, kExtents[form].rows, kExtents[form].cols};
 }
 
+// Sums of nothing: 16 bytes to a thread.
+__global__ __launch_bounds__(256) static void mx4_zero_kernel(void *C, int64_t M, int64_t N, int64_t ldc, int size) {
+    const int64_t i = block_of_many() * 256 + threadIdx.x, pieces = N * size / 16, row = i / pieces;
+    if (row < M) *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(C) + row * ldc * size + i % pieces * 16) = make_uint4(0, 0, 0, 0);
+}
+
 static Mx4Params params_of(const Mx4GemmArgs &a, Mx4Form form) {
     Mx4Params p;
     p.A = a.A; p.B = a.B; p.sa = a.sa; p.sb = a.sb; p.C = a.C; p.M = a.M; p.N = a.N; p.ldc = a.ldc; p.KB = (int)(mx4_width(a.K) / 128); p.c_f32 = a.c_f32;
@@ -625,7 +630,7 @@ static Mx4Params params_of(const Mx4GemmArgs &a, Mx4Form form) {
 
 // Where both have small tiles and the chip holds them all at once, one launch (777 x 2064 -> 1376 and its weights' gradient 8.1 + 5.8 us in two).
 void launch_mx4_gemm_pair(const Mx4GemmArgs &a, const Mx4GemmArgs &b, hipStream_t st) {
-    if (a.M > 0 && b.M > 0 && choose_form(a) == TILE_128 && choose_form(b) == TILE_128 && count_of(a, TILE_128) + count_of(b, TILE_128) <= 512) {
+    if (a.M > 0 && b.M > 0 && a.K > 0 && b.K > 0 && choose_form(a) == TILE_128 && choose_form(b) == TILE_128 && count_of(a, TILE_128) + count_of(b, TILE_128) <= 512) {
         const int first = (int)count_of(a, TILE_128), all = first + (int)count_of(b, TILE_128);
         profile_before(kTagMx4Gemm, st);
         hipLaunchKernelGGL((mx4_tile_pair_kernel<2, 2>), dim3(all), dim3(256), 0, st, params_of(a, TILE_128), params_of(b, TILE_128), first);
@@ -638,6 +643,11 @@ void launch_mx4_gemm_pair(const Mx4GemmArgs &a, const Mx4GemmArgs &b, hipStream_
 
 void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st) {
     if (a.M == 0) return;
+    if (a.K == 0) {
+        const int size = a.c_f32 ? 4 : 2;
+        hipLaunchKernelGGL(mx4_zero_kernel, grid_of_many((a.M * (a.N * size / 16) + 255) / 256), dim3(256), 0, st, a.C, a.M, a.N, a.ldc, size);
+        return;
+    }
     const Mx4Form form = choose_form(a);
     const Mx4Params p = params_of(a, form);
     auto go = [&](auto kernel, int threads, int64_t most) {

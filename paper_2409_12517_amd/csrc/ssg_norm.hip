@@ -380,9 +380,9 @@ template <bool DYBF16, bool SBF16> void launch_norm_bwd_as(const NormBwdArgs &a,
     else if (runs <= 64) as(Share<256, 4, 64>{}, kHeld<1>);
     else if (runs <= 128) as(Share<256, 2, 32>{}, kHeld<1>);
     else if (runs <= 256) as(Share<256, 1, 64>{}, kHeld<1>);
-    else if (runs <= 512) as(Share<256, 1, 64>{}, kHeld<2>);
-    else if (runs <= 768) as(Share<256, 1, 64>{}, kHeld<3>);
-    else if (runs <= 1024) as(Share<512, 1, 64>{}, kHeld<2>);
+    else if (runs <= 512) as(Share<512, 1, 64>{}, kHeld<1>);
+    else if (runs <= 768) as(Share<768, 1, 64>{}, kHeld<1>);
+    else if (runs <= 1024) as(Share<1024, 1, 64>{}, kHeld<1>);
     else if (runs <= 1536) as(Share<512, 1, 64>{}, kHeld<3>);
     else if (runs <= 2048) as(Share<512, 1, 64>{}, kHeld<4>);
     else as(Share<1024, 1, 64>{}, kHeld<4>);

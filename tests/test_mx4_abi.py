@@ -87,6 +87,28 @@ def test_linear_bwd_refusals(status, word, change):
     refused(status, word, ssg.ssg_mx4_linear_bwd, *args, **more)
 
 
+def test_nothing_to_compute_is_refused_without_rows_too():
+    args, more = bwd(M=0, dx=None, dW=None)
+    refused(ssg.SSG_ERR_ARG, "both NULL", ssg.ssg_mx4_linear_bwd, *args, **more)
+
+
+def test_plan():
+    """Host logic only: which kernel a product runs in."""
+    def plan(*args):
+        p = ssg.ssg_mx4_gemm_plan(*args)
+        return p.tile or (p.rows, p.cols)
+
+    assert [plan(M, 4096, 4096) for M in (1, 16, 17, 32, 33, 64, 128, 256)] == [(16, 16)] * 2 + [(32, 16)] * 2 + [(32, 32)] * 2 + [(64, 32), (64, 64)]
+    # more workgroups than compute units in any block: by rows
+    assert [plan(M, 11008, 4096) for M in (1, 16, 32, 64, 65, 512)] == [(16, 16), (16, 16), (32, 16), (64, 64), 128, 128]
+    assert plan(64, 16400, 4096) == (32, 32)
+    # few columns: the smallest blocks whose workgroups the chip holds at once
+    assert [plan(M, 1040, 2736) for M in (32, 64, 128, 256)] == [(16, 16), (32, 16), (32, 32), (64, 32)]
+    # 64 x 64 for long sums only
+    assert plan(512, 1376, 2560) == (64, 64) and plan(512, 1376, 2304) == 128
+    assert plan(4096, 4096, 11008) == 256 == plan(4096, 11008, 4096) and plan(2048, 4096, 11008) == 128 and plan(8192, 8192, 512) == 128
+
+
 def fwd(desc, x=4096, residual=None, w=4096, residual_out=None, y=4096, y_scale=None, y_amax=None, rstd=4096, y_bytes=BIG):
     return (desc, x, residual, w, residual_out, y, y_scale, y_amax, rstd), {"y_bytes": y_bytes}
 
@@ -141,6 +163,7 @@ def test_norm_buffers():
     no_bwd(ssg.SSG_ERR_ARG, "all NULL", plain, dx=None, dw=None)
     no_bwd(ssg.SSG_ERR_ARG, "w is NULL", plain, w=None)
     no_bwd(ssg.SSG_ERR_ARG, "ds is not", res, ds=4104)
+    no_bwd(ssg.SSG_ERR_ARG, "dw is not", plain, dw=4100)
     no_bwd(ssg.SSG_ERR_ARG, "workspace is NULL", plain, work=None)
     no_bwd(ssg.SSG_ERR_WORKSPACE, "workspace holds", plain, nbytes=ssg.ssg_rmsnorm_bwd_workspace_bytes(plain) - 1)
     ssg.ssg_rmsnorm_fwd(ssg.make_rmsnorm_desc(0, 64, 1e-5), None, None, 4096, None, None, None, None, None, stream=0)     # no rows: nothing to do
