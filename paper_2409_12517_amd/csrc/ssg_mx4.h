@@ -20,6 +20,18 @@ __device__ __forceinline__ uint32_t mx4_scale_byte(uint32_t top_bits, int ceil) 
 }
 __device__ __forceinline__ float mx4_scale(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x400000u); }
 
+// The word of the lane beside (D = 1) or one over (D = 2) among four neighbouring ones.
+template <int D> __device__ __forceinline__ uint32_t quad_xor(uint32_t v) {
+    static_assert(D == 1 || D == 2, "of four");
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, D == 1 ? 0xb1 : 0x4e, 0xf, 0xf, true);     // quad_perm [1,0,3,2], [2,3,0,1]
+}
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    uint32_t o = quad_xor<1>(v);
+    v = v > o ? v : o;
+    o = quad_xor<2>(v);
+    return v > o ? v : o;
+}
+
 // Eight values to eight codes, by the conversion instruction (nearest, ties to even codes, saturating), which divides by the scale itself.
 __device__ __forceinline__ uint32_t mx4_codes8(const float (&v)[8], float scale) {
     uint32_t c = 0;

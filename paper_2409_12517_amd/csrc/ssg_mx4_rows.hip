@@ -45,20 +45,19 @@ inline int64_t both_tiles_n(int64_t N, bool rows, bool bf16) { const int cols = 
 inline int64_t both_tiles(int64_t M, int64_t N, bool rows, bool bf16) { return mx4_width(M) / kTileTokens * both_tiles_n(N, rows, bf16); }
 
 // a four by four transpose of words among four neighbouring lanes: lane i's word j becomes lane j's word i
-__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
-    const int lane = threadIdx.x & 3;
+template <int D> __device__ __forceinline__ void exchange4(uint32_t (&w)[4]) {
+    const bool up = threadIdx.x & D;                         // gives word j and takes word j + D; the others the other way round
 #pragma unroll
-    for (int d = 1; d < 4; d *= 2) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j & d) continue;
-            const bool up = lane & d;                        // gives word j and takes word j + d; the others the other way round
-            const uint32_t out = up ? w[j] : w[j + d];
-            const uint32_t in = (uint32_t)__shfl_xor((int)out, d, 64);
-            if (up) w[j] = in;
-            else w[j + d] = in;
-        }
+    for (int j = 0; j < 4; ++j) {
+        if (j & D) continue;
+        const uint32_t in = quad_xor<D>(up ? w[j] : w[j + D]);
+        w[j] = up ? in : w[j];
+        w[j + D] = up ? w[j + D] : in;
     }
+}
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+    exchange4<1>(w);
+    exchange4<2>(w);
 }
 
 template <bool BF16> __device__ __forceinline__ void both_tile(const Mx4Both &a, int64_t tile, uint32_t (*lds)[128]) {
@@ -98,12 +97,7 @@ template <bool BF16> __device__ __forceinline__ void both_tile(const Mx4Both &a,
 #pragma unroll
             for (int i = 0; i < kWords; ++i) top = larger(top, w[e][i] & kAbs);
             if (BF16) top = (top & 0xffff0000u) > top << 16 ? top & 0xffff0000u : top << 16;
-#pragma unroll
-            for (int d = 1; d < 4; d *= 2) {
-                const uint32_t o = (uint32_t)__shfl_xor((int)top, d, 64);
-                top = top > o ? top : o;
-            }
-            byte[e] = mx4_scale_byte(top, a.ceil);
+            byte[e] = mx4_scale_byte(quad_max(top), a.ceil);
             if constexpr (BF16) code[e] = mx4_codes8(w[e], mx4_scale(byte[e]));
             else {
                 float f[8];

@@ -209,8 +209,7 @@ template <bool XBF16, int RES, int OUT, class SHARE, int HELD> __global__ __laun
             uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = Larger{}(top, __float_as_uint(s[i][j]) & 0x7fffffffu);
-            top = Larger{}(top, __shfl_xor(top, 1, 64));     // (four neighbouring threads have the four runs of a block)
-            top = Larger{}(top, __shfl_xor(top, 2, 64));
+            top = quad_max(top);                             // (four neighbouring threads have the four runs of a block)
             if (col >= padded) continue;
             const uint32_t byte = mx4_scale_byte(top, a.ceil);
             const uint32_t codes = byte == 255u ? 0u : mx4_codes8(s[i], mx4_scale(byte));
