@@ -72,6 +72,11 @@ __device__ __forceinline__ void store4(const Mx4Params &p, int64_t row, int64_t 
 // A workgroup has several tiles one after the other and the rings run on from one to the next: while a tile's last steps are
 // multiplied and its results stored, the first stages of the next are on their way.  A tile with no more rows than half
 // loads and multiplies half of them.
+// Bound by the matrix cores under the chip's power: 4096 x 4096 x 11008 takes 83 to 85 us, 4.4 PFLOP/s, the MFMAs half of the cycles at 2.1 GHz; without its
+// loads to LDS 75, without those, the reads and the stores 67, and MFMAs alone hold 5 to 6 PFLOP/s at 1.5 to 1.9 GHz on random codes.  4096 x 11008 x 4096 100 us:
+// 688 tiles are 2.7 rounds of 256, and the stores of a round take half a step's time from the loads behind them.  8192^3 238 us, 4.6 PFLOP/s.  (16 x 16 x 128
+// MFMAs 103 us for 85; results through LDS and the wait for their stores before the next tile's first step 113 for 100; tiles of 128 x 256 twice on a
+// compute unit, three stages each, 91 for 85 and 110 for 100; non-temporal stores, groups of two or eight row tiles, loads all at once: within 4 %.)
 constexpr int kStages = 4, kScaleSlots = 2;
 static_assert(kStages % 2 == 0, "a pair's scales come with the first of two stages, and a tile's last stage with the second of a pair of steps");
 template <int TA, int TB> struct TileShape {
@@ -426,7 +431,8 @@ template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::
 
 // ---- few rows ------------------------------------------------------------------------------------------
 // RB blocks of 16 rows by CB blocks of 16 columns to a workgroup, whose waves share K out in pairs of blocks and add their sums in LDS, wave after
-// wave.  Both operands come straight from memory in the order of the lanes, U pairs' loads at a time.
+// wave.  Both operands come straight from memory in the order of the lanes, U pairs' loads at a time.  Bound by the weights' bytes and by the start
+// and end of one round of workgroups: 24 MB of 4096 x 11008 by up to 16 rows 7.0 us, 9 MB of 4096 x 4096 4.2.
 template <int RB, int CB, int WAVES> __global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(Mx4Params p) {
     __shared__ v4f_t part[WAVES][RB * CB][64];
     const int row_blocks = (int)((p.M + 15) / 16), col_blocks = (int)(p.N / 16), pairs = p.KB / 2;
@@ -507,7 +513,7 @@ template <int RB, int CB, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
 // ---- up to four rows, quantized on the way ------------------------------------------------------------------
 // 16 columns to a workgroup, whose waves share K out.  Its threads quantize the rows, a block each, into LDS while the first weights are on their way.
 // (In the registers of the lanes that multiply them, where four of 64 have a row's values, the vector ALU took 3 us: 1 x 4096 -> 11008
-// 10.6 us.)  Bound by the weights' bytes and the start and end of one round of workgroups.
+// 10.6 us for 7.5.)  Bound by the weights' bytes, 24 MB there, and the start and end of one round of workgroups.
 template <bool BF16, int WAVES> __global__ __launch_bounds__(64 * WAVES) void mx4_token_kernel(Mx4TokenArgs a) {
     constexpr int U = 4;                                     // pairs of blocks at a time
     extern __shared__ __attribute__((aligned(16))) uint8_t codes[];          // rows of Kp / 2, then their scales, rows of Kp / 32
