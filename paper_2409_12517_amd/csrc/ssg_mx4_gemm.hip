@@ -177,8 +177,9 @@ template <int TA, int TB> __device__ __forceinline__ void run_tiles(const Mx4Par
         for (int j = 0; j < TA; ++j) a_lane[j] = lane + src.a_off[j];
 #pragma unroll
         for (int j = 0; j < TB; ++j) b_lane[j] = lane + src.b_off[j];
-        const uint32_t block = (uint32_t)(s_first + lane_id / 8);
-        s_lane = (block < src.s_last ? block : src.s_last) * (uint32_t)KB * 64u + (lane_id & 7) * 16;
+        // in LDS, for every two blocks, what the 64 lanes read for a half lies side by side: half, run of 32, block, 8 rows
+        const uint32_t block = (uint32_t)(s_first + (lane_id >> 4) * 2 + (lane_id >> 1 & 1));
+        s_lane = (block < src.s_last ? block : src.s_last) * (uint32_t)KB * 64u + (lane_id >> 2 & 3) * 32 + (lane_id & 1) * 16;
     };
     take_lanes();
     // load j of a stage into `slot`: where to, and the load
@@ -249,7 +250,7 @@ template <int TA, int TB> __device__ __forceinline__ void run_tiles(const Mx4Par
         uint32_t xa[2][QA], xb[2][QB];
         // lanes 0 to 15 and 32 to 47 have the first block's rows, 16 to 31 and 48 to 63 the second's; the upper half of the lanes the next run of 32
         const int l16 = lane_id & 15, lhi = lane_id >> 4 & 1, run = lane_id >> 5;
-        const uint32_t frag_lane = lhi * 1024 + run * 256 + l16 * 16, scale_lane = lhi * 128 + (run * 16 + l16) * 2;
+        const uint32_t frag_lane = lhi * 1024 + run * 256 + l16 * 16, scale_lane = run * 64 + lhi * 32 + l16 * 2;
         const uint8_t *a_frag = smem + wm * QA * 2048 + frag_lane, *b_frag = smem + (kA + wn * 2 * TB) * 1024 + frag_lane;
         const uint8_t *a_scale = smem + kRing + wm * QA * 256 + scale_lane, *b_scale = smem + kRing + (kA + wn * 2 * TB) * 128 + scale_lane;
         // fragment i of a half in the order of use: the first column's and the rows', then the other columns'
@@ -258,8 +259,8 @@ template <int TA, int TB> __device__ __forceinline__ void run_tiles(const Mx4Par
             else fb[half][i == 0 ? 0 : i - QA] = *reinterpret_cast<const v4i_t *>(b_frag + slot + half * 512 + (i == 0 ? 0 : i - QA) * 2048);
         };
         auto read_scale = [&](int half, int i, uint32_t slot) {
-            if (i < QA) xa[half][i] = *reinterpret_cast<const uint16_t *>(a_scale + slot + half * 64 + i * 256);
-            else xb[half][i - QA] = *reinterpret_cast<const uint16_t *>(b_scale + slot + half * 64 + (i - QA) * 256);
+            if (i < QA) xa[half][i] = *reinterpret_cast<const uint16_t *>(a_scale + slot + half * 128 + i * 256);
+            else xb[half][i - QA] = *reinterpret_cast<const uint16_t *>(b_scale + slot + half * 128 + (i - QA) * 256);
         };
         // One half of a step; `other`: what is read and loaded between the MFMAs.
         auto multiply = [&](auto parity, auto half, auto &&other) {
@@ -676,7 +677,7 @@ void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st) {
 }
 
 static int64_t token_lds(int64_t M, int64_t K) { return M * (mx4_width(K) / 32 * 17); }
-bool mx4_token_ok(int64_t M, int64_t, int64_t K) { return M <= kMx4TokenRows && token_lds(M, K) <= kMx4TokenLds; }
+bool mx4_token_ok(int64_t M, int64_t K) { return M <= kMx4TokenRows && token_lds(M, K) <= kMx4TokenLds; }
 
 void launch_mx4_token(const Mx4TokenArgs &a, hipStream_t st) {
     profile_before(kTagMx4Gemm, st);

@@ -246,8 +246,9 @@ template <bool XBF16, int RES> void launch_norm_as(const NormArgs &a, hipStream_
         auto form = [&](auto out) {
             constexpr int OUT = decltype(out)::value;
             auto as = [&](auto share, auto held) { go(norm_kernel<XBF16, RES, OUT, decltype(share), decltype(held)::value>, share); };
-            if (OUT == OUT_I8 && runs <= 16) as(Share<256, 16, 4>{}, kHeld<1>);
-            else if (runs <= 32) as(Share<256, 8, 4>{}, kHeld<1>);
+            if constexpr (OUT == OUT_I8)                     // (4 bits fill rows up to 32 runs)
+                if (runs <= 16) return as(Share<256, 16, 4>{}, kHeld<1>);
+            if (runs <= 32) as(Share<256, 8, 4>{}, kHeld<1>);
             else if (runs <= 64) as(Share<256, 4, 4>{}, kHeld<1>);
             else if (runs <= 128) as(Share<256, 4, 4>{}, kHeld<2>);
             else if (runs <= 256) as(Share<512, 4, 4>{}, kHeld<2>);
