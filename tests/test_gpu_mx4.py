@@ -239,3 +239,36 @@ def test_linear_bwd(which, dtype, M, N, K, gap):
         if out is not None:
             got = f32(out)
             assert np.array_equal(got[:-1, :K], as_type(want, t)) and (got[:, K:] == 3).all() and (got[-1] == 3).all()
+
+
+@pytest.mark.parametrize("M,K", [(1, 92160), (1, 92416), (1, 94208), (2, 46080), (3, 30976), (4, 23040), (4, 23056)])
+def test_long_rows_of_few_tokens(M, K):
+    """On both sides of what a workgroup quantizes itself.  Scales of 1: terms of at most 36, whole numbers of quarters, whose sums stay below 2^24 quarters."""
+    gen = torch.Generator().manual_seed(K)
+    x = (torch.rand(M, K, generator=gen) * 12 - 6).to(torch.bfloat16)
+    x[:, ::32] = 5.0
+    qw, w = operand(32, K, 5, 0, 0)
+    y = torch.empty(M, 32, device=DEV)
+    ssg.ssg_mx4_linear(x.to(DEV), ssg.SSG_BF16, M, K, K, 0, qw, 32, y, ssg.SSG_F32, 32, buffer(M, K))
+    assert np.array_equal(f32(y), as_type(mx4.values(*mx4.quantize(f32(x))) @ w.T, torch.float32))
+
+
+@pytest.mark.parametrize("dy_dtype,x_dtype,dx_dtype,dw_dtype", [(torch.bfloat16, torch.float32, torch.float32, torch.bfloat16),
+                                                                 (torch.float32, torch.bfloat16, torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("rule", [ssg.SSG_MX_FLOOR, ssg.SSG_MX_CEIL])
+@pytest.mark.parametrize("M,N,K", [(45, 48, 272), (700, 1040, 528), (2100, 2064, 1376)])
+def test_linear_bwd_of_mixed_types(dy_dtype, x_dtype, dx_dtype, dw_dtype, rule, M, N, K):
+    """Sums of N, and of M, terms in fp32, each addition off by at most 2^-23 of a partial sum; results in bf16 rounded once more, by half a step."""
+    dy, x = spread(M, N, 1).to(dy_dtype), spread(M, K, 2).to(x_dtype)
+    W = spread(K, N, 3)
+    qt = buffer(K, N, 0)
+    ssg.ssg_mx4_quantize(W.to(DEV), ssg.SSG_F32, K, N, N, 0, rule, qt)
+    dx, dW = torch.empty(M, K, dtype=dx_dtype, device=DEV), torch.empty(N, K, dtype=dw_dtype, device=DEV)
+    work = torch.full((ssg.ssg_mx4_linear_bwd_workspace_bytes(M, N, K),), 0xA5, dtype=torch.uint8, device=DEV)
+    ssg.ssg_mx4_linear_bwd(dy.to(DEV), SSG[dy_dtype], N, x.to(DEV), SSG[x_dtype], K, M, N, K, rule, qt, dx, SSG[dx_dtype], K, dW, SSG[dw_dtype], K, work)
+    ceil = rule == ssg.SSG_MX_CEIL
+    a, b, wt = (mx4.values(*mx4.quantize(v, ceil)) for v in (f32(dy), f32(dy).T, f32(W)))
+    xt = mx4.values(*mx4.quantize(f32(x).T, ceil))
+    for out, t, p, q, n in ((dx, dx_dtype, a, wt, N), (dW, dw_dtype, b, xt, M)):
+        want, off = p @ q.T, n * 2.0 ** -23 * (np.abs(p) @ np.abs(q).T)
+        assert (np.abs(f32(out) - want) <= off + (2.0 ** -8 * (np.abs(want) + off) if t == torch.bfloat16 else 0)).all()

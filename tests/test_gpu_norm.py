@@ -204,3 +204,72 @@ def test_backward_of_no_rows():
     ssg.ssg_rmsnorm_bwd(desc, None, ssg.SSG_BF16, 80, None, None, torch.ones(80, dtype=BF, device=DEV), None, None, None, dw,
                         torch.empty(ssg.ssg_rmsnorm_bwd_workspace_bytes(desc), dtype=torch.uint8, device=DEV))
     assert not dw.any()
+
+
+@pytest.mark.parametrize("T,d", [(1, 64), (37, 80), (19, 528), (5, 4096), (3, 11008)])
+@pytest.mark.parametrize("form", [ssg.SSG_NORM_BF16, ssg.SSG_NORM_F32, ssg.SSG_NORM_E4M3])
+def test_strides(T, d, form):
+    """Rows inside wider matrices: the same results, and what lies between and behind them stays."""
+    dtype = {ssg.SSG_NORM_BF16: BF, ssg.SSG_NORM_F32: F, ssg.SSG_NORM_E4M3: torch.uint8}[form]
+    x, r, w = rows(T, d, BF, 1), rows(T, d, F, 2), weights(d, BF)[0].to(DEV)
+    scale = torch.tensor([30.0], device=DEV) if form == ssg.SSG_NORM_E4M3 else None
+
+    def run(gx, gr, gy):
+        xs, rs = torch.full((T + 1, d + gx), 7.0, dtype=BF, device=DEV), torch.full((T + 1, d + gr), 7.0, device=DEV)
+        xs[:T, :d], rs[:T, :d] = x.to(DEV), r.to(DEV)
+        kept, y, rstd = torch.full_like(rs, 5.0), torch.full((T + 1, d + gy), 5, dtype=dtype, device=DEV), torch.full((T + 1,), 5.0, device=DEV)
+        desc = ssg.make_rmsnorm_desc(T, d, EPS, residual=1, r_dtype=ssg.SSG_F32, y_format=form, ldx=d + gx, ldr=d + gr, ldy=d + gy)
+        ssg.ssg_rmsnorm_fwd(desc, xs, rs, w, kept, y, scale, None, rstd)
+        for t in (kept, y):
+            assert bool((t[T] == 5).all()) and bool((t[:, d:] == 5).all())
+        assert float(rstd[T]) == 5
+        # the gradient with the same strides
+        dy, ds = rows(T, d, BF, 3, 8).to(DEV), torch.full_like(rs, 7.0)
+        ds[:T, :d] = rows(T, d, F, 4).to(DEV)
+        dx, dr, dw = torch.full_like(xs, 5.0), torch.full_like(rs, 5.0), torch.empty(d, device=DEV)
+        work = torch.empty(ssg.ssg_rmsnorm_bwd_workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+        ssg.ssg_rmsnorm_bwd(desc, dy, ssg.SSG_BF16, d + 8, kept, rstd, w, ds, dx, dr, dw, work)
+        for t in (dx, dr):
+            assert bool((t[T] == 5).all()) and bool((t[:, d:] == 5).all())
+        return [kept[:T, :d], y[:T, :d], rstd[:T], dx[:T, :d], dr[:T, :d], dw]
+
+    assert all(torch.equal(a, b) for a, b in zip(run(0, 0, 0), run(8, 4, 16)))
+
+
+def test_gradient_without_weights():
+    T, d = 40, 528
+    s, dy = rows(T, d, F, 1), rows(T, d, F, 2)
+    rstd = torch.from_numpy(norm.forward(f32(s), np.ones(d), EPS)[1].astype(np.float32))
+    dx = torch.empty(T, d, device=DEV)
+    ssg.ssg_rmsnorm_bwd(ssg.make_rmsnorm_desc(T, d, EPS, x_dtype=ssg.SSG_F32), dy.to(DEV), ssg.SSG_F32, d, s.to(DEV), rstd.to(DEV), None, None, dx, None, None, None)
+    want, _ = norm.backward(f32(dy), f32(s), rstd.numpy(), np.ones(d))
+    off, _ = backward_bounds(f32(dy), f32(s), rstd.numpy(), np.ones(d, np.float32))
+    assert (np.abs(f32(dx) - want) <= off + STEP[F] * (np.abs(want) + off)).all()
+
+
+@pytest.mark.parametrize("d", [64, 528, 4096])
+def test_gradient_against_differences(d):
+    """sum(y dy) along a direction v: the central difference of the forward pass is off by h^2 / 6 of its third derivative, whose terms are bounded by 15 |v|^3 rstd^3
+    times |y dy|, and by the forward pass's rounding over h."""
+    T, h = 3, 2.0 ** -5
+    s, dy, v = rows(T, d, F, 1), rows(T, d, F, 2), torch.randn(T, d, generator=torch.Generator().manual_seed(3))
+    w, g = weights(d, F)
+    desc = ssg.make_rmsnorm_desc(T, d, EPS, x_dtype=ssg.SSG_F32, w_dtype=ssg.SSG_F32, y_format=ssg.SSG_NORM_F32)
+
+    def total(x):
+        y, rstd = torch.empty(T, d, device=DEV), torch.empty(T, device=DEV)
+        ssg.ssg_rmsnorm_fwd(desc, x.to(DEV), None, w.to(DEV), None, y, None, None, rstd)
+        return (f32(y).astype(np.float64) * f32(dy)).sum(-1), f32(y), rstd
+
+    _, y0, rstd = total(s)
+    ds = torch.empty(T, d, device=DEV)
+    ssg.ssg_rmsnorm_bwd(desc, dy.to(DEV), ssg.SSG_F32, d, s.to(DEV), rstd, w.to(DEV), None, ds, None, None, None)
+    got = (f32(ds).astype(np.float64) * f32(v)).sum(-1)
+    up, y1, _ = total(s + h * v)
+    down, y2, _ = total(s - h * v)
+    a = np.abs(f32(dy).astype(np.float64))
+    speed = np.sqrt((f32(v).astype(np.float64) ** 2).mean(-1)) * rstd.cpu().numpy()               # |v| in the rows' own units
+    third = 15 * speed ** 2 * ((np.abs(f32(v)) * rstd.cpu().numpy()[:, None] + speed[:, None] * np.abs(y0 / g)) * np.abs(g) * a).sum(-1)
+    rounding = (2.0 ** -24 + Y) * (a * (np.abs(y1) + np.abs(y2))).sum(-1) / (2 * h)
+    off, _ = backward_bounds(f32(dy), f32(s), rstd.cpu().numpy(), g)
+    assert (np.abs((up - down) / (2 * h) - got) <= h * h / 6 * third + rounding + (off * np.abs(f32(v))).sum(-1)).all()
