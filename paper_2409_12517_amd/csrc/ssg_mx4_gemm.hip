@@ -73,7 +73,7 @@ __device__ __forceinline__ void store4(const Mx4Params &p, int64_t row, int64_t 
 // multiplied and its results stored, the first stages of the next are on their way.  A tile with no more rows than half
 // loads and multiplies half of them.
 // Bound by the matrix cores under the chip's power: 4096 x 4096 x 11008 takes 83 to 85 us, 4.4 PFLOP/s, the MFMAs half of the cycles at 2.1 GHz; without its
-// loads to LDS 75, without those, the reads and the stores 67, and MFMAs alone hold 5 to 6 PFLOP/s at 1.5 to 1.9 GHz on random codes.  4096 x 11008 x 4096 100 us:
+// loads to LDS 75, without those, the reads and the stores 67, and MFMAs alone hold 5 to 6 PFLOP/s at 1.5 to 1.9 GHz on random codes; operands of zeros 59.  4096 x 11008 x 4096 99 us:
 // 688 tiles are 2.7 rounds of 256, and the stores of a round take half a step's time from the loads behind them.  8192^3 238 us, 4.6 PFLOP/s.  (16 x 16 x 128
 // MFMAs 103 us for 85; results through LDS and the wait for their stores before the next tile's first step 113 for 100; tiles of 128 x 256 twice on a
 // compute unit, three stages each, 91 for 85 and 110 for 100; non-temporal stores, groups of two or eight row tiles, loads all at once: within 4 %.)

@@ -249,8 +249,10 @@ def test_gradient_without_weights():
 
 @pytest.mark.parametrize("d", [64, 528, 4096])
 def test_gradient_against_differences(d):
-    """sum(y dy) along a direction v: the central difference of the forward pass is off by h^2 / 6 of its third derivative, whose terms are bounded by 15 |v|^3 rstd^3
-    times |y dy|, and by the forward pass's rounding over h."""
+    """sum(y dy) along a direction v: a central difference is off by h^2 / 6 of the third derivative between its ends, and by the forward
+    pass's rounding over h.  With m = mean(s^2) + eps, r = m^-1/2 and V^2 = mean(v^2): the first derivative of m is at most 2 V / r (Cauchy and
+    Schwarz), its second is 2 V^2, so the second of m^-1/2 is at most 4 V^2 r^3, the third at most 24 V^3 r^4, and that of y = g s m^-1/2 at most
+    |g| (24 |s| V^3 r^4 + 12 |v| V^2 r^3).  Up to h away r is at most r / (1 - h V r) and |s| grows by h |v|."""
     T, h = 3, 2.0 ** -5
     s, dy, v = rows(T, d, F, 1), rows(T, d, F, 2), torch.randn(T, d, generator=torch.Generator().manual_seed(3))
     w, g = weights(d, F)
@@ -261,15 +263,18 @@ def test_gradient_against_differences(d):
         ssg.ssg_rmsnorm_fwd(desc, x.to(DEV), None, w.to(DEV), None, y, None, None, rstd)
         return (f32(y).astype(np.float64) * f32(dy)).sum(-1), f32(y), rstd
 
-    _, y0, rstd = total(s)
+    rstd = total(s)[2]
     ds = torch.empty(T, d, device=DEV)
     ssg.ssg_rmsnorm_bwd(desc, dy.to(DEV), ssg.SSG_F32, d, s.to(DEV), rstd, w.to(DEV), None, ds, None, None, None)
     got = (f32(ds).astype(np.float64) * f32(v)).sum(-1)
     up, y1, _ = total(s + h * v)
     down, y2, _ = total(s - h * v)
     a = np.abs(f32(dy).astype(np.float64))
-    speed = np.sqrt((f32(v).astype(np.float64) ** 2).mean(-1)) * rstd.cpu().numpy()               # |v| in the rows' own units
-    third = 15 * speed ** 2 * ((np.abs(f32(v)) * rstd.cpu().numpy()[:, None] + speed[:, None] * np.abs(y0 / g)) * np.abs(g) * a).sum(-1)
+    r = rstd.cpu().numpy().astype(np.float64)[:, None]
+    V = np.sqrt((f32(v).astype(np.float64) ** 2).mean(-1, keepdims=True))
+    assert (h * V * r < 0.9).all()
+    r = r / (1 - h * V * r)
+    third = (np.abs(g) * a * (24 * (np.abs(f32(s)) + h * np.abs(f32(v))) * V ** 3 * r ** 4 + 12 * np.abs(f32(v)) * V ** 2 * r ** 3)).sum(-1)
     rounding = (2.0 ** -24 + Y) * (a * (np.abs(y1) + np.abs(y2))).sum(-1) / (2 * h)
     off, _ = backward_bounds(f32(dy), f32(s), rstd.cpu().numpy(), g)
     assert (np.abs((up - down) / (2 * h) - got) <= h * h / 6 * third + rounding + (off * np.abs(f32(v))).sum(-1)).all()
