@@ -7,26 +7,30 @@ namespace ssg {
 
 namespace {
 
-// A wave has 16 rows by 256 columns: lane l row l % 16 and in each half the l / 16-th run of 32, so that the codes of a half leave as
-// one piece of 1 KB and the scales as one of 128 bytes.  (A lane's four loads
-// of 16 bytes take the same cache lines.)  Bound by memory: 4096 x 11008 bf16, 114 MB, 22.8 us, 5.0 TB/s, what a large copy reaches.
-template <bool BF16> __global__ __launch_bounds__(256) void mx4_rows_kernel(Mx4RowsArgs a) {
-    const int64_t pairs = mx4_width(a.K) / 256, wave = block_of_many() * 4 + threadIdx.x / 64, rb = wave / pairs, p = wave % pairs;
+// A wave has 16 rows by 256 columns, or with HALVES = 1 by 128: lane l row l % 16 and in each half the l / 16-th run of 32, so that the codes of a half leave
+// as one piece of 1 KB and the scales as one of 128 bytes (of 64 pieces of one where there is one half).  (A lane's four loads of 16 bytes take the same
+// cache lines.)  Bound by memory: 4096 x 11008 bf16, 114 MB, 22.4 us, 5.1 TB/s, what a large copy reaches; little ones by latency, so a wave is a block by itself, on
+// any compute unit, and has one half where there are few: 333 x 2736 bf16 2.5 us, two halves 2.6, four waves to a block 2.9, in fp32 3.1, 3.0 and 4.0;
+// 64 x 4096 fp32 2.4, 2.7 and 4.0; 1024 x 4096 bf16 4.1, 4.3 and 4.1; 4096 x 4096 8.6, 8.2 and 8.3.
+template <bool BF16, int HALVES> __global__ __launch_bounds__(64) void mx4_rows_kernel(Mx4RowsArgs a) {
+    const int64_t pairs = mx4_width(a.K) / 256, wave = block_of_many() / (2 / HALVES), rb = wave / pairs, p = wave % pairs;
     if (rb * 16 >= a.rows) return;
-    const int l = threadIdx.x & 63, g = l >> 4;
+    const int l = threadIdx.x, g = l >> 4, first = HALVES == 1 ? (int)(block_of_many() & 1) : 0;
     const int64_t row = rb * 16 + (l & 15);
     const uint8_t *src = static_cast<const uint8_t *>(a.src) + row * a.ld * (BF16 ? 2 : 4);
-    Mx4Block<BF16> v[2];
+    Mx4Block<BF16> v[HALVES];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) v[h].load(src, p * 256 + h * 128 + g * 32, a.K, row < a.rows);
+    for (int h = 0; h < HALVES; ++h) v[h].load(src, p * 256 + (first + h) * 128 + g * 32, a.K, row < a.rows);
     uint32_t bytes = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < HALVES; ++h) {
         const uint32_t byte = mx4_scale_byte(v[h].top_bits(), a.ceil);
         bytes |= byte << 8 * h;
-        *reinterpret_cast<uint4 *>(a.codes + ((rb * pairs + p) * 2 + h) * 1024 + l * 16) = v[h].codes(byte);
+        *reinterpret_cast<uint4 *>(a.codes + ((rb * pairs + p) * 2 + first + h) * 1024 + l * 16) = v[h].codes(byte);
     }
-    *reinterpret_cast<uint16_t *>(a.scales + (rb * pairs + p) * 128 + l * 2) = (uint16_t)bytes;
+    uint8_t *scales = a.scales + (rb * pairs + p) * 128 + l * 2 + first;
+    if (HALVES == 2) *reinterpret_cast<uint16_t *>(scales) = (uint16_t)bytes;
+    else *scales = (uint8_t)bytes;
 }
 
 // The transpose, and with it the rows where both are wanted: a block has 64 of the source's rows (tokens) by 512 bytes of each.  Its threads read pieces of
@@ -284,8 +288,12 @@ void launch_mx4_quantize(const Mx4RowsArgs &a, hipStream_t st) {
         if (a.bf16) hipLaunchKernelGGL((mx4_columns_kernel<true, true>), grid_of_many(tiles), dim3(256), 0, st, b, b, tiles, tiles);
         else hipLaunchKernelGGL((mx4_columns_kernel<false, false>), grid_of_many(tiles), dim3(256), 0, st, b, b, tiles, tiles);
     } else {
-        if (a.bf16) hipLaunchKernelGGL(mx4_rows_kernel<true>, grid_of_pairs(a.rows, a.K), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL(mx4_rows_kernel<false>, grid_of_pairs(a.rows, a.K), dim3(256), 0, st, a);
+        const int64_t pairs = (a.rows + 15) / 16 * (mx4_width(a.K) / 256);
+        auto go = [&](auto kernel, int64_t blocks) { hipLaunchKernelGGL(kernel, grid_of_many(blocks), dim3(64), 0, st, a); };
+        if (a.bf16 && pairs <= 1024) go(mx4_rows_kernel<true, 1>, 2 * pairs);
+        else if (a.bf16) go(mx4_rows_kernel<true, 2>, pairs);
+        else if (pairs <= 1024) go(mx4_rows_kernel<false, 1>, 2 * pairs);
+        else go(mx4_rows_kernel<false, 2>, pairs);
     }
     profile_after(st);
 }
