@@ -43,15 +43,19 @@ template <int STEP> __device__ __forceinline__ v16f mfma_mx4_wide(const v4i_t &w
 }
 
 // Tile number v of rows * tiles_n: the column tiles of one row tile after the other in groups of four row tiles, and eight contiguous
-// ranges of that order for the eight XCDs.
+// ranges of that order for the eight XCDs.  Each group starts TURN columns behind the one before: from the same column on, XCDs whose ranges start
+// with a group would write one part of every row at the same time, and with it a part of the memory's channels (fp32 results 4096 x 16384 x 2048 160 us,
+// 112 turned; 4096 x 16384 x 512 in small tiles 93 and 70; 4096 x 11008 x 512 65 and 47; bf16 4096 x 16384 x 2048 103 and 88; at worst 8192 x 4096 x 512 39.9 and 41.7).
+constexpr int kGroup = 4;
 struct Mx4Tile { int rb, cb; };                          // first row block and column block
-__device__ __forceinline__ Mx4Tile find_tile(const Mx4Params &p, int row_blocks, int col_blocks, int rows, int v) {
+template <int TURN> __device__ __forceinline__ Mx4Tile find_tile(const Mx4Params &p, int row_blocks, int col_blocks, int rows, int v) {
     const int all = rows * p.tiles_n, full = all & ~7;
     const int t = v < full ? (v & 7) * (full >> 3) + (v >> 3) : v;
-    constexpr int kGroup = 4;
     const int group = t / (kGroup * p.tiles_n), in_group = t - group * (kGroup * p.tiles_n);
     const int height = rows - group * kGroup < kGroup ? rows - group * kGroup : kGroup;
-    return {__builtin_amdgcn_readfirstlane((group * kGroup + in_group % height) * row_blocks), __builtin_amdgcn_readfirstlane(in_group / height * col_blocks)};
+    int col = in_group / height;
+    if (TURN > 0) col = (col + group * TURN) % p.tiles_n;
+    return {__builtin_amdgcn_readfirstlane((group * kGroup + in_group % height) * row_blocks), __builtin_amdgcn_readfirstlane(col * col_blocks)};
 }
 
 // Four neighbouring columns of a row.
@@ -84,6 +88,7 @@ template <int TA, int TB> struct TileShape {
     static constexpr int kRows = 16 * kA, kCols = 16 * kB, kStage = (kA + kB) * 1024, kRing = kStages * kStage;
     static constexpr int kScales = (kA + kB) * 128;      // of a pair: the rows', then the columns'
     static constexpr int kLds = kRing + kScaleSlots * kScales, kAtOnce = 163840 / kLds;
+    static constexpr int kTurn = 32 * kAtOnce / kGroup;  // columns that an XCD's compute units have at once
 };
 // wait_dma, unless `no` is above zero (wave-uniform)
 template <int N> __device__ __forceinline__ void wait_dma_unless(int no) {
@@ -143,7 +148,7 @@ template <int TA, int TB> __device__ __forceinline__ void run_tiles(const Mx4Par
         for (int j = 0; j < TB; ++j) s.b_off[j] = (uint32_t)(w * TB + j < last_c ? w * TB + j : last_c) * (uint32_t)KB * 1024u;
         return s;
     };
-    Mx4Tile tile = find_tile(p, kA, kB, rows, v), next_tile = tile;
+    Mx4Tile tile = find_tile<Shape::kTurn>(p, kA, kB, rows, v), next_tile = tile;
     Source src = source(tile), next_src = src;
     auto scalar = [](const Source &s) {
         auto u32 = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
@@ -216,7 +221,7 @@ template <int TA, int TB> __device__ __forceinline__ void run_tiles(const Mx4Par
     auto look_ahead = [&]() {
         const int n = v + stride;
         if (n < all) {
-            next_tile = find_tile(p, kA, kB, rows, n);
+            next_tile = find_tile<Shape::kTurn>(p, kA, kB, rows, n);
             next_src = source(next_tile);
         } else {
             next_src = source(tile);
@@ -437,7 +442,7 @@ template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::
 template <int RB, int CB, int WAVES> __global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(Mx4Params p) {
     __shared__ v4f_t part[WAVES][RB * CB][64];
     const int row_blocks = (int)((p.M + 15) / 16), col_blocks = (int)(p.N / 16), pairs = p.KB / 2;
-    const Mx4Tile tile = find_tile(p, RB, CB, (row_blocks + RB - 1) / RB, blockIdx.x);
+    const Mx4Tile tile = find_tile<0>(p, RB, CB, (row_blocks + RB - 1) / RB, blockIdx.x);
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint8_t *a_src[RB], *b_src[CB], *sa_src[RB], *sb_src[CB];
 #pragma unroll
