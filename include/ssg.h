@@ -482,7 +482,7 @@ ssg_status ssg_moe_view_workspace(const ssg_moe_desc *desc, const void *workspac
  * ssg_mx4_dequantize: the values that the codes stand for, exact in both types, into dst [rows, K], rows `ld` elements apart on 16 bytes; what
  * lies between rows is left alone.
  * ssg_mx4_pack: from codes [rows, K / 2], the even column's in the low half of a byte, on 8 bytes, and scales [rows, (K + 31) / 32] that a program
- * has already; ssg_mx4_unpack the way back; K a multiple of 16. */
+ * has already, of any value (253 and 254 are scales like the others; their values may be infinite); ssg_mx4_unpack the way back; K a multiple of 16. */
 typedef enum { SSG_MX_FLOOR = 0, SSG_MX_CEIL = 1 } ssg_mx_rule;
 size_t ssg_mx4_bytes(int64_t rows, int64_t K);
 ssg_status ssg_mx4_quantize(const void *src, ssg_dtype src_dtype, int64_t rows, int64_t K, int64_t ld, int transposed, ssg_mx_rule rule, void *q,
@@ -504,7 +504,7 @@ ssg_status ssg_mx4_linear(const void *x, ssg_dtype x_dtype, int64_t M, int64_t K
                           int64_t N, void *y, ssg_dtype y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
 /* Its backward pass, straight through every quantization: each product's operands are quantized in blocks along the axis that it sums over,
  *     dx = Q(dy) Q(W^T)^T  (blocks along N)        dW = Q(dy^T) Q(x^T)^T  (blocks along the M rows)
- * dy [M,N], x [M,K], dx [M,K], dW [N,K]; M any number, also 0 (dW is zeros then).  Wt: W^T quantized, K rows of N (ssg_mx4_quantize of W with
+ * dy [M,N], x [M,K], dx [M,K], dW [N,K]; M up to 2^24, also 0 (dW is zeros then).  Wt: W^T quantized, K rows of N (ssg_mx4_quantize of W with
  * transposed = 1).  dx or dW may be NULL: that product, and what it alone needs (Wt; x), is left out. */
 size_t ssg_mx4_linear_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K);
 ssg_status ssg_mx4_linear_bwd(const void *dy, ssg_dtype dy_dtype, int64_t lddy, const void *x, ssg_dtype x_dtype, int64_t ldx, int64_t M, int64_t N,

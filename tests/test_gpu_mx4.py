@@ -272,3 +272,26 @@ def test_linear_bwd_of_mixed_types(dy_dtype, x_dtype, dx_dtype, dw_dtype, rule, 
     for out, t, p, q, n in ((dx, dx_dtype, a, wt, N), (dW, dw_dtype, b, xt, M)):
         want, off = p @ q.T, n * 2.0 ** -23 * (np.abs(p) @ np.abs(q).T)
         assert (np.abs(f32(out) - want) <= off + (2.0 ** -8 * (np.abs(want) + off) if t == torch.bfloat16 else 0)).all()
+
+
+@pytest.mark.parametrize("low_a,high_a,low_b,high_b", [(-127, -107, 105, 125), (105, 125, -127, -107), (-127, -100, -40, 0), (-70, -66, -70, -66), (-127, -100, -127, -100)])
+@pytest.mark.parametrize("M,N,K", [(3, 48, 4112), (40, 272, 2736), (300, 528, 1376), (1100, 1040, 640)])
+def test_products_over_the_range_of_scales(M, N, K, low_a, high_a, low_b, high_b):
+    """As with scales far apart; a partial sum below 2^-126 is rounded to a multiple of 2^-149, or away, with half of that beside the rest."""
+    qa, a = operand(M, K, 1, low_a, high_a)
+    qb, b = operand(N, K, 2, low_b, high_b)
+    got = product(qa, M, qb, N, K, torch.float32).astype(np.float64)
+    assert (np.abs(got - a @ b.T) <= K * (2.0 ** -23 * (np.abs(a) @ np.abs(b).T) + 2.0 ** -150)).all()
+
+
+def test_values_beyond_the_types():
+    """Bytes that only another program's scales have: values behind the largest number are infinite, 255 is no number."""
+    codes, scales = np.tile(np.arange(16, dtype=np.uint8), (4, 2)), np.array([[252], [253], [254], [255]], np.uint8)
+    c, s = mx4.layout(codes, scales)
+    q = buffer(4, 32, 0)
+    q[:c.size + s.size] = torch.from_numpy(np.concatenate([c, s])).to(DEV)
+    for dtype in BOTH:
+        out = torch.empty(4, 32, dtype=dtype, device=DEV)
+        ssg.ssg_mx4_dequantize(q, 4, 32, out, SSG[dtype], 32)
+        with np.errstate(over="ignore"):
+            assert np.array_equal(f32(out), mx4.values(codes, scales).astype(np.float32), equal_nan=True)
