@@ -505,7 +505,8 @@ ssg_status ssg_mx4_linear(const void *x, ssg_dtype x_dtype, int64_t M, int64_t K
 /* Its backward pass, straight through every quantization: each product's operands are quantized in blocks along the axis that it sums over,
  *     dx = Q(dy) Q(W^T)^T  (blocks along N)        dW = Q(dy^T) Q(x^T)^T  (blocks along the M rows)
  * dy [M,N], x [M,K], dx [M,K], dW [N,K]; M up to 2^24, also 0 (dW is zeros then).  Wt: W^T quantized, K rows of N (ssg_mx4_quantize of W with
- * transposed = 1).  dx or dW may be NULL: that product, and what it alone needs (Wt; x), is left out. */
+ * transposed = 1).  dx or dW may be NULL: that product, and what it alone needs (Wt; x), is left out.  The same call gives the same bits; without
+ * the other product a sum's order, and with it its last bits, may be another's. */
 size_t ssg_mx4_linear_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K);
 ssg_status ssg_mx4_linear_bwd(const void *dy, ssg_dtype dy_dtype, int64_t lddy, const void *x, ssg_dtype x_dtype, int64_t ldx, int64_t M, int64_t N,
                               int64_t K, ssg_mx_rule rule, const void *Wt, size_t Wt_bytes, void *dx, ssg_dtype dx_dtype, int64_t lddx, void *dW,

@@ -241,6 +241,13 @@ def test_linear_bwd(which, dtype, M, N, K, gap):
             assert np.array_equal(got[:-1, :K], as_type(want, t)) and (got[:, K:] == 3).all() and (got[-1] == 3).all()
 
 
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("M,N,K", [(3, 768, 1120), (61, 1696, 2192), (256, 4096, 2064), (740, 2352, 1120), (1776, 1216, 128), (700, 64, 4112), (105, 4864, 384)])
+def test_linear_bwd_in_one_launch(dtype, M, N, K):
+    """Either product's sum the longer, from one tile to more than the chip holds; the last one in two launches."""
+    test_linear_bwd("both", dtype, M, N, K, 8)
+
+
 @pytest.mark.parametrize("M,K", [(1, 92160), (1, 92416), (1, 94208), (2, 46080), (3, 30976), (4, 23040), (4, 23056)])
 def test_long_rows_of_few_tokens(M, K):
     """On both sides of what a workgroup quantizes itself.  Scales of 1: terms of at most 36, whole numbers of quarters, whose sums stay below 2^24 quarters."""
