@@ -642,14 +642,15 @@ static Mx4Params params_of(const Mx4GemmArgs &a, Mx4Form form) {
 
 // Two products in tiles of 128 in one launch, a tile to a workgroup and the one with the longer sum first, so that its few long tiles run beside the
 // other's.  Backward passes of M rows, N -> K, whole, in two launches and in one: 2383 x 4688 -> 288 34.8 26.0 us; 586 x 3696 -> 2816 34.3 29.0; 256 x 4096 -> 4096
-// 28.1 21.9; 777 x 2064 -> 1376 23.9 19.2; 48 x 768 -> 2512 11.2 8.9; over 70 of 1 to 2048 rows and 64 to 12000 columns 11 % less time, at worst 14 % more (1070 x 128 -> 288 9.9 11.3).
-// A long sum that blocks of few rows share out takes longer in tiles (.33 us a step for about .1), which does not pay beside a short launch (105 x 4864 -> 384
+// 28.1 21.9; 777 x 2064 -> 1376 23.9 19.2; 48 x 768 -> 2512 11.2 8.9; over 70 of 1 to 2048 rows and 64 to 12000 columns 11 % less time, at worst 9 % more (1070 x 128 -> 288 9.9 10.8).
+// A long sum that blocks of few rows share out takes longer in tiles (.33 us a step; .05 in blocks of 16 x 16, .2 in 64 x 64), which does not pay beside a short launch (105 x 4864 -> 384
 // 13.1 17.1, 141 x 7136 -> 112 13.4 20.2).  Large tiles keep their launches.
 static bool in_one_launch(const Mx4GemmArgs &longer, const Mx4GemmArgs &other) {
     const Mx4Form form = choose_form(longer);
     if (form > TILE_128 || choose_form(other) > TILE_128) return false;
     const double KB = (double)(mx4_width(longer.K) / 128), other_KB = (double)(mx4_width(other.K) / 128);
-    return form == TILE_128 || .33 * KB + 1.5 <= .1 * KB + 3 + std::max(5., (double)count_of(other, TILE_128) / 512 * (.51 * other_KB + 5) + 1);
+    const double few = 3.5 + KB * std::sqrt((double)kExtents[form].rows * kExtents[form].cols) / 320;
+    return form == TILE_128 || .33 * KB + 1.5 <= few + std::max(5., (double)count_of(other, TILE_128) / 512 * (.51 * other_KB + 5) + 2);
 }
 void launch_mx4_gemm_pair(const Mx4GemmArgs &a, const Mx4GemmArgs &b, hipStream_t st) {
     const Mx4GemmArgs &longer = b.K > a.K ? b : a, &other = b.K > a.K ? a : b;
