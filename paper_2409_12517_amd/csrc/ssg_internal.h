@@ -423,8 +423,7 @@ struct Mx4GemmArgs {
 I8Plan mx4_gemm_plan(const Mx4GemmArgs &a);
 void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st);
 void launch_mx4_gemm_pair(const Mx4GemmArgs &a, const Mx4GemmArgs &b, hipStream_t st);      // two products that do not depend on each other
-// up to kMx4TokenRows rows of x, quantized in the product's own kernel
-constexpr int kMx4TokenRows = 4;
+// few rows of x, quantized in the product's own kernel
 constexpr int64_t kMx4TokenLds = 48 << 10;
 struct Mx4TokenArgs {
     const void *x = nullptr;         // rows of K, `ld` elements apart
@@ -433,7 +432,7 @@ struct Mx4TokenArgs {
     int64_t N = 0, K = 0, ld = 0, ldc = 0;
     int rows = 1, bf16 = 0, c_f32 = 0, ceil = 0;
 };
-bool mx4_token_ok(int64_t M, int64_t K);
+bool mx4_token_ok(int64_t M, int64_t N, int64_t K);
 void launch_mx4_token(const Mx4TokenArgs &a, hipStream_t st);
 constexpr int kTagMx4Rows = 55, kTagMx4Gemm = 56, kTagNorm = 57, kTagNormBwd = 58;
 

@@ -516,7 +516,7 @@ template <int RB, int CB, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
     }
 }
 
-// ---- up to four rows, quantized on the way ------------------------------------------------------------------
+// ---- few rows, quantized on the way ---------------------------------------------------------------------------
 // 16 columns to a workgroup, whose waves share K out.  Its threads quantize the rows, a block each, into LDS while the first weights are on their way.
 // (In the registers of the lanes that multiply them, where four of 64 have a row's values, the vector ALU took 3 us: 1 x 4096 -> 11008
 // 10.6 us for 7.5.)  Bound by the weights' bytes, 24 MB there, and the start and end of one round of workgroups.
@@ -694,7 +694,13 @@ void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st) {
 }
 
 static int64_t token_lds(int64_t M, int64_t K) { return M * (mx4_width(K) / 32 * 17); }
-bool mx4_token_ok(int64_t M, int64_t K) { return M <= kMx4TokenRows && token_lds(M, K) <= kMx4TokenLds; }
+// Every workgroup quantizes all rows, which costs .22 us a row of 4096 for each round of workgroups, and a launch before it 2 (more where launches cost
+// the host time).  Microseconds of both, 5, 8 and 12 rows: 4096 -> 4096 5.4 6.4, 6.0 6.4, 6.9 6.4; 1024 -> 1024 3.6 4.9, 3.6 4.9, 3.9 5.0; 2736 -> 1040 4.2 5.4,
+// 4.5 5.5, 5.0 5.4; 4096 -> 11008 9.8 9.2, 11.7 9.2, 14.0 9.2.
+bool mx4_token_ok(int64_t M, int64_t N, int64_t K) {
+    if (M > 16 || token_lds(M, K) > kMx4TokenLds) return false;
+    return M <= 4 || M * K * std::max<int64_t>(N, 4096) <= (int64_t)9 << 24;
+}
 
 void launch_mx4_token(const Mx4TokenArgs &a, hipStream_t st) {
     profile_before(kTagMx4Gemm, st);

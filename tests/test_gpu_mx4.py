@@ -206,7 +206,14 @@ def test_linear(rule, x_dtype, y_dtype, M, N, K, gap):
     assert np.array_equal(got[:M, :N], want) and (got[:, N:] == 3).all() and (got[M] == 3).all()
 
 
-@pytest.mark.parametrize("M", [1, 4])
+@pytest.mark.parametrize("x_dtype,y_dtype", [(torch.bfloat16, torch.float32), (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("M,N,K", [(5, 48, 16), (7, 4096, 5264), (7, 4112, 5264), (8, 272, 528), (9, 4096, 4096), (9, 16, 4112), (13, 1040, 2736), (16, 16, 2304), (16, 272, 2320), (16, 528, 784)])
+def test_linear_of_few_rows(x_dtype, y_dtype, M, N, K):
+    """On both sides of where the product's own launch quantizes the rows."""
+    test_linear(ssg.SSG_MX_CEIL, x_dtype, y_dtype, M, N, K, 8)
+
+
+@pytest.mark.parametrize("M", [1, 4, 9, 16])
 def test_token_with_no_number(M):
     x = torch.ones(M, 512)
     x[M - 1, 300] = torch.inf
