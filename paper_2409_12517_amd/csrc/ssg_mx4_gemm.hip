@@ -435,6 +435,20 @@ template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::
     run_tiles<TA, TB>(p, smem, (int)blockIdx.x - (in_first ? 0 : first), gridDim.x);
 }
 
+// Two products one after the other in the same workgroups.  The second's tiles are counted from the last workgroup, so that those that had one more
+// of the first product's have one less of them.  Backward passes of M rows, N -> K, whole, in two launches and in this one: 4096 x 11008 -> 4096 239 233 us;
+// 5000 x 2736 -> 8192 185 170; 5608 x 8704 -> 4432 278 251; 3212 x 2416 -> 11136 166 153; of 20 large ones 2 % less time, at worst 1.4 % more.  (Half of
+// the workgroups with the products the other way round, so that results of some are stored while others multiply: 1.5 % less, at worst 13 % more.)
+template <int TA, int TB> __global__ __launch_bounds__(256, (TileShape<TA, TB>::kAtOnce)) void mx4_tile_both_kernel(Mx4Params a, Mx4Params b) {
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[TileShape<TA, TB>::kLds];
+#pragma nounroll
+    for (int i = 0; i < 2; ++i) {
+        const Mx4Params p = i ? b : a;
+        run_tiles<TA, TB>(p, smem, i ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x, gridDim.x);
+        __syncthreads();                                 // (every wave is through with the first one's LDS)
+    }
+}
+
 // ---- few rows ------------------------------------------------------------------------------------------
 // RB blocks of 16 rows by CB blocks of 16 columns to a workgroup, whose waves share K out in pairs of blocks and add their sums in LDS, wave after
 // wave.  Both operands come straight from memory in the order of the lanes, U pairs' loads at a time.  Bound by the weights' bytes and by the start
@@ -644,7 +658,7 @@ static Mx4Params params_of(const Mx4GemmArgs &a, Mx4Form form) {
 // other's.  Backward passes of M rows, N -> K, whole, in two launches and in one: 2383 x 4688 -> 288 34.8 26.0 us; 586 x 3696 -> 2816 34.3 29.0; 256 x 4096 -> 4096
 // 28.1 21.9; 777 x 2064 -> 1376 23.9 19.2; 48 x 768 -> 2512 11.2 8.9; over 70 of 1 to 2048 rows and 64 to 12000 columns 11 % less time, at worst 9 % more (1070 x 128 -> 288 9.9 10.8).
 // A long sum that blocks of few rows share out takes longer in tiles (.33 us a step; .05 in blocks of 16 x 16, .2 in 64 x 64), which does not pay beside a short launch (105 x 4864 -> 384
-// 13.1 17.1, 141 x 7136 -> 112 13.4 20.2).  Large tiles keep their launches.
+// 13.1 17.1, 141 x 7136 -> 112 13.4 20.2).
 static bool in_one_launch(const Mx4GemmArgs &longer, const Mx4GemmArgs &other) {
     const Mx4Form form = choose_form(longer);
     if (form > TILE_128 || choose_form(other) > TILE_128) return false;
@@ -658,6 +672,13 @@ void launch_mx4_gemm_pair(const Mx4GemmArgs &a, const Mx4GemmArgs &b, hipStream_
         const int first = (int)count_of(longer, TILE_128), all = first + (int)count_of(other, TILE_128);
         profile_before(kTagMx4Gemm, st);
         hipLaunchKernelGGL((mx4_tile_pair_kernel<2, 2>), dim3(all), dim3(256), 0, st, params_of(longer, TILE_128), params_of(other, TILE_128), first);
+        profile_after(st);
+        return;
+    }
+    if (a.M > 0 && b.M > 0 && a.K > 0 && b.K > 0 && choose_form(a) == TILE_256 && choose_form(b) == TILE_256) {
+        profile_before(kTagMx4Gemm, st);
+        const unsigned all = (unsigned)std::min<int64_t>(std::max(count_of(a, TILE_256), count_of(b, TILE_256)), 256);
+        hipLaunchKernelGGL((mx4_tile_both_kernel<4, 4>), dim3(all), dim3(256), 0, st, params_of(a, TILE_256), params_of(b, TILE_256));
         profile_after(st);
         return;
     }

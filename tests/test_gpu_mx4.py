@@ -255,6 +255,27 @@ def test_linear_bwd_in_one_launch(dtype, M, N, K):
     test_linear_bwd("both", dtype, M, N, K, 8)
 
 
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("M,N,K", [(1570, 4112, 8032), (4096, 4096, 4096), (3300, 2416, 11136), (1570, 7600, 8032)])
+def test_linear_bwd_in_large_tiles(dtype, M, N, K):
+    """Both products, of one and of several rounds of large tiles and of different numbers of them, against each alone (every sum is exact, see above)."""
+    assert ssg.ssg_mx4_gemm_plan(M, K, N).tile == ssg.ssg_mx4_gemm_plan(N, K, M).tile == 256
+    dy, x = exact_rows(M, N, 1, dtype), exact_rows(M, K, 2, dtype)
+    dy[::32], x[::32] = (torch.where(torch.rand(-(-M // 32), n, generator=torch.Generator().manual_seed(3)) < 0.5, 4.0, 8.0).to(dtype) for n in (N, K))
+    dy, x, qt = dy.to(DEV), x.to(DEV), buffer(K, N)
+    ssg.ssg_mx4_quantize(exact_rows(K, N, 5, torch.float32).to(DEV), ssg.SSG_F32, K, N, N, 0, 0, qt)
+    work = buffer(1, 1).new_full((ssg.ssg_mx4_linear_bwd_workspace_bytes(M, N, K),), 0xA5)
+
+    def run(with_dx, with_dW):
+        dx, dW = torch.full((M + 1, K), 3.0, dtype=dtype, device=DEV), torch.full((N + 1, K), 3.0, device=DEV)
+        ssg.ssg_mx4_linear_bwd(dy, SSG[dtype], N, x, SSG[dtype], K, M, N, K, 0, qt, dx if with_dx else None, SSG[dtype], K, dW if with_dW else None, ssg.SSG_F32, K, work)
+        return dx, dW
+
+    dx, dW = run(True, True)
+    assert torch.equal(dx, run(True, False)[0]) and torch.equal(dW, run(False, True)[1])
+    assert bool((dx[M] == 3).all()) and bool((dW[N] == 3).all())
+
+
 @pytest.mark.parametrize("M,K", [(1, 92160), (1, 92416), (1, 94208), (2, 46080), (3, 30976), (4, 23040), (4, 23056)])
 def test_long_rows_of_few_tokens(M, K):
     """On both sides of what a workgroup quantizes itself.  Scales of 1: terms of at most 36, whole numbers of quarters, whose sums stay below 2^24 quarters."""
