@@ -182,19 +182,22 @@ Mx4Both both_args(const Mx4RowsArgs &t, const Mx4RowsArgs *rows) {
     return b;
 }
 
-// The values that the codes stand for.  (Exact in fp32, and in bf16: 0 to 6 times a power of two from 2^-127 up.)  A wave has 16 rows by 256 columns
-// and stores 16 bytes to a lane side by side along a row, 256 (512) bytes of four (two) rows at a time; the codes, 4 (2) bytes to a lane, come out of
-// the cache lines of a 1 KB block.  Bound by memory: 4096 x 11008 to bf16 25 us, 4.5 TB/s (41 with 64 bytes of a row to a lane), to fp32 55, 3.7.
-template <bool BF16> __global__ __launch_bounds__(256) void mx4_values_kernel(Mx4ValuesArgs a) {
-    constexpr int kEach = BF16 ? 8 : 4, kLanes = 128 / kEach, kRowsAtOnce = 64 / kLanes, kSteps = 16 / kRowsAtOnce;      // values of a lane, lanes to 128 columns
-    const int64_t pairs = mx4_width(a.K) / 256, wave = block_of_many() * 4 + threadIdx.x / 64, rb = wave / pairs, p = wave % pairs;
-    if (rb * 16 >= a.rows) return;
-    const int l = threadIdx.x & 63, c = l % kLanes * kEach, g = c / 32;      // column of the 128, its run of 32
+// The values that the codes stand for.  (Exact in fp32, and in bf16: 0 to 6 times a power of two from 2^-127 up.)  A wave has 16 rows by 256 columns, or one of
+// PARTS shares of the rows, and stores 16 bytes to a lane side by side along a row, 256 (512) bytes of four (two) rows at a time; the codes, 4 (2) bytes to a lane, come out of
+// the cache lines of a 1 KB block.  Bound by memory: 4096 x 11008 to bf16 25 us, 4.5 TB/s (41 with 64 bytes of a row to a lane), to fp32 55, 3.7;
+// little ones by latency: 75 x 2736 in one, two and four parts 2.8 2.4 2.3, to fp32 3.8 2.9 2.5 (four waves to a block 3.0 and 4.2); 333 x 11008 4.3 4.0 4.0
+// and 6.7 6.2 6.1; 4096 x 4096 8.7 7.9 9.1 and 16.5 20.8 19.7.
+template <bool BF16, int PARTS> __global__ __launch_bounds__(64) void mx4_values_kernel(Mx4ValuesArgs a) {
+    constexpr int kEach = BF16 ? 8 : 4, kLanes = 128 / kEach, kRowsAtOnce = 64 / kLanes, kRows = 16 / PARTS, kSteps = kRows / kRowsAtOnce;      // values of a lane, lanes to 128 columns
+    const int64_t pairs = mx4_width(a.K) / 256, wave = block_of_many() / PARTS, rb = wave / pairs, p = wave % pairs;
+    const int first = (int)(block_of_many() % PARTS) * kRows;
+    if (rb * 16 + first >= a.rows) return;
+    const int l = threadIdx.x, c = l % kLanes * kEach, g = c / 32;      // column of the 128, its run of 32
     const uint8_t *codes = a.codes + (rb * pairs + p) * 2048 + g * 256 + c % 32 / 2, *scales = a.scales + (rb * pairs + p) * 128 + g * 32;
     uint32_t word[2][kSteps], bytes[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        const int r = i * kRowsAtOnce + l / kLanes;
+        const int r = first + i * kRowsAtOnce + l / kLanes;
         bytes[i] = *reinterpret_cast<const uint16_t *>(scales + r * 2);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -204,7 +207,7 @@ template <bool BF16> __global__ __launch_bounds__(256) void mx4_values_kernel(Mx
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const int64_t row = rb * 16 + i * kRowsAtOnce + l / kLanes, k = p * 256 + h * 128 + c;
+            const int64_t row = rb * 16 + first + i * kRowsAtOnce + l / kLanes, k = p * 256 + h * 128 + c;
             const uint32_t byte = bytes[i] >> 8 * h & 255u;
             const float scale = byte == 255u ? __uint_as_float(0x7fc00000u) : mx4_scale(byte);
             float v[kEach];
@@ -313,8 +316,12 @@ void launch_mx4_quantize_bwd(const Mx4RowsArgs *rows, const Mx4RowsArgs &dy, con
 void launch_mx4_dequantize(const Mx4ValuesArgs &a, hipStream_t st) {
     if (a.rows == 0) return;
     profile_before(kTagMx4Rows, st, (double)a.rows * a.K * (a.bf16 ? 2 : 4) + (double)(mx4_code_bytes(a.rows, a.K) + mx4_scale_bytes(a.rows, a.K)));
-    if (a.bf16) hipLaunchKernelGGL(mx4_values_kernel<true>, grid_of_pairs(a.rows, a.K), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(mx4_values_kernel<false>, grid_of_pairs(a.rows, a.K), dim3(256), 0, st, a);
+    const int64_t pairs = (a.rows + 15) / 16 * (mx4_width(a.K) / 256);
+    auto go = [&](auto kernel, int64_t blocks) { hipLaunchKernelGGL(kernel, grid_of_many(blocks), dim3(64), 0, st, a); };
+    if (a.bf16 && pairs < 1024) go(mx4_values_kernel<true, 4>, 4 * pairs);
+    else if (a.bf16) go(mx4_values_kernel<true, 2>, 2 * pairs);
+    else if (pairs < 1024) go(mx4_values_kernel<false, 4>, 4 * pairs);
+    else go(mx4_values_kernel<false, 1>, pairs);
     profile_after(st);
 }
 

@@ -46,7 +46,7 @@ def wide(x, gap, fill=7.0):
 
 @pytest.mark.parametrize("rule", [ssg.SSG_MX_FLOOR, ssg.SSG_MX_CEIL])
 @pytest.mark.parametrize("dtype", BOTH)
-@pytest.mark.parametrize("rows,K,gap", [(1, 16, 0), (1, 4096, 0), (15, 48, 8), (16, 256, 0), (17, 272, 16), (75, 2736, 0), (100, 1040, 8), (300, 528, 0)])
+@pytest.mark.parametrize("rows,K,gap", [(1, 16, 0), (1, 4096, 0), (15, 48, 8), (16, 256, 0), (17, 272, 16), (75, 2736, 0), (100, 1040, 8), (300, 528, 0), (1030, 4096, 8), (9000, 272, 0)])
 def test_quantize_rows(rule, dtype, rows, K, gap):
     x = spread(rows, K, rows + K).to(dtype)
     x[rows // 2, :32] = 0
@@ -93,7 +93,7 @@ def test_extremes(dtype, transposed):
 
 
 @pytest.mark.parametrize("dtype", BOTH)
-@pytest.mark.parametrize("rows,K", [(1, 1), (5, 16), (16, 31), (17, 300), (40, 1025)])
+@pytest.mark.parametrize("rows,K", [(1, 1), (5, 16), (16, 31), (17, 300), (40, 1025), (1030, 4085), (9000, 300)])
 def test_dequantize(dtype, rows, K):
     """Exact in both types, for every code and scale; what lies between rows and behind the last one stays."""
     rng = np.random.default_rng(rows + K)
