@@ -497,9 +497,10 @@ ssg_status ssg_mx4_gemm(const void *A, size_t A_bytes, int64_t M, const void *B,
                         ssg_dtype c_dtype, int64_t ldc, void *stream);
 /* Which kernel such a product runs in, as ssg_i8_gemm_plan. */
 ssg_status ssg_mx4_gemm_plan(int64_t M, int64_t N, int64_t K, ssg_gemm_plan *out);
-/* y = x W^T with x [M,K] quantized in the call; W: N rows of K, both multiples of 16.  Up to four rows, with M K up to 92160, and
- * up to 16, with M K max(N, 4096) up to 9 * 2^24, are quantized where they are multiplied, in the product's own launch; ssg_mx4_gemm_plan tells of the
- * products of more. */
+/* y = x W^T with x [M,K] quantized in the call; W: N rows of K, both multiples of 16.  Up to 16 rows are quantized where they are multiplied, in
+ * the product's own launch, if, with c = 2 for bf16 rows and 5 for fp32, K' = K filled up to 256 and N' = max(N, 4096),
+ *     17 M K' <= 32 * 49152    and    (c M - 6) K N' + 4 (N' - 4096) max(8192 - K, 0) <= 14 * 2^24;
+ * ssg_mx4_gemm_plan tells of the products of the others. */
 size_t ssg_mx4_linear_workspace_bytes(int64_t M, int64_t K);
 ssg_status ssg_mx4_linear(const void *x, ssg_dtype x_dtype, int64_t M, int64_t K, int64_t ldx, ssg_mx_rule rule, const void *W, size_t W_bytes,
                           int64_t N, void *y, ssg_dtype y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);

@@ -432,7 +432,7 @@ struct Mx4TokenArgs {
     int64_t N = 0, K = 0, ld = 0, ldc = 0;
     int rows = 1, bf16 = 0, c_f32 = 0, ceil = 0;
 };
-bool mx4_token_ok(int64_t M, int64_t N, int64_t K);
+bool mx4_token_ok(int64_t M, int64_t N, int64_t K, int bf16);
 void launch_mx4_token(const Mx4TokenArgs &a, hipStream_t st);
 constexpr int kTagMx4Rows = 55, kTagMx4Gemm = 56, kTagNorm = 57, kTagNormBwd = 58;
 

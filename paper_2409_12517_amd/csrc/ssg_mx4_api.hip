@@ -210,7 +210,7 @@ ssg_status ssg_mx4_linear(const void *x, ssg_dtype x_dtype, int64_t M, int64_t K
     SSG_CHECK(check_mx4_buffer(who, "W", W, W_bytes, N, K));
     SSG_CHECK(check_mx4_buffer(who, "workspace", workspace, workspace_bytes, M, K));
     SSG_CHECK(check_entry(who));
-    if (ssg::mx4_token_ok(M, N, K)) {
+    if (ssg::mx4_token_ok(M, N, K, x_dtype == SSG_BF16)) {
         ssg::Mx4TokenArgs t;
         t.x = x; t.B = mx4_codes(W); t.sb = mx4_scales(W, N, K); t.C = y; t.N = N; t.K = K; t.ld = ldx; t.ldc = ldy;
         t.rows = (int)M; t.bf16 = x_dtype == SSG_BF16; t.c_f32 = y_dtype == SSG_F32; t.ceil = rule == SSG_MX_CEIL;

@@ -715,12 +715,23 @@ void launch_mx4_gemm(const Mx4GemmArgs &a, hipStream_t st) {
 }
 
 static int64_t token_lds(int64_t M, int64_t K) { return M * (mx4_width(K) / 32 * 17); }
-// Every workgroup quantizes all rows, which costs .22 us a row of 4096 for each round of workgroups, and a launch before it 2 (more where launches cost
-// the host time).  Microseconds of both, 5, 8 and 12 rows: 4096 -> 4096 5.4 6.4, 6.0 6.4, 6.9 6.4; 1024 -> 1024 3.6 4.9, 3.6 4.9, 3.9 5.0; 2736 -> 1040 4.2 5.4,
-// 4.5 5.5, 5.0 5.4; 4096 -> 11008 9.8 9.2, 11.7 9.2, 14.0 9.2.
-bool mx4_token_ok(int64_t M, int64_t N, int64_t K) {
+// Every workgroup quantizes all rows, against a launch before the product.  Microseconds of both for rows in bf16, and in fp32 (weights from memory, calls of one graph):
+//                             1 row                 2                       4                       8                      16
+//   1024 ->  4096                            3.6 5.0   3.8 5.0       3.8 5.1   4.1 5.1       3.9 5.2   4.5 5.0       4.2 5.1   5.6 5.1
+//   4096 ->  4096     4.5 6.3   4.9 6.3      4.7 6.3   5.3 6.4       5.1 6.3   6.4 6.4       6.0 6.4   8.4 6.4       7.8 6.4  12.3 6.6
+//   1024 -> 11008     5.8 6.1   6.8 5.9      6.0 5.9   6.9 6.1       6.2 6.1   7.3 6.1       6.8 6.1   8.7 6.2       7.9 6.1  11.0 6.3
+//   4096 -> 11008     7.8 9.1   8.9 9.1      8.1 9.1  10.0 9.2       9.2 9.1  12.6 9.2      11.6 9.2  18.3 9.3      16.0 9.4  29.5 9.4
+//   8192 -> 11008    10.3 13.4 12.2 13.4    11.1 13.4 14.7 13.4     13.7 13.4 20.1 13.6     17.9 13.6 31.1 13.6
+//   1024 -> 28672    10.2 9.0  12.3 8.9     10.3 8.9  12.8 9.0      10.9 9.1  14.2 9.0      11.9 9.1  17.7 9.2      14.2 9.1  23.0 9.3
+//   8192 -> 28672    21.4 26.0 25.9 25.1    21.6 25.1 30.7 25.0     26.5 25.2 41.4 25.2
+//  11008 -> 28672    30.8 34.1 36.0 32.3    31.8 32.0 42.3 32.5     37.7 32.4 58.7 32.4
+// So a row costs its share of K in every round of 256 workgroups, 4096 columns, in fp32 2.5 times as much as in bf16; a further round costs its start, which long weights
+// hide; and a launch before the product saves less on longer K.  Over 580 pairs of figures, 1 to 16 rows, K 512 to 92160, N 1024 to 60000, the rule's choice takes .3 % more
+// than the better one on average, at worst 15 % (one fp32 row 1024 -> 11008).  (One launch for up to four rows of any length, and for more by M K N alone: 8 %, at worst 87.)
+bool mx4_token_ok(int64_t M, int64_t N, int64_t K, int bf16) {
     if (M > 16 || token_lds(M, K) > kMx4TokenLds) return false;
-    return M <= 4 || M * K * std::max<int64_t>(N, 4096) <= (int64_t)9 << 24;
+    const int64_t cols = std::max<int64_t>(N, 4096);
+    return ((bf16 ? 2 : 5) * M - 6) * K * cols + 4 * (cols - 4096) * std::max<int64_t>(8192 - K, 0) <= (int64_t)14 << 24;
 }
 
 void launch_mx4_token(const Mx4TokenArgs &a, hipStream_t st) {
