@@ -67,8 +67,8 @@ __device__ __forceinline__ void store4(const Mx4Params &p, int64_t row, int64_t 
 
 // ---- tiles through LDS -----------------------------------------------------------------------------------
 // 4 waves as 2 x 2, TA x TB blocks of 32 x 32 each.
-// Products of 32 x 32 x 64, which reach the chip's rate where 16 x 16 x 128 wait on their issue (registers alone, one wave to a SIMD, random codes: 6.2
-// and 4.2 PFLOP/s): a fragment is the blocks of two neighbouring 16 rows, half of each along K.
+// Products of 32 x 32 x 64, whose rate, with one wave to a SIMD, the power bounds where 16 x 16 x 128 wait on their issue (registers alone, random codes, launches of
+// .02 to 18 ms: 5.0 to 6.1 PFLOP/s and 3.7 to 5.2): a fragment is the blocks of two neighbouring 16 rows, half of each along K.
 // K advances in steps of 128 through a ring of kStages stages, each in two halves of 64.  The fragments of a half are read while the half before it is
 // multiplied, so when all waves have passed the barrier in the middle of step k, everything of its stage is in registers, and k + kStages is loaded
 // into it.  Two steps are a pair, whose scales go through a ring of their own, of two pairs: loaded before the pair's first stage, read into
@@ -77,7 +77,7 @@ __device__ __forceinline__ void store4(const Mx4Params &p, int64_t row, int64_t 
 // multiplied and its results stored, the first stages of the next are on their way.  A tile with no more rows than half
 // loads and multiplies half of them.
 // Bound by the matrix cores under the chip's power: 4096 x 4096 x 11008 takes 83 to 85 us, 4.4 PFLOP/s, the MFMAs half of the cycles at 2.1 GHz; without its
-// loads to LDS 75, without those, the reads and the stores 67, and MFMAs alone hold 5 to 6 PFLOP/s at 1.5 to 1.9 GHz on random codes; operands of zeros 59.  4096 x 11008 x 4096 99 us:
+// loads to LDS 75, without those, the reads and the stores 67; operands of zeros 59.  4096 x 11008 x 4096 99 us:
 // 688 tiles are 2.7 rounds of 256, and the stores of a round take half a step's time from the loads behind them.  8192^3 238 us, 4.6 PFLOP/s.  (16 x 16 x 128
 // MFMAs 103 us for 85; results through LDS and the wait for their stores before the next tile's first step 113 for 100; tiles of 128 x 256 twice on a
 // compute unit, three stages each, 91 for 85 and 110 for 100; non-temporal stores, groups of two or eight row tiles, loads all at once: within 4 %.)
@@ -85,7 +85,7 @@ constexpr int kStages = 4, kScaleSlots = 2;
 static_assert(kStages % 2 == 0, "a pair's scales come with the first of two stages, and a tile's last stage with the second of a pair of steps");
 template <int TA, int TB> struct TileShape {
     static constexpr int kA = 4 * TA, kB = 4 * TB;       // blocks of 16 rows, and of 16 columns, of the tile
-    static constexpr int kRows = 16 * kA, kCols = 16 * kB, kStage = (kA + kB) * 1024, kRing = kStages * kStage;
+    static constexpr int kStage = (kA + kB) * 1024, kRing = kStages * kStage;
     static constexpr int kScales = (kA + kB) * 128;      // of a pair: the rows', then the columns'
     static constexpr int kLds = kRing + kScaleSlots * kScales, kAtOnce = 163840 / kLds;
     static constexpr int kTurn = 32 * kAtOnce / kGroup;  // columns that an XCD's compute units have at once
@@ -533,7 +533,9 @@ template <int RB, int CB, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
 // ---- few rows, quantized on the way ---------------------------------------------------------------------------
 // 16 columns to a workgroup, whose waves share K out.  Its threads quantize the rows, a block each, into LDS while the first weights are on their way.
 // (In the registers of the lanes that multiply them, where four of 64 have a row's values, the vector ALU took 3 us: 1 x 4096 -> 11008
-// 10.6 us for 7.5.)  Bound by the weights' bytes, 24 MB there, and the start and end of one round of workgroups.
+// 10.6 us for 7.7.)  Bound by the weights' bytes, 24 MB there, 4.7 us, by the start and end of one round of workgroups, and by loads that nothing needs: U pairs are asked
+// for at a time whatever a wave's share is, those beyond it its last one again (32 pairs for 16 at K = 4096, 60 for 43 at 11008).  The rows in LDS lie a multiple of 128
+// bytes apart, so that the rows of 16 lanes share banks.
 template <bool BF16, int WAVES> __global__ __launch_bounds__(64 * WAVES) void mx4_token_kernel(Mx4TokenArgs a) {
     constexpr int U = 4;                                     // pairs of blocks at a time
     extern __shared__ __attribute__((aligned(16))) uint8_t codes[];          // rows of Kp / 2, then their scales, rows of Kp / 32

@@ -9,7 +9,7 @@ namespace {
 
 // A wave has 16 rows by 256 columns, or with HALVES = 1 by 128: lane l row l % 16 and in each half the l / 16-th run of 32, so that the codes of a half leave
 // as one piece of 1 KB and the scales as one of 128 bytes (of 64 pieces of one where there is one half).  (A lane's four loads of 16 bytes take the same
-// cache lines.)  Bound by memory: 4096 x 11008 bf16, 114 MB, 22.4 us, 5.1 TB/s, what a large copy reaches; little ones by latency, so a wave is a block by itself, on
+// cache lines.)  Bound by memory: 4096 x 11008 bf16, 114 MB, 22 to 24 us, fp32, 204 MB, 43, 4.8 TB/s; little ones by latency, so a wave is a block by itself, on
 // any compute unit, and has one half where there are few: 333 x 2736 bf16 2.5 us, two halves 2.6, four waves to a block 2.9, in fp32 3.1, 3.0 and 4.0;
 // 64 x 4096 fp32 2.4, 2.7 and 4.0; 1024 x 4096 bf16 4.1, 4.3 and 4.1; 4096 x 4096 8.6, 8.2 and 8.3.
 template <bool BF16, int HALVES> __global__ __launch_bounds__(64) void mx4_rows_kernel(Mx4RowsArgs a) {
@@ -36,7 +36,7 @@ template <bool BF16, int HALVES> __global__ __launch_bounds__(64) void mx4_rows_
 // The transpose, and with it the rows where both are wanted: a block has 64 of the source's rows (tokens) by 512 bytes of each.  Its threads read pieces of
 // 16 bytes, form the rows' codes from them, four neighbouring threads a block of 32, and leave them in LDS, out of which a thread takes 32
 // tokens of a column, or of two in bf16, and forms theirs.  The tokens and columns that fill the layouts up are zeros.  Bound by memory: the transpose of
-// 4096 x 11008 bf16 23.7 us (38.6 with 32 tokens of eight columns in a thread's registers, too few of them to hide their two rounds of loads); the three
+// 4096 x 11008 bf16 24 to 25 us, 4.6 TB/s, fp32 42, 4.9 (bf16 30 beside a kernel that writes 90 MB before it; 38.6 with 32 tokens of eight columns in a thread's registers, too few of them to hide their two rounds of loads); the three
 // operands of a backward pass at 4096 x 4096 x 11008, 180 MB, 40 us, 4.5 TB/s (50 with the exchanges among four lanes through LDS).
 constexpr int kTileTokens = 64;
 struct Mx4Both {
@@ -240,7 +240,8 @@ template <bool BF16, int PARTS> __global__ __launch_bounds__(64) void mx4_values
         }
 }
 
-// Row-major codes [rows, K / 2] and scales [rows, (K + 31) / 32] into the layout and back; K a multiple of 16.
+// Row-major codes [rows, K / 2] and scales [rows, (K + 31) / 32] into the layout and back; K a multiple of 16.  Bound by memory at sizes that matter, done once for
+// a program's weights: 4096 x 11008, 48 MB, 11.4 us and 12.7 back, 4.2 and 3.8 TB/s.
 __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t K, uint8_t *out, uint8_t *out_scales) {
     const int64_t pairs = mx4_width(K) / 256, wave = block_of_many() * 4 + threadIdx.x / 64, rb = wave / pairs, p = wave % pairs;
     if (rb * 16 >= rows) return;

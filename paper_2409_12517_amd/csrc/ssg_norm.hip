@@ -95,7 +95,7 @@ enum { OUT_ROWS, OUT_I8, OUT_MX4 };
 
 // RES: 0 no residual, 1 in bf16, 2 in fp32.  OUT_I8 and OUT_MX4 write the rows and columns that fill the layout up, too.
 // One pass: a row stays in registers between its squares and its results.  Bound by memory: 16384 x 4096 bf16 with a bf16 residual to bf16, 537 MB, 94 us,
-// 5.7 TB/s; 131072 x 128 13 us; 4096 x 4096 with an fp32 residual into 4 bits, 177 MB, 41 us, 4.3 TB/s; one row of 4096 3.8 us, a launch and the row's latency.
+// 5.7 TB/s; 131072 x 128 13 us; 4096 x 4096 with an fp32 residual into 4 bits, 177 MB, 42 us, 4.2 TB/s; one row of 4096 3.7 us, a launch and the row's latency.
 template <bool XBF16, int RES, int OUT, class SHARE, int HELD> __global__ __launch_bounds__(SHARE::kThreads) void norm_kernel(NormArgs a) {
     constexpr int ROWS = SHARE::kRows;
     __shared__ float sums[2][SHARE::kWaves][ROWS];
@@ -282,9 +282,9 @@ template <bool XBF16, int RES> void launch_norm_as(const NormArgs &a, hipStream_
 
 // ---- the gradient ------------------------------------------------------------------------------------------
 // A block takes rows by a fixed stride and keeps its columns' sums of dy n in registers; they leave as one row of `partial`.  Bound by memory: 16384 x 4096
-// bf16 with the residual's gradient, 671 MB, 125 us, 5.4 TB/s; 1023 x 2736 in fp32, 56 MB, 13 us, and 3.6 for the second launch.  A thread has one run of a row
+// bf16 with the residual's gradient, 671 MB, 125 us, 5.4 TB/s; 1023 x 2736 in fp32, 56 MB, 13 us, and 4 for the second launch.  A thread has one run of a row
 // where 1024 threads reach (1023 x 2736: 512 threads with one run 15.2 us for both launches, 256 with two 16.5).  Blocks for one round of the chip:
-// 512 of up to 768 threads, 256 of 1024 (16384 x 4096 bf16: 256 blocks 115 us, 512 76, 1024 83; 4096 x 11008: 256 60, 512 66, 1024 75).
+// 512 up to 6144 columns, of up to 768 threads, 256 of wider rows, of 1024 threads or of 512 with several runs each (16384 x 4096 bf16: 256 blocks 115 us, 512 76, 1024 83; 4096 x 11008: 256 60, 512 66, 1024 75).
 template <bool DYBF16, bool SBF16, class SHARE, int HELD> __global__ __launch_bounds__(SHARE::kThreads) void norm_bwd_kernel(NormBwdArgs a) {
     constexpr int ROWS = SHARE::kRows, C = SHARE::kCols;
     __shared__ float sums[2][SHARE::kWaves][ROWS];
